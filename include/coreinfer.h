@@ -452,6 +452,147 @@ int coreinfer_ffn_dense_hidden(const void* X, int64_t M, const void* w_up, const
                                int dtype, int act, int64_t d, int64_t N, void* Y, void* H, void* ws,
                                size_t ws_bytes, void* stream);
 
+/*
+ * ---------------------------------------------------------------------------
+ * Serving in 4 bits: weights and a key-value cache that take a quarter of the
+ * 16-bit bytes, for decode steps, which are bound by the bytes they read.
+ *
+ * Both are held in groups of `group` (32, 64 or 128) neighbouring elements of a
+ * row.  A group x_0 .. x_{g-1} has
+ *     low  = fp16(min x),   step = fp16((max x - min x) / 15),
+ *     n_i  = rint((x_i - low) / step) within 0 .. 15   (0 where step is 0),
+ * differences and quotients in fp32 and values beyond +-65504 held there, and
+ * stands for low + step n_i.  A NaN makes low and step, and so the whole group, NaN.
+ * A last group that the row does not fill ranges over what there is of it.
+ * ---------------------------------------------------------------------------
+ */
+#define CI_MAX_W4_ROWS 64            /* M of coreinfer_w4_matvec                  */
+#define CI_MAX_CACHE_SLOTS 16777216  /* slots of a sentence in a cache            */
+#define CI_ACT_NONE 2                /* no activation: coreinfer_w4_matvec only   */
+
+/*
+ * Weights in 4 bits.  The packed form is the library's own (the order in which
+ * the matrix cores take it), 16-byte aligned, coreinfer_w4_size bytes.
+ *   coreinfer_w4_quantize  w [R, C] (row stride ld >= C elements, of `dtype`,
+ *                          any alignment of whole elements) -> packed.
+ *   coreinfer_w4_read      packed -> the values it stands for, in `dtype`.
+ * E.g. the buffers of coreinfer_compact: w_up_c / w_gate_c [K, d] and, with
+ * CI_DOWN_OUT_MAJOR, w_down_c [d, K] with row stride ld.
+ * Limits: 1 <= R, C <= CI_MAX_NEURONS.  A group that is none of the three:
+ * CI_ERR_UNSUPPORTED.
+ */
+int coreinfer_w4_size(int64_t R, int64_t C, int group, size_t* bytes);
+int coreinfer_w4_quantize(const void* w, int64_t R, int64_t C, int64_t ld, int dtype, int group, void* packed,
+                          void* stream);
+int coreinfer_w4_read(const void* packed, int64_t R, int64_t C, int group, void* w, int64_t ld, int dtype, void* stream);
+
+/*
+ * y = act(x W^T + b) for one to 64 rows x [M, C] over weights in 4 bits, W [R, C]:
+ *   CI_ACT_NONE, CI_ACT_RELU (gate NULL; bias [R] of `bias_dtype` or NULL), or
+ *   CI_ACT_SWIGLU: y = SiLU(x G^T) * (x W^T), gate packed as W is (same R, C,
+ *   group); a bias is CI_ERR_INVALID_ARG as everywhere for gated layers.
+ * x [M, C] of x_dtype (row stride ldx >= C) and y [M, R] of y_dtype (row stride
+ * ldy >= R) may be of different types, so that the hidden values between two
+ * products stay in fp32; both are aligned to their elements.  16-bit x is multiplied
+ * as it is, fp32 x in three bf16 pieces (24 bits); sums in fp32, in a fixed order.
+ * A row of x with an infinity or a NaN gives NaN.
+ * ws: coreinfer_w4_matvec_workspace_size bytes, 16-byte aligned; NULL where
+ * that is 0 (one row, and as many as fit 64 KB).
+ */
+int coreinfer_w4_matvec_workspace_size(int64_t M, int64_t C, int x_dtype, size_t* bytes);
+int coreinfer_w4_matvec(const void* x, int64_t M, int64_t ldx, int x_dtype, const void* w, const void* gate,
+                        const void* bias, int bias_dtype, int act, int64_t R, int64_t C, int group, void* y,
+                        int64_t ldy, int y_dtype, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * A layer's keys and values in 4 bits: B sentences, H heads of D = 64 or 128
+ * channels, room for `cap` slots a sentence (a multiple of 32).  The buffers are
+ * the caller's, 16-byte aligned, of the sizes that coreinfer_kv4_sizes states, and
+ * need no initialisation: no call uses what lies behind a sentence's last slot.
+ * Which slots are in use is not part of the struct; the calls are told by `lens` [B]
+ * int32 on the device, so that a captured step can be replayed while sentences grow.
+ * D or group not supported (group must divide D): CI_ERR_UNSUPPORTED.
+ * B * H <= 65535.
+ */
+typedef struct {
+  void* k;           /* B H cap D / 2 bytes                              */
+  void* v;           /* B H cap D / 2 bytes                              */
+  uint32_t* k_scale; /* B H (D / group) cap: step and low                */
+  uint32_t* v_scale; /* the same                                         */
+  float* weight;     /* [B, H, cap] accumulated attention weight, or NULL  */
+  int32_t* pos;      /* [B, H, cap] position of a slot's token, or NULL    */
+  int64_t B, H, cap;
+  int32_t D, group;
+} ci_kv4;
+int coreinfer_kv4_sizes(int64_t B, int64_t H, int64_t cap, int D, int group, size_t* codes_bytes, size_t* scale_bytes);
+
+/*
+ * Writes S tokens' keys and values, k and v [B, S, H, D] of `dtype` with the
+ * element strides stride[0 .. 2] of b, s and h (host array, shared by both; a row of D is
+ * contiguous), e.g. slices of one fused projection.  lens [B] counts the new
+ * tokens already: token i goes to slot lens[b] - S + i.  start [B] (or NULL):
+ * the first slot that may be written, so that sentences with fewer than S new tokens
+ * have theirs at the end of the S; slots outside 0 .. cap - 1 are not written either.
+ * weight of a written slot becomes 0, pos (where the cache has them) next[b] - S + i;
+ * next [B]: the sentence's tokens so far, evicted ones included, NULL = lens.
+ */
+int coreinfer_kv4_append(const ci_kv4* cache, const void* k, const void* v, int64_t S, const int64_t* stride, int dtype,
+                         const int32_t* start, const int32_t* lens, const int32_t* next, void* stream);
+
+/*
+ * Slots first .. first + count - 1 as the values they stand for: k and v
+ * [B, H, count, D] of `dtype`, 16-byte aligned; zeros from lens[b] on.
+ */
+int coreinfer_kv4_read(const ci_kv4* cache, const int32_t* lens, int64_t first, int64_t count, void* k, void* v,
+                       int dtype, void* stream);
+
+/*
+ * Attention of S tokens a sentence over the cache, q [B, S, Hq, D] (element
+ * strides as above; Hq a multiple of H, query head i reads head i / (Hq / H)):
+ *     out[b, s, i] = sum_t p_t v_t,   p = softmax over t of scale (q . k_t).
+ * The S tokens are the sentence's last ones: row s sees the slots t < lens[b] and
+ * t <= lens[b] - S + s.  A row that sees none gives zeros.  lens beyond
+ * 0 .. max_len are taken as its ends; max_len <= cap sizes the launches.
+ *   out [B, S, Hq, D] of `dtype`, contiguous, 16-byte aligned, not overlapping q.
+ *   lse [B, S, Hq] fp32 or NULL: log of the sum of exp(scale q . k_t) over t
+ *       (-infinity for a row that sees nothing).
+ *   weight_out [B, H, cap] fp32 or NULL: cache->weight plus, for every slot t <
+ *       lens[b], the p_t of all rows and heads that read it; other slots are left as
+ *       they are.  May be cache->weight itself, which must not be NULL then.
+ * scale > 0 and finite.  Softmax statistics and sums in fp32; keys and values enter
+ * as they are held, q as it is (fp32 q in three bf16 pieces), probabilities in
+ * two bf16 pieces (fp32 q: three).  The order of the sums is fixed.
+ * ws: coreinfer_kv4_attend_workspace_size bytes, 16-byte aligned (weights != 0: for
+ * calls with weight_out).  Limits: S * (Hq / H) <= 2^20.
+ */
+int coreinfer_kv4_attend_workspace_size(int64_t B, int64_t H, int D, int64_t S, int64_t Hq, int64_t max_len, int weights,
+                                        size_t* bytes);
+int coreinfer_kv4_attend(const ci_kv4* cache, const void* q, int64_t S, int64_t Hq, const int64_t* stride, int dtype,
+                         float scale, const int32_t* lens, int64_t max_len, void* out, float* lse, float* weight_out,
+                         void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Eviction by accumulated attention weight: of every head with more than `budget`
+ * slots in use, `budget` stay, first those of the sentence's last `recent`
+ * positions (pos >= next[b] - recent), then those with the largest weight; equal
+ * weights go to the lower slot, a NaN counts least.
+ * As in coreinfer_compact_update a slot that stays below the budget keeps its place and
+ * those that stay from above it take the places of the others, both in ascending
+ * order, so only they are moved: one row a head for a cache that is cut by one at
+ * every step.  cache->weight and cache->pos must not be NULL.
+ *   weight_out, pos_out [B, H, cap]: of the new contents; slots from the budget to
+ *     lens[b] - 1 get weight 0 and pos -1, others are left.  May be
+ *     cache->weight and cache->pos.
+ *   lens_out [B] or NULL: min(lens[b], budget); may be lens.
+ * The order of slots is no longer that of positions, which attention does not ask for.
+ * ws: coreinfer_kv4_evict_workspace_size bytes, 16-byte aligned.
+ * 1 <= budget, 0 <= recent <= budget, 1 <= max_len <= cap.
+ */
+int coreinfer_kv4_evict_workspace_size(int64_t B, int64_t H, int64_t max_len, int64_t budget, size_t* bytes);
+int coreinfer_kv4_evict(const ci_kv4* cache, const int32_t* lens, const int32_t* next, int64_t max_len, int64_t budget,
+                        int64_t recent, float* weight_out, int32_t* pos_out, int32_t* lens_out, void* ws,
+                        size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

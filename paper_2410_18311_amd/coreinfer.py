@@ -27,6 +27,7 @@ CI_ERR_UNSUPPORTED = -6
 
 CI_F32, CI_F16, CI_BF16 = 0, 1, 2
 CI_ACT_RELU, CI_ACT_SWIGLU = 0, 1
+CI_ACT_NONE = 2  # w4_matvec only
 CI_DOWN_OUT_MAJOR, CI_DOWN_NEURON_MAJOR = 0, 1
 
 DTYPE_CODE = {torch.float32: CI_F32, torch.float16: CI_F16, torch.bfloat16: CI_BF16}
@@ -47,6 +48,11 @@ class ci_ffn_weights(ctypes.Structure):
     _fields_ = [("w_up", _vp), ("w_gate", _vp), ("b_up", _vp), ("w_down", _vp), ("b_down", _vp),
                 ("core_idx", _vp), ("K", _i64), ("d", _i64), ("N", _i64), ("ld_down", _i64),
                 ("down_layout", ctypes.c_int32)]
+
+
+class ci_kv4(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("weight", _vp), ("pos", _vp),
+                ("B", _i64), ("H", _i64), ("cap", _i64), ("D", ctypes.c_int32), ("group", ctypes.c_int32)]
 
 
 _SIGNATURES = {
@@ -88,6 +94,20 @@ _SIGNATURES = {
     "coreinfer_ffn_dense_workspace_size": (_int, [_i64, _i64, _i64, _int, ctypes.POINTER(_sz)]),
     "coreinfer_ffn_dense": (_int, [_vp, _i64, _vp, _vp, _vp, _vp, _vp, _int, _int, _int, _i64, _i64,
                                    _vp, _vp, _vp, _sz, _vp]),
+    "coreinfer_w4_size": (_int, [_i64, _i64, _int, ctypes.POINTER(_sz)]),
+    "coreinfer_w4_quantize": (_int, [_vp, _i64, _i64, _i64, _int, _int, _vp, _vp]),
+    "coreinfer_w4_read": (_int, [_vp, _i64, _i64, _int, _vp, _i64, _int, _vp]),
+    "coreinfer_w4_matvec_workspace_size": (_int, [_i64, _i64, _int, ctypes.POINTER(_sz)]),
+    "coreinfer_w4_matvec": (_int, [_vp, _i64, _i64, _int, _vp, _vp, _vp, _int, _int, _i64, _i64, _int, _vp, _i64, _int, _vp,
+                                   _sz, _vp]),
+    "coreinfer_kv4_sizes": (_int, [_i64, _i64, _i64, _int, _int, ctypes.POINTER(_sz), ctypes.POINTER(_sz)]),
+    "coreinfer_kv4_append": (_int, [ctypes.POINTER(ci_kv4), _vp, _vp, _i64, ctypes.POINTER(_i64), _int, _vp, _vp, _vp, _vp]),
+    "coreinfer_kv4_read": (_int, [ctypes.POINTER(ci_kv4), _vp, _i64, _i64, _vp, _vp, _int, _vp]),
+    "coreinfer_kv4_attend_workspace_size": (_int, [_i64, _i64, _int, _i64, _i64, _i64, _int, ctypes.POINTER(_sz)]),
+    "coreinfer_kv4_attend": (_int, [ctypes.POINTER(ci_kv4), _vp, _i64, _i64, ctypes.POINTER(_i64), _int, ctypes.c_float, _vp, _i64,
+                                    _vp, _vp, _vp, _vp, _sz, _vp]),
+    "coreinfer_kv4_evict_workspace_size": (_int, [_i64, _i64, _i64, _i64, ctypes.POINTER(_sz)]),
+    "coreinfer_kv4_evict": (_int, [ctypes.POINTER(ci_kv4), _vp, _vp, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _sz, _vp]),
 }
 for _name, (_res, _args) in _SIGNATURES.items():
     _f = getattr(_lib, _name)
@@ -634,3 +654,186 @@ def ffn_dense_hidden(X: torch.Tensor, w_up, w_gate, b_up, w_down, b_down, down_l
                                            _stream(X)),
            "coreinfer_ffn_dense_hidden")
     return Y, H
+
+
+class W4:
+    """Weights [R, C] in 4 bits, in groups along C (w4_quantize)."""
+
+    def __init__(self, packed: torch.Tensor, R: int, C: int, group: int):
+        self.packed, self.R, self.C, self.group = packed, R, C, group
+
+
+def w4_size(R: int, C: int, group: int) -> int:
+    b = _sz(0)
+    _check(_lib.coreinfer_w4_size(R, C, group, ctypes.byref(b)), "coreinfer_w4_size")
+    return b.value
+
+
+def w4_quantize(w: torch.Tensor, group: int = 64, packed: Optional[torch.Tensor] = None) -> W4:
+    """coreinfer_w4_quantize on w [R, C] (rows may be strided).  Pass `packed` (w4_size bytes) to reuse a buffer."""
+    assert w.dim() == 2 and w.stride(1) == 1
+    R, C = w.shape
+    if packed is None:
+        packed = _workspace(w4_size(R, C, group), w)
+    assert packed.numel() * packed.element_size() >= w4_size(R, C, group)
+    _check(_lib.coreinfer_w4_quantize(_ptr(w), R, C, w.stride(0), DTYPE_CODE[w.dtype], group, _ptr(packed), _stream(w)),
+           "coreinfer_w4_quantize")
+    return W4(packed, R, C, group)
+
+
+def w4_read(w: W4, dtype: torch.dtype, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """coreinfer_w4_read: the values that the packed weights stand for, [R, C]."""
+    if out is None:
+        out = torch.empty((w.R, w.C), dtype=dtype, device=w.packed.device)
+    assert out.shape == (w.R, w.C) and out.dtype == dtype and out.stride(1) == 1
+    _check(_lib.coreinfer_w4_read(_ptr(w.packed), w.R, w.C, w.group, _ptr(out), out.stride(0), DTYPE_CODE[dtype],
+                                  _stream(out)), "coreinfer_w4_read")
+    return out
+
+
+def w4_matvec_workspace_size(M: int, C: int, dtype: torch.dtype) -> int:
+    b = _sz(0)
+    _check(_lib.coreinfer_w4_matvec_workspace_size(M, C, DTYPE_CODE[dtype], ctypes.byref(b)),
+           "coreinfer_w4_matvec_workspace_size")
+    return b.value
+
+
+_W4_ACT = {"none": CI_ACT_NONE, **ACT_CODE}
+
+
+def w4_matvec(x: torch.Tensor, w: W4, gate: Optional[W4] = None, bias: Optional[torch.Tensor] = None, act: str = "none",
+              y: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+              out_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """coreinfer_w4_matvec on x [M, C] (or [C]): act(x W^T + bias), "swiglu" with `gate`: SiLU(x G^T) * (x W^T)."""
+    x2 = x if x.dim() == 2 else x.unsqueeze(0)
+    M, C = x2.shape
+    assert C == w.C and x2.stride(1) == 1
+    assert gate is None or (gate.R, gate.C, gate.group) == (w.R, w.C, w.group)
+    assert bias is None or (bias.numel() == w.R and bias.is_contiguous())
+    if y is None:
+        y = torch.empty((M, w.R), dtype=out_dtype or x.dtype, device=x.device)
+    y2 = y if y.dim() == 2 else y.unsqueeze(0)
+    assert y2.shape == (M, w.R) and y2.stride(1) == 1
+    if ws is None:
+        need = w4_matvec_workspace_size(M, C, x.dtype)
+        ws = _workspace(need, x) if need else None
+    _check(_lib.coreinfer_w4_matvec(_ptr(x2), M, x2.stride(0) if M > 1 else C, DTYPE_CODE[x.dtype], _ptr(w.packed),
+                                    None if gate is None else _ptr(gate.packed), _ptr(bias),
+                                    0 if bias is None else DTYPE_CODE[bias.dtype], _W4_ACT[act], w.R, C, w.group, _ptr(y2),
+                                    y2.stride(0) if M > 1 else w.R, DTYPE_CODE[y2.dtype], _ptr(ws),
+                                    0 if ws is None else ws.numel(), _stream(x)), "coreinfer_w4_matvec")
+    return y.squeeze(0) if x.dim() == 1 and y.dim() == 2 else y
+
+
+class Kv4Cache:
+    """A layer's keys and values in 4 bits (kv4_cache), with the accumulated weight and the position of every slot."""
+
+    def __init__(self, k, v, k_scale, v_scale, weight, pos, shape):
+        self.k, self.v, self.k_scale, self.v_scale, self.weight, self.pos = k, v, k_scale, v_scale, weight, pos
+        self.B, self.H, self.cap, self.D, self.group = shape
+        self.desc = ci_kv4(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(weight), _ptr(pos), *shape)
+
+
+def kv4_cache(B: int, H: int, cap: int, D: int, group: int = 64, weights: bool = True, device="cuda") -> Kv4Cache:
+    """Buffers for `cap` slots (a multiple of 32) of B sentences and H heads of D channels; weights: with the
+    accumulated weights and positions that kv4_evict goes by."""
+    codes, scale = _sz(0), _sz(0)
+    _check(_lib.coreinfer_kv4_sizes(B, H, cap, D, group, ctypes.byref(codes), ctypes.byref(scale)), "coreinfer_kv4_sizes")
+    buf = lambda n: torch.empty(n, dtype=torch.uint8, device=device)  # noqa: E731
+    weight = torch.zeros((B, H, cap), dtype=torch.float32, device=device) if weights else None
+    pos = torch.full((B, H, cap), -1, dtype=torch.int32, device=device) if weights else None
+    return Kv4Cache(buf(codes.value), buf(codes.value), buf(scale.value), buf(scale.value), weight, pos, (B, H, cap, D, group))
+
+
+def _check_lens(cache: Kv4Cache, *lens: Optional[torch.Tensor]):
+    for t in lens:
+        assert t is None or (t.dtype == torch.int32 and t.numel() == cache.B and t.is_contiguous())
+
+
+def _strides(t: torch.Tensor):
+    return (_i64 * 3)(*t.stride()[:3])
+
+
+def kv4_append(cache: Kv4Cache, k: torch.Tensor, v: torch.Tensor, lens: torch.Tensor, start: Optional[torch.Tensor] = None,
+               next_pos: Optional[torch.Tensor] = None) -> None:
+    """coreinfer_kv4_append: k, v [B, S, H, D] (any strides, the same for both, channels contiguous) become the last S of
+    the lens[b] slots of each sentence."""
+    assert k.shape == v.shape and k.dtype == v.dtype and k.dim() == 4 and k.stride() == v.stride() and k.stride(3) == 1
+    B, S, H, D = k.shape
+    assert (B, H, D) == (cache.B, cache.H, cache.D)
+    _check_lens(cache, lens, start, next_pos)
+    _check(_lib.coreinfer_kv4_append(ctypes.byref(cache.desc), _ptr(k), _ptr(v), S, _strides(k), DTYPE_CODE[k.dtype],
+                                     _ptr(start), _ptr(lens), _ptr(next_pos), _stream(k)), "coreinfer_kv4_append")
+
+
+def kv4_read(cache: Kv4Cache, lens: torch.Tensor, first: int, count: int, dtype: torch.dtype,
+             k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None):
+    """coreinfer_kv4_read: the values of slots first .. first + count - 1, (k, v) [B, H, count, D]; zeros from lens on."""
+    shape = (cache.B, cache.H, count, cache.D)
+    if k is None:
+        k = torch.empty(shape, dtype=dtype, device=cache.k.device)
+    if v is None:
+        v = torch.empty(shape, dtype=dtype, device=cache.k.device)
+    for t in (k, v):
+        assert t.shape == shape and t.dtype == dtype and t.is_contiguous()
+    _check_lens(cache, lens)
+    _check(_lib.coreinfer_kv4_read(ctypes.byref(cache.desc), _ptr(lens), first, count, _ptr(k), _ptr(v), DTYPE_CODE[dtype],
+                                   _stream(k)), "coreinfer_kv4_read")
+    return k, v
+
+
+def kv4_attend_workspace_size(cache: Kv4Cache, S: int, Hq: int, max_len: int, weights: bool) -> int:
+    b = _sz(0)
+    _check(_lib.coreinfer_kv4_attend_workspace_size(cache.B, cache.H, cache.D, S, Hq, max_len, int(bool(weights)),
+                                                    ctypes.byref(b)), "coreinfer_kv4_attend_workspace_size")
+    return b.value
+
+
+def kv4_attend(q: torch.Tensor, cache: Kv4Cache, lens: torch.Tensor, scale: Optional[float] = None,
+               max_len: Optional[int] = None, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+               weight_out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """coreinfer_kv4_attend: q [B, S, Hq, D], the last S tokens of each sentence, over the cache.  scale: 1 / sqrt(D) by
+    default; max_len: the most any of lens is (the cache's capacity by default; the launches are sized by it)."""
+    B, S, Hq, D = q.shape
+    assert (B, D) == (cache.B, cache.D) and q.stride(3) == 1
+    _check_lens(cache, lens)
+    max_len = cache.cap if max_len is None else max_len
+    if out is None:
+        out = torch.empty((B, S, Hq, D), dtype=q.dtype, device=q.device)
+    assert out.shape == q.shape and out.dtype == q.dtype and out.is_contiguous()
+    assert lse is None or (lse.shape == (B, S, Hq) and lse.dtype == torch.float32 and lse.is_contiguous())
+    assert weight_out is None or (weight_out.shape == (B, cache.H, cache.cap) and weight_out.dtype == torch.float32 and
+                                  weight_out.is_contiguous())
+    if ws is None:
+        ws = _workspace(kv4_attend_workspace_size(cache, S, Hq, max_len, weight_out is not None), q)
+    _check(_lib.coreinfer_kv4_attend(ctypes.byref(cache.desc), _ptr(q), S, Hq, _strides(q), DTYPE_CODE[q.dtype],
+                                     D ** -0.5 if scale is None else scale, _ptr(lens), max_len, _ptr(out), _ptr(lse),
+                                     _ptr(weight_out), _ptr(ws), ws.numel(), _stream(q)), "coreinfer_kv4_attend")
+    return out
+
+
+def kv4_evict_workspace_size(cache: Kv4Cache, max_len: int, budget: int) -> int:
+    b = _sz(0)
+    _check(_lib.coreinfer_kv4_evict_workspace_size(cache.B, cache.H, max_len, budget, ctypes.byref(b)),
+           "coreinfer_kv4_evict_workspace_size")
+    return b.value
+
+
+def kv4_evict(cache: Kv4Cache, lens: torch.Tensor, next_pos: torch.Tensor, budget: int, recent: int,
+              max_len: Optional[int] = None, weight_out: Optional[torch.Tensor] = None,
+              pos_out: Optional[torch.Tensor] = None, lens_out: Optional[torch.Tensor] = None,
+              ws: Optional[torch.Tensor] = None) -> None:
+    """coreinfer_kv4_evict: cuts heads of more than `budget` slots to those of the last `recent` positions and of the largest
+    accumulated weights.  weight_out, pos_out and lens_out are the cache's own and `lens` by default."""
+    _check_lens(cache, lens, next_pos, lens_out)
+    max_len = cache.cap if max_len is None else max_len
+    weight_out = cache.weight if weight_out is None else weight_out
+    pos_out = cache.pos if pos_out is None else pos_out
+    lens_out = lens if lens_out is None else lens_out
+    for t, dtype in ((weight_out, torch.float32), (pos_out, torch.int32)):
+        assert t is None or (t.shape == (cache.B, cache.H, cache.cap) and t.dtype == dtype and t.is_contiguous())
+    if ws is None:
+        ws = _workspace(kv4_evict_workspace_size(cache, max_len, budget), lens)
+    _check(_lib.coreinfer_kv4_evict(ctypes.byref(cache.desc), _ptr(lens), _ptr(next_pos), max_len, budget, recent,
+                                    _ptr(weight_out), _ptr(pos_out), _ptr(lens_out), _ptr(ws), ws.numel(), _stream(lens)),
+           "coreinfer_kv4_evict")

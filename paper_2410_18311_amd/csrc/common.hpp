@@ -272,4 +272,23 @@ int launch_gemm_down(const void* H, int64_t M, const void* w_down, const void* b
                      int down_layout, int dtype, int64_t d, int64_t N, void* Y, float* partial,
                      const GemmPlan& p, hipStream_t s);
 
+// Weights in 4 bits (w4.hip).
+size_t w4_bytes(int64_t R, int64_t C, int group);
+size_t w4_matvec_ws_bytes(int64_t M, int64_t C, int x_dtype);
+int launch_w4_quantize(const void* w, int64_t R, int64_t C, int64_t ld, int dtype, int group, void* packed, hipStream_t s);
+int launch_w4_read(const void* packed, int64_t R, int64_t C, int group, void* w, int64_t ld, int dtype, hipStream_t s);
+int launch_w4_matvec(const void* x, int64_t M, int64_t ldx, int x_dtype, const void* w, const void* gate, const void* bias,
+                     int bias_dtype, int act, int64_t R, int64_t C, int group, void* y, int64_t ldy, int y_dtype, void* ws,
+                     hipStream_t s);
+// A cache in 4 bits (kv4.hip, kv4_attend.hip).
+int launch_kv4_append(const ci_kv4& c, const void* k, const void* v, int64_t S, const int64_t (&stride)[3], int dtype,
+                      const int32_t* start, const int32_t* lens, const int32_t* next, hipStream_t s);
+int launch_kv4_read(const ci_kv4& c, const int32_t* lens, int64_t first, int64_t count, void* k, void* v, int dtype, hipStream_t s);
+size_t kv4_attend_ws_bytes(int64_t heads, int D, int64_t S, int64_t G, int64_t max_len, bool weights);
+int launch_kv4_attend(const ci_kv4& c, const void* q, int64_t S, int64_t G, const int64_t (&stride)[3], int dtype, float scale,
+                      const int32_t* lens, int64_t max_len, void* out, float* lse, float* weight_out, void* ws, hipStream_t s);
+size_t kv4_evict_ws_bytes(int64_t heads, int64_t max_len, int64_t budget);
+int launch_kv4_evict(const ci_kv4& c, const int32_t* lens, const int32_t* next, int64_t max_len, int64_t budget, int64_t recent,
+                     float* weight_out, int32_t* pos_out, int32_t* lens_out, void* ws, hipStream_t s);
+
 }  // namespace ci

@@ -1,0 +1,556 @@
+// Attention over a cache in 4 bits (kv4.hpp): out = softmax(scale q k^T, causal) v for S rows of each query head, one token or a prompt's
+// chunk, in one pass over the cache with a running maximum and sum.
+//
+// A wave takes tiles of 16 rows (the S G rows that share a head of the cache, G query heads to each) and steps of 32 slots.  The logits come out
+// of the matrix cores with slots down and rows across, four slots to a lane: just the layout in which the probabilities enter the product with
+// the values, so nothing is exchanged between lanes and nothing but the sums of waves passes through the LDS.  Steps and lowest values enter in
+// fp32: logit = step (q . codes) + low (sum q), and the probabilities are multiplied by the values' steps before they are split into
+// bf16 pieces (16 bits of them for 16-bit results, 24 for fp32).  The running maximum is raised only when a logit passes it by 2^8, which a
+// first look at the lane's own eight logits decides; the sums hold that range in fp32.
+//
+// Bound: the cache's bytes where few rows meet many slots; 256 vector instructions a step (unpacking, the softmax, the pieces), which
+// is 10 TB/s of cache, leave room for that.  With 16 rows and more, the instructions.
+#pragma once
+
+#include "kv4.hpp"
+
+namespace ci {
+namespace {
+
+template <class T> struct AttendType;
+template <> struct AttendType<F32> { static constexpr int P = 3, OPV = kOpExact; };
+template <> struct AttendType<F16> { static constexpr int P = 2, OPV = kOpBF16; };
+template <> struct AttendType<BF16> { static constexpr int P = 2, OPV = kOpBF16; };
+
+__device__ __forceinline__ uint32_t word_of(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+
+// A lane's 16 (D = 64: 8) bytes.
+template <int D>
+__device__ __forceinline__ uint4 ld_row(const uint32_t* p) {
+  if constexpr (D == 128) return ld16(p);
+  const uint2 u = *reinterpret_cast<const uint2*>(p);
+  return make_uint4(u.x, u.y, 0, 0);
+}
+
+// The rows of a tile as operands, zero rows nowhere: rows past the last repeat it.  sums: of the row's channels by group, minus-offset.
+template <class T, int D, int GR>
+__device__ __forceinline__ void load_rows(const Kv4Attend& a, int b, int h, int row, uint4 (&q)[D / 32][Q4Type<T>::PIECES],
+                                          float (&sums)[D / GR]) {
+  constexpr int OP = Q4Type<T>::OP, PIECES = Q4Type<T>::PIECES;
+  const int g = (threadIdx.x & 63) >> 4, s = row / a.G, i = row % a.G;
+  const typename T::T* src = reinterpret_cast<const typename T::T*>(a.q) + b * a.q_b + s * a.q_s + (int64_t)(h * a.G + i) * a.q_h + 8 * g;
+#pragma unroll
+  for (int j = 0; j < D / 32; ++j) {
+    if constexpr (T::VEC == 8) {
+      if (a.q_vectors) q[j][0] = ld16(src + 32 * j);
+      else {
+        uint32_t p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          p[e] = (uint32_t)__builtin_bit_cast(uint16_t, src[32 * j + 2 * e]) |
+                 (uint32_t)__builtin_bit_cast(uint16_t, src[32 * j + 2 * e + 1]) << 16;
+        q[j][0] = make_uint4(p[0], p[1], p[2], p[3]);
+      }
+    } else {
+      uint32_t p[4][3];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) split_bf16<3>(src[32 * j + 2 * e], src[32 * j + 2 * e + 1], p[e]);
+#pragma unroll
+      for (int c = 0; c < 3; ++c) q[j][c] = make_uint4(p[0][c], p[1][c], p[2][c], p[3][c]);
+    }
+  }
+  const uint4 ones = make_uint4(kOnes<OP>, kOnes<OP>, kOnes<OP>, kOnes<OP>);
+#pragma unroll
+  for (int f = 0; f < D / GR; ++f) {
+    f32x4q acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int j = f * (GR / 32); j < (f + 1) * (GR / 32); ++j)
+#pragma unroll
+      for (int c = 0; c < PIECES; ++c) acc = mfma_q4<OP>(ones, q[j][c], acc);
+    sums[f] = acc[0];
+  }
+}
+
+// Logits (without the scale) of 16 slots, four to a lane, and the rows of q.
+template <class T, int D, int GR>
+__device__ __forceinline__ f32x4q logits_of(const uint4 (&k)[D / 32], const uint4 (&scale)[D / GR],
+                                            const uint4 (&q)[D / 32][Q4Type<T>::PIECES], const float (&sums)[D / GR]) {
+  constexpr int OP = Q4Type<T>::OP, PIECES = Q4Type<T>::PIECES;
+  f32x4q x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int f = 0; f < D / GR; ++f) {
+    const float c0 = -kOffset<OP> * sums[f];
+    f32x4q acc = {c0, c0, c0, c0};
+#pragma unroll
+    for (int j = f * (GR / 32); j < (f + 1) * (GR / 32); ++j)
+#pragma unroll
+      for (int c = 0; c < PIECES; ++c) acc = mfma_q4<OP>(k[j], q[j][c], acc);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const uint32_t s = word_of(scale[f], r);
+      x[r] = __builtin_fmaf(half_lo(s), acc[r], __builtin_fmaf(half_hi(s), sums[f], x[r]));
+    }
+  }
+  return x;
+}
+
+// Four results of neighbouring channels.
+template <class T>
+__device__ __forceinline__ void store_out(const Kv4Attend& a, int D, int b, int h, int row, int d, const f32x4q& v) {
+  const int s = row / a.G, i = row % a.G;
+  typename T::T* dst = reinterpret_cast<typename T::T*>(a.out) + (((int64_t)b * a.S + s) * a.c.H * a.G + h * a.G + i) * D + d;
+  if constexpr (T::VEC == 4) {
+    *reinterpret_cast<float4*>(dst) = make_float4(v[0], v[1], v[2], v[3]);
+  } else {
+    uint2 u;
+    if constexpr (Q4Type<T>::OP == kOpF16) {
+      half2_t x, y;
+      x[0] = (_Float16)v[0]; x[1] = (_Float16)v[1]; y[0] = (_Float16)v[2]; y[1] = (_Float16)v[3];
+      u = make_uint2(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y));
+    } else {
+      u = make_uint2(pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3]));
+    }
+    *reinterpret_cast<uint2*>(dst) = u;
+  }
+}
+
+// Slots that a row sees: those before the limit.
+__device__ __forceinline__ int row_limit(const Kv4Attend& a, int len, int row) { return min(len, len - a.S + row / a.G + 1); }
+// log2 of a row's sum over slots; +infinity where it sees none, so that every probability against it is 0.
+__device__ __forceinline__ float log_sum(float m, float l) { return l == 0.0f ? INFINITY : m + __builtin_amdgcn_logf(l); }
+__device__ __forceinline__ void store_lse(const Kv4Attend& a, int b, int h, int row, float z) {
+  if (!a.lse) return;
+  const int s = row / a.G, i = row % a.G;
+  // natural logarithm; -infinity for a row that sees nothing
+  a.lse[((int64_t)b * a.S + s) * a.c.H * a.G + h * a.G + i] = z == INFINITY ? -INFINITY : z * 0.69314718055994531f;
+}
+
+template <class T, int D, int GR, int NR, bool LOGITS>
+__global__ __launch_bounds__(256) void gemm_q4_attend_kernel(Kv4Attend a) {
+  constexpr int OP = Q4Type<T>::OP, OPV = AttendType<T>::OPV, PIECES = Q4Type<T>::PIECES, P = AttendType<T>::P;
+  constexpr int NG = D / GR, JK = D / 32, JV = D / 16;
+  __shared__ float ml[2][4][NR][16];
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int bh = blockIdx.x, b = bh / a.c.H, h = bh % a.c.H, split = blockIdx.z;
+  const bool joined = a.token_waves == 4;
+  const int tile0 = (joined ? (int)blockIdx.y : (int)blockIdx.y * 4 + wave) * NR;
+  const int row0 = tile0 * 16;
+  if (!joined && row0 >= a.R) return;   // no barrier follows
+  const int len = min(max(a.lens[b], 0), a.max_len);
+
+  uint4 q[NR][JK][PIECES];
+  float sums[NR][NG];
+  int limit[NR];
+#pragma unroll
+  for (int u = 0; u < NR; ++u) {
+    const int row = min(row0 + 16 * u + n, a.R - 1);
+    load_rows<T, D, GR>(a, b, h, row, q[u], sums[u]);
+    limit[u] = row_limit(a, len, row);
+  }
+  const int low_limit = row_limit(a, len, row0), high_limit = row_limit(a, len, min(row0 + 16 * NR, a.R) - 1);
+
+  f32x4q o[NR][JV], one[NR][NG];
+  float m[NR], l[NR], low[NR][NG];
+#pragma unroll
+  for (int u = 0; u < NR; ++u) {
+    m[u] = -INFINITY;
+    l[u] = 0.0f;
+#pragma unroll
+    for (int f = 0; f < NG; ++f) one[u][f] = f32x4q{0.0f, 0.0f, 0.0f, 0.0f}, low[u][f] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < JV; ++j) o[u][j] = f32x4q{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+
+  // where the lane's share of a step lies
+  const uint32_t* kp = a.c.k + ((size_t)bh * a.c.cap + n) * (D / 8) + g * (D / 32);
+  const uint32_t* vp = a.c.v + ((size_t)bh * (a.c.cap / 4) + g) * (D / 2) + n * (D / 32);
+  const uint32_t* ksp = a.c.ks + (size_t)bh * NG * a.c.cap + 4 * g;
+  const uint32_t* vsp = a.c.vs + (size_t)bh * NG * a.c.cap + 4 * g;
+  struct Stage {
+    uint4 k[2], v[2], ks[2][NG], vs[2][NG];
+  };
+  const int step0 = split * a.chunk + (joined ? wave : 0), stride = joined ? 4 : 1;
+  const int steps = min((split + 1) * a.chunk, (max(high_limit, 0) + 31) / 32);
+  auto load = [&](Stage& st, int step) {
+    const int t = step * 32;   // t + 32 <= cap, which is whole steps
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      st.k[i] = ld_row<D>(kp + (size_t)(t + 16 * i) * (D / 8));
+      st.v[i] = ld_row<D>(vp + (size_t)(t / 4 + 4 * i) * (D / 2));
+#pragma unroll
+      for (int f = 0; f < NG; ++f) {
+        st.ks[i][f] = ld16(ksp + (size_t)f * a.c.cap + t + 16 * i);
+        st.vs[i][f] = ld16(vsp + (size_t)f * a.c.cap + t + 16 * i);
+      }
+    }
+  };
+  const Q4Magic mk = q4_magic<OP>(), mv = q4_magic<OPV>();
+  const uint4 ones = make_uint4(kOnes<OPV>, kOnes<OPV>, kOnes<OPV>, kOnes<OPV>);
+
+  Stage cur, next;
+  if (step0 < steps) load(cur, step0);
+  for (int step = step0; step < steps; step += stride) {
+    load(next, min(step + stride, steps - 1));
+    const int t0 = step * 32;
+    const bool partial = t0 + 32 > low_limit;
+    uint4 kop[2][JK];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < JK; ++j) kop[i][j] = q4_operand<OP>(word_of(cur.k[i], j), mk);
+    uint4 piece[NR][NG][P];
+#pragma unroll
+    for (int u = NR - 1; u >= 0; --u) {   // later rows see more
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const f32x4q y = logits_of<T, D, GR>(kop[i], cur.ks[i], q[u], sums[u]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[4 * i + r] = y[r];
+      }
+      if (partial) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (t0 + 16 * (i / 4) + 4 * g + i % 4 >= limit[u]) x[i] = -INFINITY;
+        // no probability of a slot that the row does not see meets its step and lowest value, which may be anything
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int see = limit[u] - (t0 + 16 * i + 4 * g);
+#pragma unroll
+          for (int f = 0; f < NG; ++f) {
+            cur.vs[i][f].x = see > 0 ? cur.vs[i][f].x : 0;
+            cur.vs[i][f].y = see > 1 ? cur.vs[i][f].y : 0;
+            cur.vs[i][f].z = see > 2 ? cur.vs[i][f].z : 0;
+            cur.vs[i][f].w = see > 3 ? cur.vs[i][f].w : 0;
+          }
+        }
+      }
+      if constexpr (LOGITS) {   // one tile of rows
+        if (n < a.R) {
+          float4* dst = reinterpret_cast<float4*>(a.logits + ((size_t)bh * a.R + n) * ((a.max_len + 31) / 32 * 32) + t0 + 4 * g);
+          dst[0] = make_float4(x[0] * a.scale, x[1] * a.scale, x[2] * a.scale, x[3] * a.scale);
+          dst[4] = make_float4(x[4] * a.scale, x[5] * a.scale, x[6] * a.scale, x[7] * a.scale);
+        }
+      }
+      float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))) * a.scale;
+      if (__any(top > m[u] + 8.0f)) {
+        top = fmaxf(top, __shfl_xor(top, 16, kWave));
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        top = fmaxf(top, m[u]);
+        const float f = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[u] - top);
+        m[u] = top;
+        l[u] *= f;
+#pragma unroll
+        for (int e = 0; e < NG; ++e) {
+          low[u][e] *= f;
+          one[u][e] *= f;
+        }
+#pragma unroll
+        for (int j = 0; j < JV; ++j) o[u][j] *= f;
+      }
+      const float base = m[u] == -INFINITY ? 0.0f : m[u];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale, -base));
+        l[u] += x[i];
+      }
+#pragma unroll
+      for (int f = 0; f < NG; ++f) {
+        uint32_t p[4][P];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t s0 = word_of(cur.vs[i / 2][f], 2 * (i % 2)), s1 = word_of(cur.vs[i / 2][f], 2 * (i % 2) + 1);
+          low[u][f] = __builtin_fmaf(half_hi(s0), x[2 * i], low[u][f]);
+          low[u][f] = __builtin_fmaf(half_hi(s1), x[2 * i + 1], low[u][f]);
+          split_bf16<P>(half_lo(s0) * x[2 * i], half_lo(s1) * x[2 * i + 1], p[i]);
+        }
+#pragma unroll
+        for (int c = 0; c < P; ++c) {
+          piece[u][f][c] = make_uint4(p[0][c], p[1][c], p[2][c], p[3][c]);
+          if constexpr (OPV != kOpExact) one[u][f] = mfma_q4<OPV>(ones, piece[u][f][c], one[u][f]);
+        }
+      }
+    }
+    // channels 16 j + n of eight slots: bits 4 i of the words of half f of each pair of slots
+#pragma unroll
+    for (int f = 0; f < D / 64; ++f) {
+      uint4 vop[4];
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = word_of(cur.v[i / 2], (D / 64) * (i % 2) + f);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t e[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          if constexpr (OPV == kOpBF16) {
+            e[c] = ((w[c] >> (4 * i)) & mv.mask) | mv.magic;
+          } else {
+            const uint32_t two = (w[c] >> (4 * i)) & 0x000f000fu;
+            e[c] = __builtin_amdgcn_perm(f2u((float)(two >> 16)), f2u((float)(two & 0xffffu)), 0x07060302u);
+          }
+        }
+        vop[i] = make_uint4(e[0], e[1], e[2], e[3]);
+      }
+#pragma unroll
+      for (int u = 0; u < NR; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int c = 0; c < P; ++c) o[u][4 * f + i] = mfma_q4<OPV>(vop[i], piece[u][(4 * f + i) * 16 / GR][c], o[u][4 * f + i]);
+    }
+    cur = next;
+  }
+
+  // sums over the lanes of a row, and the constants that entered with the codes
+#pragma unroll
+  for (int u = 0; u < NR; ++u) {
+    l[u] += __shfl_xor(l[u], 16, kWave);
+    l[u] += __shfl_xor(l[u], 32, kWave);
+#pragma unroll
+    for (int f = 0; f < NG; ++f) {
+      low[u][f] += __shfl_xor(low[u][f], 16, kWave);
+      low[u][f] += __shfl_xor(low[u][f], 32, kWave);
+      if constexpr (OPV != kOpExact) low[u][f] = __builtin_fmaf(-kOffset<OPV>, one[u][f][0], low[u][f]);
+    }
+#pragma unroll
+    for (int j = 0; j < JV; ++j) o[u][j] += low[u][j * 16 / GR];
+  }
+  const size_t part = ((size_t)bh * a.splits + split) * a.row_tiles * 16;
+  if (!joined) {
+#pragma unroll
+    for (int u = 0; u < NR; ++u) {
+      const int row = row0 + 16 * u + n;
+      if (row >= a.R) continue;
+      if (a.splits > 1) {
+        if (g == 0) a.m[part + row] = m[u], a.l[part + row] = l[u];
+#pragma unroll
+        for (int j = 0; j < JV; ++j)
+          *reinterpret_cast<float4*>(a.o + (part + row) * D + 16 * j + 4 * g) = make_float4(o[u][j][0], o[u][j][1], o[u][j][2], o[u][j][3]);
+      } else {
+        const float inv = l[u] == 0.0f ? 0.0f : 1.0f / l[u], z = log_sum(m[u], l[u]);
+#pragma unroll
+        for (int j = 0; j < JV; ++j) store_out<T>(a, D, b, h, row, 16 * j + 4 * g, o[u][j] * inv);
+        if (g == 0) {
+          store_lse(a, b, h, row, z);
+          if (a.weights) a.z[(size_t)bh * a.R + row] = z;
+        }
+      }
+    }
+    return;
+  }
+
+  // the waves' sums
+  float4* shared = reinterpret_cast<float4*>(smem);   // [wave][u][j][lane]
+  if (g == 0)
+#pragma unroll
+    for (int u = 0; u < NR; ++u) ml[0][wave][u][n] = m[u], ml[1][wave][u][n] = l[u];
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < NR; ++u) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[0][w][u][n]);
+    const float f = m[u] == -INFINITY ? (l[u] != l[u] ? l[u] : 0.0f) : __builtin_amdgcn_exp2f(m[u] - top);   // a row of NaNs stays one
+#pragma unroll
+    for (int j = 0; j < JV; ++j)
+      shared[((wave * NR + u) * JV + j) * 64 + lane] = make_float4(o[u][j][0] * f, o[u][j][1] * f, o[u][j][2] * f, o[u][j][3] * f);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < NR * JV * 64; i += 256) {
+    const int at = i & 63, j = (i >> 6) % JV, u = (i >> 6) / JV, col = at & 15, row = row0 + 16 * u + col;
+    if (row >= a.R) continue;
+    float top = -INFINITY, total = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[0][w][u][col]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float mw = ml[0][w][u][col], lw = ml[1][w][u][col];
+      total += mw == -INFINITY ? lw : lw * __builtin_amdgcn_exp2f(mw - top);   // no maximum: 0, or NaN
+    }
+    f32x4q v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float4 s = shared[((w * NR + u) * JV + j) * 64 + at];
+      v[0] += s.x; v[1] += s.y; v[2] += s.z; v[3] += s.w;
+    }
+    const int d = 16 * j + 4 * (at >> 4);
+    if (a.splits > 1) {
+      *reinterpret_cast<float4*>(a.o + (part + row) * D + d) = make_float4(v[0], v[1], v[2], v[3]);
+      if (d == 0) a.m[part + row] = top, a.l[part + row] = total;
+    } else {
+      const float z = log_sum(top, total);
+      store_out<T>(a, D, b, h, row, d, v * (total == 0.0f ? 0.0f : 1.0f / total));
+      if (d == 0) {
+        store_lse(a, b, h, row, z);
+        if (a.weights) a.z[(size_t)bh * a.R + row] = z;
+      }
+    }
+  }
+}
+
+// A row's maximum and sum over the splits.
+__device__ __forceinline__ void join_split(const Kv4Attend& a, size_t bh, int row, float* top, float* total) {
+  const size_t at = bh * a.splits * a.row_tiles * 16 + row, next = (size_t)a.row_tiles * 16;
+  float m = -INFINITY, l = 0.0f;
+  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.m[at + s * next]);
+  for (int s = 0; s < a.splits; ++s) {
+    const float ms = a.m[at + s * next], ls = a.l[at + s * next];
+    l += ms == -INFINITY ? ls : ls * __builtin_amdgcn_exp2f(ms - m);
+  }
+  *top = m;
+  *total = l;
+}
+
+// The splits' results, in their order: workgroups x < join_blocks; the others add the weights of 1024 slots up from the stored logits.
+template <class T, int D>
+__global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Attend a, int join_blocks) {
+  const int bh = blockIdx.y, b = bh / a.c.H, h = bh % a.c.H;
+  if ((int)blockIdx.x < join_blocks) {
+    constexpr int ROWS = 256 / (D / 4);
+    const int row = blockIdx.x * ROWS + threadIdx.x / (D / 4), d = threadIdx.x % (D / 4) * 4;
+    if (row >= a.R) return;
+    float top, total;
+    join_split(a, bh, row, &top, &total);
+    const size_t at = (size_t)bh * a.splits * a.row_tiles * 16 + row, next = (size_t)a.row_tiles * 16;
+    f32x4q v = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s = 0; s < a.splits; ++s) {
+      const float ms = a.m[at + s * next], f = ms == -INFINITY ? (a.l[at + s * next] != 0.0f ? NAN : 0.0f) : __builtin_amdgcn_exp2f(ms - top);
+      const float4 p = *reinterpret_cast<const float4*>(a.o + (at + s * next) * D + d);
+      v[0] += p.x * f; v[1] += p.y * f; v[2] += p.z * f; v[3] += p.w * f;
+    }
+    const float z = log_sum(top, total);
+    store_out<T>(a, D, b, h, row, d, v * (total == 0.0f ? 0.0f : 1.0f / total));
+    if (d == 0) {
+      store_lse(a, b, h, row, z);
+      if (a.weights) a.z[(size_t)bh * a.R + row] = z;
+    }
+    return;
+  }
+  __shared__ float zs[16];
+  if ((int)threadIdx.x < a.R) {
+    float z;
+    if (a.splits > 1) {
+      float top, total;
+      join_split(a, bh, threadIdx.x, &top, &total);
+      z = log_sum(top, total);
+    } else {
+      z = a.z[(size_t)bh * a.R + threadIdx.x];
+    }
+    zs[threadIdx.x] = z;
+  }
+  __syncthreads();
+  const int len = min(max(a.lens[b], 0), a.max_len);
+  const int pitch = (a.max_len + 31) / 32 * 32;
+  const int t0 = ((int)blockIdx.x - join_blocks) * 1024 + threadIdx.x * 4;
+  if (t0 >= len) return;
+  float w[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int r = 0; r < a.R; ++r) {
+    if (t0 >= row_limit(a, len, r)) continue;   // also: no logits were stored there
+    const float4 x = *reinterpret_cast<const float4*>(a.logits + ((size_t)bh * a.R + r) * pitch + t0);
+    w[0] += __builtin_amdgcn_exp2f(x.x - zs[r]);
+    w[1] += __builtin_amdgcn_exp2f(x.y - zs[r]);
+    w[2] += __builtin_amdgcn_exp2f(x.z - zs[r]);
+    w[3] += __builtin_amdgcn_exp2f(x.w - zs[r]);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (t0 + i < len) {
+      const size_t at = (size_t)bh * a.c.cap + t0 + i;
+      a.weight_out[at] = a.c.weight[at] + w[i];
+    }
+}
+
+// Weights of many rows: the logits are computed again, 32 slots a wave against all rows that see them, and every slot's sum stays in its
+// lane until the end, so there is no order to depend on and nothing of S x T is stored.
+template <class T, int D, int GR>
+__global__ __launch_bounds__(256) void gemm_q4_weights_kernel(Kv4Attend a) {
+  constexpr int OP = Q4Type<T>::OP, PIECES = Q4Type<T>::PIECES, NG = D / GR, JK = D / 32;
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int bh = blockIdx.x, b = bh / a.c.H, h = bh % a.c.H;
+  const int len = min(max(a.lens[b], 0), a.max_len);
+  const int t0 = ((int)blockIdx.y * 4 + wave) * 32;
+  if (t0 >= len) return;
+  const Q4Magic mk = q4_magic<OP>();
+  const uint32_t* kp = a.c.k + ((size_t)bh * a.c.cap + t0 + n) * (D / 8) + g * (D / 32);
+  const uint32_t* ksp = a.c.ks + (size_t)bh * NG * a.c.cap + t0 + 4 * g;
+  uint4 kop[2][JK], ks[2][NG];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint4 k = ld_row<D>(kp + (size_t)(16 * i) * (D / 8));
+#pragma unroll
+    for (int j = 0; j < JK; ++j) kop[i][j] = q4_operand<OP>(word_of(k, j), mk);
+#pragma unroll
+    for (int f = 0; f < NG; ++f) ks[i][f] = ld16(ksp + (size_t)f * a.c.cap + 16 * i);
+  }
+  float w[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+  const int first = max(0, t0 - (len - a.S)) * a.G / 16;   // rows of earlier tiles see none of these slots
+  for (int tile = first; tile < a.row_tiles && tile * 16 < a.R; ++tile) {
+    const int row = min(tile * 16 + n, a.R - 1);
+    uint4 q[JK][PIECES];
+    float sums[NG];
+    load_rows<T, D, GR>(a, b, h, row, q, sums);
+    const float z = tile * 16 + n < a.R ? a.z[(size_t)bh * a.R + row] : INFINITY;
+    const int limit = row_limit(a, len, row);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const f32x4q x = logits_of<T, D, GR>(kop[i], ks[i], q, sums);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.scale, -z));
+        w[4 * i + r] += t0 + 16 * i + 4 * g + r < limit ? p : 0.0f;
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int off = 1; off < 16; off <<= 1) w[i] += __shfl_xor(w[i], off, kWave);
+  if (n == 0)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int t = t0 + 16 * (i / 4) + 4 * g + i % 4;
+      const size_t at = (size_t)bh * a.c.cap + t;
+      if (t < len) a.weight_out[at] = a.c.weight[at] + w[i];
+    }
+}
+
+template <class T, int D, int GR, int NR, bool LOGITS>
+int launch_attend(const Kv4Attend& a, hipStream_t s) {
+  const int tiles = (a.R + 15) / 16, per = a.token_waves == 4 ? NR : 4 * NR;
+  const dim3 grid(a.c.B * a.c.H, (tiles + per - 1) / per, a.splits);
+  const size_t lds = a.token_waves == 4 ? (size_t)4 * NR * D * 64 : 0;
+  hipLaunchKernelGGL((gemm_q4_attend_kernel<T, D, GR, NR, LOGITS>), grid, dim3(256), lds, s, a);
+  CI_HIP_CHECK_LAUNCH();
+  if (a.splits > 1 || a.weights == 1) {
+    constexpr int ROWS = 256 / (D / 4);
+    const int join = a.splits > 1 ? (a.R + ROWS - 1) / ROWS : 0, weight = a.weights == 1 ? (a.max_len + 1023) / 1024 : 0;
+    hipLaunchKernelGGL((kv4_join_kernel<T, D>), dim3(join + weight, a.c.B * a.c.H), dim3(256), 0, s, a, join);
+    CI_HIP_CHECK_LAUNCH();
+  }
+  if (a.weights == 2) {
+    hipLaunchKernelGGL((gemm_q4_weights_kernel<T, D, GR>), dim3(a.c.B * a.c.H, (a.max_len + 127) / 128), dim3(256), 0, s, a);
+    CI_HIP_CHECK_LAUNCH();
+  }
+  return CI_OK;
+}
+
+template <class T, int D, int GR>
+int launch_attend_rows(const Kv4Attend& a, hipStream_t s) {
+  if (a.weights == 1) return launch_attend<T, D, GR, 1, true>(a, s);
+  return a.NR == 2 ? launch_attend<T, D, GR, 2, false>(a, s) : launch_attend<T, D, GR, 1, false>(a, s);
+}
+
+}  // namespace
+
+template <class T>
+int launch_kv4_attend_type(const Kv4Attend& a, int D, int group, hipStream_t s) {
+  if (D == 64) return group == 32 ? launch_attend_rows<T, 64, 32>(a, s) : launch_attend_rows<T, 64, 64>(a, s);
+  if (group == 32) return launch_attend_rows<T, 128, 32>(a, s);
+  return group == 64 ? launch_attend_rows<T, 128, 64>(a, s) : launch_attend_rows<T, 128, 128>(a, s);
+}
+
+}  // namespace ci

@@ -1,0 +1,131 @@
+// Numbers in 4 bits, as the weights (w4.hip) and the cache (kv4.hip) hold them, and their matrix products on gfx950.
+//
+// A group of 32, 64 or 128 elements along a row is held as codes n = 0 .. 15 with low = fp16(min) and step = fp16((max - min) / 15),
+// n = rint((x - low) / step) in fp32, and stands for low + step n.  A product with a row x of such groups is, per group,
+//   step (sum n x) + low (sum x),
+// so the matrix cores multiply the codes themselves and the two fp16 numbers enter once per group, in fp32.
+//
+// A code becomes an operand without a conversion: the bits of a code in the mantissa of 128 (bf16) are 128 + n, in that of 64 (fp16)
+// 64 + n, and one instruction puts two of them there.  The constant comes out again with the sum of x, which the matrix cores form
+// beside (a product with ones): 0.9 vector instructions an element, where a conversion takes more than 2.  It costs log2(128 / 8) = 4
+// (fp16: 3) of the 24 bits of the sums, which 16-bit results do not show; operands for fp32 results carry the codes exactly and take twice the
+// instructions.
+#pragma once
+
+#include "common.hpp"
+
+namespace ci {
+namespace {
+
+typedef float f32x4q __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8q __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8q __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2q __attribute__((ext_vector_type(2)));
+typedef float f32x2q __attribute__((ext_vector_type(2)));
+
+// What multiplies: bf16 with 128 + n, fp16 with 64 + n, bf16 with n.
+enum { kOpBF16, kOpF16, kOpExact };
+template <int OP> constexpr float kOffset = OP == kOpBF16 ? 128.0f : OP == kOpF16 ? 64.0f : 0.0f;
+template <int OP> constexpr uint32_t kMagic = OP == kOpBF16 ? 0x43004300u : 0x54005400u;
+template <int OP> constexpr uint32_t kOnes = OP == kOpF16 ? 0x3c003c00u : 0x3f803f80u;
+
+// The other operand in as many pieces as hold it whole: fp32 values in three bf16 ones, 16-bit values as they are.
+template <class D> struct Q4Type;
+template <> struct Q4Type<F32> { static constexpr int OP = kOpExact, PIECES = 3; };
+template <> struct Q4Type<F16> { static constexpr int OP = kOpF16, PIECES = 1; };
+template <> struct Q4Type<BF16> { static constexpr int OP = kOpBF16, PIECES = 1; };
+
+template <int OP>
+__device__ __forceinline__ f32x4q mfma_q4(const uint4& a, const uint4& b, f32x4q c) {
+  if constexpr (OP == kOpF16)
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8q, a), __builtin_bit_cast(f16x8q, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8q, a), __builtin_bit_cast(bf16x8q, b), c, 0, 0, 0);
+}
+
+// Mask and constant in registers of their own: an instruction with two literals does not exist, and with the constants known the compiler
+// makes two of it.
+struct Q4Magic {
+  uint32_t mask, magic;
+};
+template <int OP>
+__device__ __forceinline__ Q4Magic q4_magic() {
+  Q4Magic m{OP == kOpF16 ? 0x00f000f0u : 0x000f000fu, kMagic<OP>};
+  asm("" : "+s"(m.mask), "+v"(m.magic));
+  return m;
+}
+
+// Eight codes as an operand's eight elements: element 2 i is the nibble i of w, element 2 i + 1 the nibble i + 4.
+template <int OP>
+__device__ __forceinline__ uint4 q4_operand(uint32_t w, const Q4Magic& m) {
+  if constexpr (OP == kOpBF16)
+    return make_uint4((w & m.mask) | m.magic, ((w >> 4) & m.mask) | m.magic, ((w >> 8) & m.mask) | m.magic,
+                      ((w >> 12) & m.mask) | m.magic);
+  else if constexpr (OP == kOpF16)
+    return make_uint4(((w << 4) & m.mask) | m.magic, (w & m.mask) | m.magic, ((w >> 4) & m.mask) | m.magic,
+                      ((w >> 8) & m.mask) | m.magic);
+  else {
+    // bytes 0 .. 3 of even: nibbles 0, 2, 4, 6; a code below 16 is exact in the upper half of its fp32 image
+    const uint32_t even = w & 0x0f0f0f0fu, odd = (w >> 4) & 0x0f0f0f0fu;
+    auto pair = [](uint32_t a, uint32_t b) {
+      return __builtin_amdgcn_perm(f2u((float)(b & 0xffu)), f2u((float)(a & 0xffu)), 0x07060302u);
+    };
+    return make_uint4(pair(even, even >> 16), pair(odd, odd >> 16), pair(even >> 8, even >> 24), pair(odd >> 8, odd >> 24));
+  }
+}
+// Where an element e of eight goes in the word.
+__device__ __forceinline__ int q4_nibble(int e) { return (e >> 1) + 4 * (e & 1); }
+
+__device__ __forceinline__ uint32_t pk_bf16(float a, float b) {
+  f32x2q f;
+  f.x = a;
+  f.y = b;
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2q));
+}
+__device__ __forceinline__ float bf16_lo(uint32_t p) { return u2f(p << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t p) { return u2f(p & 0xffff0000u); }
+
+// Two fp32 values in N bf16 pieces, each the rounded rest of the ones before: 8 bits more with every piece.
+template <int N>
+__device__ __forceinline__ void split_bf16(float a, float b, uint32_t (&piece)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    piece[i] = pk_bf16(a, b);
+    if (i + 1 < N) {
+      a -= bf16_lo(piece[i]);
+      b -= bf16_hi(piece[i]);
+    }
+  }
+}
+
+__device__ __forceinline__ float half_lo(uint32_t p) { return (float)__builtin_bit_cast(half2_t, p)[0]; }
+__device__ __forceinline__ float half_hi(uint32_t p) { return (float)__builtin_bit_cast(half2_t, p)[1]; }
+
+// Step (lower half) and lowest value (upper half) of a group from its extremes; what fp16 does not hold is held at its largest.  NaN
+// extremes make both NaN.
+__device__ __forceinline__ uint32_t q4_scale(float lo, float hi) {
+  constexpr float kMax = 65504.0f;
+  float step = (hi - lo) / 15.0f;
+  if (step > kMax) step = kMax;
+  if (lo > kMax) lo = kMax;
+  if (lo < -kMax) lo = -kMax;
+  half2_t h;
+  h[0] = (_Float16)step;
+  h[1] = (_Float16)lo;
+  return __builtin_bit_cast(uint32_t, h);
+}
+__device__ __forceinline__ uint32_t q4_code(float x, uint32_t scale) {
+  const float step = half_lo(scale);
+  if (!(step > 0.0f)) return 0;
+  const float n = rintf((x - half_hi(scale)) / step);
+  return (uint32_t)fminf(fmaxf(n, 0.0f), 15.0f);
+}
+__device__ __forceinline__ float q4_value(uint32_t code, uint32_t scale) {
+  return __builtin_fmaf(half_lo(scale), (float)code, half_hi(scale));
+}
+// Extremes that a NaN takes over.
+__device__ __forceinline__ float min_nan(float a, float b) { return a < b || a != a ? a : b; }
+__device__ __forceinline__ float max_nan(float a, float b) { return a > b || a != a ? a : b; }
+
+}  // namespace
+}  // namespace ci
