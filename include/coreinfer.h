@@ -563,7 +563,8 @@ int coreinfer_kv4_read(const ci_kv4* cache, const int32_t* lens, int64_t first, 
  * as they are held, q as it is (fp32 q in three bf16 pieces), probabilities in
  * two bf16 pieces (fp32 q: three).  The order of the sums is fixed.
  * ws: coreinfer_kv4_attend_workspace_size bytes, 16-byte aligned (weights != 0: for
- * calls with weight_out).  Limits: S * (Hq / H) <= 2^20.
+ * calls with weight_out).  Calls that share a workspace must not overlap in time.
+ * Limits: S * (Hq / H) <= 2^20.
  */
 int coreinfer_kv4_attend_workspace_size(int64_t B, int64_t H, int D, int64_t S, int64_t Hq, int64_t max_len, int weights,
                                         size_t* bytes);

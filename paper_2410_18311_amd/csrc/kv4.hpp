@@ -22,6 +22,8 @@ struct Kv4 {
   int B, H, cap;
 };
 
+constexpr int kMaxSplits = 64;  // of a call over the slots: the lanes of the join keep a factor of each
+
 struct Kv4Attend {
   Kv4 c;
   const void* q;
@@ -33,11 +35,13 @@ struct Kv4Attend {
   int S, G, R, max_len;   // R = S G rows of a head of the cache
   float scale;            // of the logits, with log2(e)
   int q_vectors;
-  // partial results, [B H, splits, row_tiles 16] twice, [B H, splits, row_tiles 16, D]; log-sums [B H, R]; logits [B H, R, steps 32]
+  // Work of the launch: `blocks` workgroups (times those along the rows) share the slots of all sentences; see Shares.  wanted 0: one workgroup a head.
+  int blocks, wanted, least;
+  int row_tiles, token_waves, NR;  // tiles of 16 rows; waves of a workgroup along the slots (4 or 1); tiles of 16 rows a wave
+  int weights;                     // 0 none, 1 from stored logits, 2 from logits computed again
+  int2* place;  // [B]: a sentence's first piece and how many it has
+  // partial results [blocks, row_tiles 16] twice and [blocks, row_tiles 16, D]; log-sums [B H, R]; logits [B H, R, whole steps of slots]
   float *m, *l, *o, *z, *logits;
-  int splits, chunk, row_tiles;  // steps of 32 slots to a split; tiles of 16 rows
-  int token_waves, NR;           // waves of a workgroup along the slots (4 or 1); tiles of 16 rows a wave
-  int weights;                   // 0 none, 1 from stored logits, 2 from logits computed again
 };
 
 template <class D> int launch_kv4_attend_type(const Kv4Attend& a, int head_dim, int group, hipStream_t s);

@@ -10,8 +10,8 @@ constexpr int kCus = 256;   // of an MI355X; a workspace query knows no device
 constexpr double kLog2e = 1.4426950408889634;
 
 struct AttendPlan {
-  int R, row_tiles, NR, token_waves, splits, chunk, weights;
-  size_t m, l, o, z, logits, bytes;   // places in the workspace
+  int R, row_tiles, NR, token_waves, blocks, wanted, least, weights;
+  size_t place, m, l, o, z, logits, bytes;   // places in the workspace
 };
 
 AttendPlan attend_plan(int64_t heads, int D, int64_t S, int64_t G, int64_t max_len, bool weights) {
@@ -24,19 +24,20 @@ AttendPlan attend_plan(int64_t heads, int D, int64_t S, int64_t G, int64_t max_l
   p.token_waves = wave_tiles >= 4 ? 1 : 4;
   const int64_t row_blocks = p.token_waves == 4 ? wave_tiles : (wave_tiles + 3) / 4;
   const int64_t steps = (max_len + 31) / 32, blocks = heads * row_blocks;
-  // enough workgroups for the chip, and no split below two steps a wave
-  const int64_t wanted = p.token_waves == 4 ? 2 * kCus : kCus;
-  const int64_t most = std::max<int64_t>(1, steps / (p.token_waves == 4 ? 8 : 16));
-  const int64_t splits = std::min(most, std::max<int64_t>(1, wanted / blocks));
-  p.chunk = (int)((steps + splits - 1) / splits);
-  p.splits = (int)((steps + p.chunk - 1) / p.chunk);
+  // Three workgroups a compute unit where waves share the slots (what the registers leave room for), one where they share the rows; no
+  // piece below two steps a wave, respectively 16 steps.
+  const int64_t wanted = (p.token_waves == 4 ? 3 : 1) * kCus;
+  p.least = p.token_waves == 4 ? 8 : 16;
+  p.wanted = blocks * 2 > wanted || steps <= p.least ? 0 : (int)(wanted / row_blocks);
+  p.blocks = (int)heads + p.wanted;
   auto take = [&](size_t floats) {
     const size_t at = p.bytes;
     p.bytes += (floats * sizeof(float) + 255) / 256 * 256;
     return at;
   };
   p.bytes = 0;
-  const size_t rows = p.splits > 1 ? (size_t)heads * p.splits * p.row_tiles * 16 : 0;
+  const size_t rows = p.wanted ? (size_t)p.blocks * p.row_tiles * 16 : 0;
+  p.place = take(p.wanted ? 2 * (size_t)heads : 0);   // as many sentences at most
   p.m = take(rows);
   p.l = take(rows);
   p.o = take(rows * D);
@@ -74,13 +75,15 @@ int launch_kv4_attend(const ci_kv4& c, const void* q, int64_t S, int64_t G, cons
   const int e = elem_bytes(dtype);
   a.q_vectors = aligned16(q) && stride[0] * e % 16 == 0 && stride[1] * e % 16 == 0 && stride[2] * e % 16 == 0;
   char* base = reinterpret_cast<char*>(ws);
+  a.place = reinterpret_cast<int2*>(base + p.place);
   a.m = reinterpret_cast<float*>(base + p.m);
   a.l = reinterpret_cast<float*>(base + p.l);
   a.o = reinterpret_cast<float*>(base + p.o);
   a.z = reinterpret_cast<float*>(base + p.z);
   a.logits = reinterpret_cast<float*>(base + p.logits);
-  a.splits = p.splits;
-  a.chunk = p.chunk;
+  a.blocks = p.blocks;
+  a.wanted = p.wanted;
+  a.least = p.least;
   a.row_tiles = p.row_tiles;
   a.token_waves = p.token_waves;
   a.NR = p.NR;

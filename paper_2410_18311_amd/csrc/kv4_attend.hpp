@@ -125,21 +125,168 @@ __device__ __forceinline__ void store_lse(const Kv4Attend& a, int b, int h, int 
   a.lse[((int64_t)b * a.S + s) * a.c.H * a.G + h * a.G + i] = z == INFINITY ? -INFINITY : z * 0.69314718055994531f;
 }
 
+// How the slots of all sentences are shared out: pieces of `chunk` steps, so that a long sentence among short ones has as many workgroups
+// as its length asks for.  Everything follows from lens, in every wave for itself.
+struct Shares {
+  int chunk;
+  __device__ static int steps_of(const Kv4Attend& a, int b) { return (min(max(a.lens[b], 0), a.max_len) + 31) / 32; }
+  __device__ int count(int steps) const { return max(1, (steps + chunk - 1) / chunk); }
+
+  __device__ explicit Shares(const Kv4Attend& a) {
+    if (a.wanted == 0) {
+      chunk = 1 << 30;
+      return;
+    }
+    int64_t total = 0;
+    int longest = 0;
+    if (a.c.B == 1) {
+      total = longest = steps_of(a, 0);
+    } else {
+      for (int b = threadIdx.x & 63; b < a.c.B; b += 64) {
+        const int n = steps_of(a, b);
+        total += n;
+        longest = max(longest, n);
+      }
+#pragma unroll
+      for (int off = 1; off < 64; off <<= 1) {
+        total += __shfl_xor(total, off, kWave);
+        longest = max(longest, __shfl_xor(longest, off, kWave));
+      }
+    }
+    // all pieces together are at most wanted + B H: a sentence's last one need not be full
+    const int64_t even = (total * a.c.H + a.wanted - 1) / a.wanted, least = max(a.least, (longest + kMaxSplits - 1) / kMaxSplits);
+    const int64_t steps = max(even, least);
+    chunk = __builtin_amdgcn_readfirstlane((int)((steps + a.token_waves - 1) / a.token_waves * a.token_waves));
+  }
+  // The sentence of piece `at` and the pieces before that sentence's; b = B where there is no such piece.
+  __device__ void find(const Kv4Attend& a, int at, int* b, int* first) const {
+    if (a.wanted == 0) {
+      *b = at / a.c.H;
+      *first = *b * a.c.H;
+      return;
+    }
+    if (a.c.B == 1) {
+      *b = at < count(steps_of(a, 0)) * a.c.H ? 0 : 1;
+      *first = 0;
+      return;
+    }
+    const int lane = threadIdx.x & 63;
+    int base = 0;
+    for (int b0 = 0; b0 < a.c.B; b0 += 64) {
+      const int mine = b0 + lane < a.c.B ? count(steps_of(a, b0 + lane)) * a.c.H : 0;
+      int upto = mine;
+#pragma unroll
+      for (int off = 1; off < 64; off <<= 1) {
+        const int n = __shfl_up(upto, off, kWave);
+        if (lane >= off) upto += n;
+      }
+      const uint64_t past = __ballot(base + upto > at);
+      if (past) {
+        const int hit = __builtin_ctzll(past);
+        *b = b0 + hit;
+        *first = base + __shfl(upto - mine, hit, kWave);
+        return;
+      }
+      base += __shfl(upto, 63, kWave);
+    }
+    *b = a.c.B;
+    *first = base;
+  }
+};
+
+// A row's maximum and sum over its pieces (their values `next` apart), which N neighbouring lanes share; factor[i]: of piece N i + the
+// lane's number, against that maximum.
+template <int N>
+__device__ __forceinline__ void join_pieces(const float* m, const float* l, size_t next, int pieces, float* top, float* total,
+                                            float (&factor)[kMaxSplits / N]) {
+  const int lane = threadIdx.x % N;
+  float mi[kMaxSplits / N], li[kMaxSplits / N], t = -INFINITY, sum = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kMaxSplits / N; ++i) {
+    const int s = lane + N * i;
+    mi[i] = s < pieces ? m[s * next] : -INFINITY;
+    li[i] = s < pieces ? l[s * next] : 0.0f;
+  }
+#pragma unroll
+  for (int i = 0; i < kMaxSplits / N; ++i) t = fmaxf(t, mi[i]);
+#pragma unroll
+  for (int off = 1; off < N; off <<= 1) t = fmaxf(t, __shfl_xor(t, off, kWave));
+#pragma unroll
+  for (int i = 0; i < kMaxSplits / N; ++i) {
+    // a piece without a maximum saw nothing, or nothing but NaN
+    factor[i] = mi[i] == -INFINITY ? (li[i] != 0.0f ? NAN : 0.0f) : __builtin_amdgcn_exp2f(mi[i] - t);
+    sum += mi[i] == -INFINITY ? li[i] : li[i] * factor[i];
+  }
+#pragma unroll
+  for (int off = 1; off < N; off <<= 1) sum += __shfl_xor(sum, off, kWave);
+  *top = t;
+  *total = sum;
+}
+
+// Waves of a SIMD that the registers are to leave room for.
+template <class T, int D, int GR, int NR> constexpr int kAttendWaves = NR > 1 ? 1 : D / GR == 4 || T::VEC == 4 ? 2 : 3;
+
 template <class T, int D, int GR, int NR, bool LOGITS>
-__global__ __launch_bounds__(256) void gemm_q4_attend_kernel(Kv4Attend a) {
+__global__ __launch_bounds__(256, (kAttendWaves<T, D, GR, NR>)) void gemm_q4_attend_kernel(Kv4Attend a) {
   constexpr int OP = Q4Type<T>::OP, OPV = AttendType<T>::OPV, PIECES = Q4Type<T>::PIECES, P = AttendType<T>::P;
   constexpr int NG = D / GR, JK = D / 32, JV = D / 16;
   __shared__ float ml[2][4][NR][16];
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int bh = blockIdx.x, b = bh / a.c.H, h = bh % a.c.H, split = blockIdx.z;
+  const Shares shares(a);
+  int b, first;
+  shares.find(a, blockIdx.x, &b, &first);
+  b = __builtin_amdgcn_readfirstlane(b);
+  first = __builtin_amdgcn_readfirstlane(first);
+  if (b >= a.c.B) return;
+  const int h = ((int)blockIdx.x - first) % a.c.H, split = ((int)blockIdx.x - first) / a.c.H, bh = b * a.c.H + h;
   const bool joined = a.token_waves == 4;
   const int tile0 = (joined ? (int)blockIdx.y : (int)blockIdx.y * 4 + wave) * NR;
   const int row0 = tile0 * 16;
   if (!joined && row0 >= a.R) return;   // no barrier follows
   const int len = min(max(a.lens[b], 0), a.max_len);
+  const int pieces = a.wanted == 0 ? 1 : shares.count((len + 31) / 32);
+  if (a.wanted && (int)blockIdx.x == first && blockIdx.y == 0 && threadIdx.x == 0) a.place[b] = make_int2(first, pieces);   // for the join
 
+  const int low_limit = row_limit(a, len, row0), high_limit = row_limit(a, len, min(row0 + 16 * NR, a.R) - 1);
+
+  // where the lane's share of a step lies
+  const uint32_t* kp = a.c.k + ((size_t)bh * a.c.cap + n) * (D / 8) + g * (D / 32);
+  const uint32_t* vp = a.c.v + ((size_t)bh * (a.c.cap / 4) + g) * (D / 2) + n * (D / 32);
+  const uint32_t* ksp = a.c.ks + (size_t)bh * NG * a.c.cap + 4 * g;
+  const uint32_t* vsp = a.c.vs + (size_t)bh * NG * a.c.cap + 4 * g;
+  // Keys and values are each requested again as soon as they have been used: the keys' way is behind the softmax and the values' product, and
+  // the other way round, with one set of registers.  (A ring in LDS with twice as much on its way was no faster.)
+  uint4 k[2], ks[2][NG], v[2], vs[2][NG];
+  auto load_keys = [&](int step) {
+    const int t = step * 32;   // t + 32 <= cap, which is whole steps
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      k[i] = ld_row<D>(kp + (size_t)(t + 16 * i) * (D / 8));
+#pragma unroll
+      for (int f = 0; f < NG; ++f) ks[i][f] = ld16(ksp + (size_t)f * a.c.cap + t + 16 * i);
+    }
+  };
+  auto load_values = [&](int step) {
+    const int t = step * 32;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      v[i] = ld_row<D>(vp + (size_t)(t / 4 + 4 * i) * (D / 2));
+#pragma unroll
+      for (int f = 0; f < NG; ++f) vs[i][f] = ld16(vsp + (size_t)f * a.c.cap + t + 16 * i);
+    }
+  };
+  const int begin = split ? split * shares.chunk : 0;   // one piece: the chunk may be anything
+  const int step0 = begin + (joined ? wave : 0), stride = joined ? 4 : 1;
+  const int end = pieces == 1 ? 1 << 30 : begin + shares.chunk, steps = min(end, (max(high_limit, 0) + 31) / 32);
+  const Q4Magic mk = q4_magic<OP>(), mv = q4_magic<OPV>();
+  const uint4 ones = make_uint4(kOnes<OPV>, kOnes<OPV>, kOnes<OPV>, kOnes<OPV>);
+
+  if (step0 < steps) {
+    load_keys(step0);
+    load_values(step0);
+  }
   uint4 q[NR][JK][PIECES];
   float sums[NR][NG];
   int limit[NR];
@@ -149,7 +296,6 @@ __global__ __launch_bounds__(256) void gemm_q4_attend_kernel(Kv4Attend a) {
     load_rows<T, D, GR>(a, b, h, row, q[u], sums[u]);
     limit[u] = row_limit(a, len, row);
   }
-  const int low_limit = row_limit(a, len, row0), high_limit = row_limit(a, len, min(row0 + 16 * NR, a.R) - 1);
 
   f32x4q o[NR][JV], one[NR][NG];
   float m[NR], l[NR], low[NR][NG];
@@ -163,53 +309,27 @@ __global__ __launch_bounds__(256) void gemm_q4_attend_kernel(Kv4Attend a) {
     for (int j = 0; j < JV; ++j) o[u][j] = f32x4q{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
-  // where the lane's share of a step lies
-  const uint32_t* kp = a.c.k + ((size_t)bh * a.c.cap + n) * (D / 8) + g * (D / 32);
-  const uint32_t* vp = a.c.v + ((size_t)bh * (a.c.cap / 4) + g) * (D / 2) + n * (D / 32);
-  const uint32_t* ksp = a.c.ks + (size_t)bh * NG * a.c.cap + 4 * g;
-  const uint32_t* vsp = a.c.vs + (size_t)bh * NG * a.c.cap + 4 * g;
-  struct Stage {
-    uint4 k[2], v[2], ks[2][NG], vs[2][NG];
-  };
-  const int step0 = split * a.chunk + (joined ? wave : 0), stride = joined ? 4 : 1;
-  const int steps = min((split + 1) * a.chunk, (max(high_limit, 0) + 31) / 32);
-  auto load = [&](Stage& st, int step) {
-    const int t = step * 32;   // t + 32 <= cap, which is whole steps
+  for (int step = step0; step < steps; step += stride) {
+    const int t0 = step * 32, after = min(step + stride, steps - 1);
+    const bool partial = t0 + 32 > low_limit;
+    float xs[NR][8];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      st.k[i] = ld_row<D>(kp + (size_t)(t + 16 * i) * (D / 8));
-      st.v[i] = ld_row<D>(vp + (size_t)(t / 4 + 4 * i) * (D / 2));
+      uint4 kop[JK];
 #pragma unroll
-      for (int f = 0; f < NG; ++f) {
-        st.ks[i][f] = ld16(ksp + (size_t)f * a.c.cap + t + 16 * i);
-        st.vs[i][f] = ld16(vsp + (size_t)f * a.c.cap + t + 16 * i);
+      for (int j = 0; j < JK; ++j) kop[j] = q4_operand<OP>(word_of(k[i], j), mk);
+#pragma unroll
+      for (int u = 0; u < NR; ++u) {
+        const f32x4q y = logits_of<T, D, GR>(kop, ks[i], q[u], sums[u]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) xs[u][4 * i + r] = y[r];
       }
     }
-  };
-  const Q4Magic mk = q4_magic<OP>(), mv = q4_magic<OPV>();
-  const uint4 ones = make_uint4(kOnes<OPV>, kOnes<OPV>, kOnes<OPV>, kOnes<OPV>);
-
-  Stage cur, next;
-  if (step0 < steps) load(cur, step0);
-  for (int step = step0; step < steps; step += stride) {
-    load(next, min(step + stride, steps - 1));
-    const int t0 = step * 32;
-    const bool partial = t0 + 32 > low_limit;
-    uint4 kop[2][JK];
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int j = 0; j < JK; ++j) kop[i][j] = q4_operand<OP>(word_of(cur.k[i], j), mk);
+    load_keys(after);
     uint4 piece[NR][NG][P];
 #pragma unroll
     for (int u = NR - 1; u >= 0; --u) {   // later rows see more
-      float x[8];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const f32x4q y = logits_of<T, D, GR>(kop[i], cur.ks[i], q[u], sums[u]);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) x[4 * i + r] = y[r];
-      }
+      float (&x)[8] = xs[u];
       if (partial) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -220,10 +340,10 @@ __global__ __launch_bounds__(256) void gemm_q4_attend_kernel(Kv4Attend a) {
           const int see = limit[u] - (t0 + 16 * i + 4 * g);
 #pragma unroll
           for (int f = 0; f < NG; ++f) {
-            cur.vs[i][f].x = see > 0 ? cur.vs[i][f].x : 0;
-            cur.vs[i][f].y = see > 1 ? cur.vs[i][f].y : 0;
-            cur.vs[i][f].z = see > 2 ? cur.vs[i][f].z : 0;
-            cur.vs[i][f].w = see > 3 ? cur.vs[i][f].w : 0;
+            vs[i][f].x = see > 0 ? vs[i][f].x : 0;
+            vs[i][f].y = see > 1 ? vs[i][f].y : 0;
+            vs[i][f].z = see > 2 ? vs[i][f].z : 0;
+            vs[i][f].w = see > 3 ? vs[i][f].w : 0;
           }
         }
       }
@@ -261,7 +381,7 @@ __global__ __launch_bounds__(256) void gemm_q4_attend_kernel(Kv4Attend a) {
         uint32_t p[4][P];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const uint32_t s0 = word_of(cur.vs[i / 2][f], 2 * (i % 2)), s1 = word_of(cur.vs[i / 2][f], 2 * (i % 2) + 1);
+          const uint32_t s0 = word_of(vs[i / 2][f], 2 * (i % 2)), s1 = word_of(vs[i / 2][f], 2 * (i % 2) + 1);
           low[u][f] = __builtin_fmaf(half_hi(s0), x[2 * i], low[u][f]);
           low[u][f] = __builtin_fmaf(half_hi(s1), x[2 * i + 1], low[u][f]);
           split_bf16<P>(half_lo(s0) * x[2 * i], half_lo(s1) * x[2 * i + 1], p[i]);
@@ -279,7 +399,7 @@ __global__ __launch_bounds__(256) void gemm_q4_attend_kernel(Kv4Attend a) {
       uint4 vop[4];
       uint32_t w[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = word_of(cur.v[i / 2], (D / 64) * (i % 2) + f);
+      for (int i = 0; i < 4; ++i) w[i] = word_of(v[i / 2], (D / 64) * (i % 2) + f);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         uint32_t e[4];
@@ -301,7 +421,7 @@ __global__ __launch_bounds__(256) void gemm_q4_attend_kernel(Kv4Attend a) {
 #pragma unroll
           for (int c = 0; c < P; ++c) o[u][4 * f + i] = mfma_q4<OPV>(vop[i], piece[u][(4 * f + i) * 16 / GR][c], o[u][4 * f + i]);
     }
-    cur = next;
+    load_values(after);
   }
 
   // sums over the lanes of a row, and the constants that entered with the codes
@@ -318,13 +438,13 @@ __global__ __launch_bounds__(256) void gemm_q4_attend_kernel(Kv4Attend a) {
 #pragma unroll
     for (int j = 0; j < JV; ++j) o[u][j] += low[u][j * 16 / GR];
   }
-  const size_t part = ((size_t)bh * a.splits + split) * a.row_tiles * 16;
+  const size_t part = (size_t)blockIdx.x * a.row_tiles * 16;
   if (!joined) {
 #pragma unroll
     for (int u = 0; u < NR; ++u) {
       const int row = row0 + 16 * u + n;
       if (row >= a.R) continue;
-      if (a.splits > 1) {
+      if (pieces > 1) {
         if (g == 0) a.m[part + row] = m[u], a.l[part + row] = l[u];
 #pragma unroll
         for (int j = 0; j < JV; ++j)
@@ -354,14 +474,16 @@ __global__ __launch_bounds__(256) void gemm_q4_attend_kernel(Kv4Attend a) {
 #pragma unroll
     for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[0][w][u][n]);
     const float f = m[u] == -INFINITY ? (l[u] != l[u] ? l[u] : 0.0f) : __builtin_amdgcn_exp2f(m[u] - top);   // a row of NaNs stays one
+    if (row0 + 16 * u + n < a.R)
 #pragma unroll
-    for (int j = 0; j < JV; ++j)
-      shared[((wave * NR + u) * JV + j) * 64 + lane] = make_float4(o[u][j][0] * f, o[u][j][1] * f, o[u][j][2] * f, o[u][j][3] * f);
+      for (int j = 0; j < JV; ++j)
+        shared[((wave * NR + u) * JV + j) * 64 + lane] = make_float4(o[u][j][0] * f, o[u][j][1] * f, o[u][j][2] * f, o[u][j][3] * f);
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < NR * JV * 64; i += 256) {
-    const int at = i & 63, j = (i >> 6) % JV, u = (i >> 6) / JV, col = at & 15, row = row0 + 16 * u + col;
-    if (row >= a.R) continue;
+  const int rows = min(NR * 16, a.R - row0);
+  for (int i = threadIdx.x; i < rows * (D / 4); i += 256) {
+    const int r = i / (D / 4), d = i % (D / 4) * 4, u = r / 16, col = r % 16, row = row0 + r;
+    const int at = (u * JV + d / 16) * 64 + d % 16 / 4 * 16 + col;
     float top = -INFINITY, total = 0.0f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[0][w][u][col]);
@@ -373,12 +495,11 @@ __global__ __launch_bounds__(256) void gemm_q4_attend_kernel(Kv4Attend a) {
     f32x4q v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      const float4 s = shared[((w * NR + u) * JV + j) * 64 + at];
+      const float4 s = shared[w * NR * JV * 64 + at];
       v[0] += s.x; v[1] += s.y; v[2] += s.z; v[3] += s.w;
     }
-    const int d = 16 * j + 4 * (at >> 4);
-    if (a.splits > 1) {
-      *reinterpret_cast<float4*>(a.o + (part + row) * D + d) = make_float4(v[0], v[1], v[2], v[3]);
+    if (pieces > 1) {
+      *reinterpret_cast<f32x4q*>(a.o + (part + row) * D + d) = v;
       if (d == 0) a.m[part + row] = top, a.l[part + row] = total;
     } else {
       const float z = log_sum(top, total);
@@ -391,76 +512,82 @@ __global__ __launch_bounds__(256) void gemm_q4_attend_kernel(Kv4Attend a) {
   }
 }
 
-// A row's maximum and sum over the splits.
-__device__ __forceinline__ void join_split(const Kv4Attend& a, size_t bh, int row, float* top, float* total) {
-  const size_t at = bh * a.splits * a.row_tiles * 16 + row, next = (size_t)a.row_tiles * 16;
-  float m = -INFINITY, l = 0.0f;
-  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.m[at + s * next]);
-  for (int s = 0; s < a.splits; ++s) {
-    const float ms = a.m[at + s * next], ls = a.l[at + s * next];
-    l += ms == -INFINITY ? ls : ls * __builtin_amdgcn_exp2f(ms - m);
-  }
-  *top = m;
-  *total = l;
-}
-
-// The splits' results, in their order: workgroups x < join_blocks; the others add the weights of 1024 slots up from the stored logits.
+// The pieces' results in their order (workgroups x < join_blocks), and the weights that up to 16 rows give each slot, from the stored logits
+// (the others, 256 slots each).  Latency is all of it, so whatever does not depend on the rows' sums is requested ahead of them, and
+// workgroups are a wave each, for as many as possible to wait at a time.
 template <class T, int D>
-__global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Attend a, int join_blocks) {
+__global__ __launch_bounds__(64) void kv4_join_kernel(Kv4Attend a, int join_blocks) {
   const int bh = blockIdx.y, b = bh / a.c.H, h = bh % a.c.H;
+  const int2 place = a.wanted == 0 ? make_int2(b * a.c.H, 1) : a.place[b];
+  const int pieces = place.y;
+  const size_t next = (size_t)a.c.H * a.row_tiles * 16, base = ((size_t)place.x + h) * a.row_tiles * 16;
   if ((int)blockIdx.x < join_blocks) {
-    constexpr int ROWS = 256 / (D / 4);
-    const int row = blockIdx.x * ROWS + threadIdx.x / (D / 4), d = threadIdx.x % (D / 4) * 4;
-    if (row >= a.R) return;
-    float top, total;
-    join_split(a, bh, row, &top, &total);
-    const size_t at = (size_t)bh * a.splits * a.row_tiles * 16 + row, next = (size_t)a.row_tiles * 16;
-    f32x4q v = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int s = 0; s < a.splits; ++s) {
-      const float ms = a.m[at + s * next], f = ms == -INFINITY ? (a.l[at + s * next] != 0.0f ? NAN : 0.0f) : __builtin_amdgcn_exp2f(ms - top);
-      const float4 p = *reinterpret_cast<const float4*>(a.o + (at + s * next) * D + d);
-      v[0] += p.x * f; v[1] += p.y * f; v[2] += p.z * f; v[3] += p.w * f;
+    if (pieces == 1) return;   // written where it was computed
+    constexpr int N = D / 4, ROWS = 64 / N, AHEAD = 8;   // lanes of a row
+    const int r = blockIdx.x * ROWS + threadIdx.x / N, row = min(r, a.R - 1), d = threadIdx.x % N * 4;
+    const size_t at = base + row;
+    f32x4q p[AHEAD], v = {0.0f, 0.0f, 0.0f, 0.0f};
+    auto piece = [&](int s) { return *reinterpret_cast<const f32x4q*>(a.o + (at + s * next) * D + d); };
+#pragma unroll
+    for (int s = 0; s < AHEAD; ++s) p[s] = piece(min(s, pieces - 1));
+    float top, total, factor[kMaxSplits / N];
+    join_pieces<N>(a.m + at, a.l + at, next, pieces, &top, &total, factor);
+    auto factor_of = [&](float f, int s) { return __shfl(f, (threadIdx.x & 63) / N * N + s % N, kWave); };
+#pragma unroll
+    for (int s = 0; s < AHEAD; ++s) {
+      const float f = factor_of(factor[0], s);
+      if (s < pieces) v += p[s] * f;
     }
+#pragma unroll
+    for (int i = 0; i < kMaxSplits / N; ++i)
+#pragma unroll 8
+      for (int s = max(AHEAD, N * i); s < min(pieces, N * (i + 1)); ++s) v += piece(s) * factor_of(factor[i], s);
+    if (r >= a.R) return;
     const float z = log_sum(top, total);
     store_out<T>(a, D, b, h, row, d, v * (total == 0.0f ? 0.0f : 1.0f / total));
     if (d == 0) {
       store_lse(a, b, h, row, z);
-      if (a.weights) a.z[(size_t)bh * a.R + row] = z;
+      if (a.weights == 2) a.z[(size_t)bh * a.R + row] = z;
     }
     return;
   }
   __shared__ float zs[16];
-  if ((int)threadIdx.x < a.R) {
-    float z;
-    if (a.splits > 1) {
-      float top, total;
-      join_split(a, bh, threadIdx.x, &top, &total);
-      z = log_sum(top, total);
-    } else {
-      z = a.z[(size_t)bh * a.R + threadIdx.x];
-    }
-    zs[threadIdx.x] = z;
+  const int len = min(max(a.lens[b], 0), a.max_len);
+  const int t0 = ((int)blockIdx.x - join_blocks) * 256 + threadIdx.x * 4, pitch = (a.max_len + 31) / 32 * 32;
+  if (t0 - (int)threadIdx.x * 4 >= len) return;   // the whole workgroup
+  const float* logits = a.logits + (size_t)bh * a.R * pitch + min(t0, pitch - 4);
+  const float* before = a.c.weight + (size_t)bh * a.c.cap + min(t0, pitch - 4);
+  constexpr int AHEAD = 4;
+  f32x4q x[AHEAD];
+#pragma unroll
+  for (int r = 0; r < AHEAD; ++r) x[r] = *reinterpret_cast<const f32x4q*>(logits + (size_t)min(r, a.R - 1) * pitch);
+  float w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = before[i];
+  if (pieces > 1) {
+    const int r = threadIdx.x >> 2;   // four lanes a row
+    const size_t at = base + min(r, a.R - 1);
+    float top, total, factor[kMaxSplits / 4];
+    join_pieces<4>(a.m + at, a.l + at, next, pieces, &top, &total, factor);
+    if ((threadIdx.x & 3) == 0) zs[r] = log_sum(top, total);
+  } else if ((int)threadIdx.x < a.R) {
+    zs[threadIdx.x] = a.z[(size_t)bh * a.R + threadIdx.x];
   }
   __syncthreads();
-  const int len = min(max(a.lens[b], 0), a.max_len);
-  const int pitch = (a.max_len + 31) / 32 * 32;
-  const int t0 = ((int)blockIdx.x - join_blocks) * 1024 + threadIdx.x * 4;
-  if (t0 >= len) return;
-  float w[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int r = 0; r < a.R; ++r) {
-    if (t0 >= row_limit(a, len, r)) continue;   // also: no logits were stored there
-    const float4 x = *reinterpret_cast<const float4*>(a.logits + ((size_t)bh * a.R + r) * pitch + t0);
-    w[0] += __builtin_amdgcn_exp2f(x.x - zs[r]);
-    w[1] += __builtin_amdgcn_exp2f(x.y - zs[r]);
-    w[2] += __builtin_amdgcn_exp2f(x.z - zs[r]);
-    w[3] += __builtin_amdgcn_exp2f(x.w - zs[r]);
-  }
+  f32x4q sum = {0.0f, 0.0f, 0.0f, 0.0f};
+  auto add = [&](int r, const f32x4q& y) {
+    if (t0 >= row_limit(a, len, r)) return;   // also: no logits were stored there
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] += __builtin_amdgcn_exp2f(y[i] - zs[r]);
+  };
+#pragma unroll
+  for (int r = 0; r < AHEAD; ++r)
+    if (r < a.R) add(r, x[r]);
+#pragma unroll 4
+  for (int r = AHEAD; r < a.R; ++r) add(r, *reinterpret_cast<const f32x4q*>(logits + (size_t)r * pitch));
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    if (t0 + i < len) {
-      const size_t at = (size_t)bh * a.c.cap + t0 + i;
-      a.weight_out[at] = a.c.weight[at] + w[i];
-    }
+    if (t0 + i < len) a.weight_out[(size_t)bh * a.c.cap + t0 + i] = w[i] + sum[i];
 }
 
 // Weights of many rows: the logits are computed again, 32 slots a wave against all rows that see them, and every slot's sum stays in its
@@ -521,14 +648,14 @@ __global__ __launch_bounds__(256) void gemm_q4_weights_kernel(Kv4Attend a) {
 template <class T, int D, int GR, int NR, bool LOGITS>
 int launch_attend(const Kv4Attend& a, hipStream_t s) {
   const int tiles = (a.R + 15) / 16, per = a.token_waves == 4 ? NR : 4 * NR;
-  const dim3 grid(a.c.B * a.c.H, (tiles + per - 1) / per, a.splits);
+  const dim3 grid(a.blocks, (tiles + per - 1) / per);
   const size_t lds = a.token_waves == 4 ? (size_t)4 * NR * D * 64 : 0;
   hipLaunchKernelGGL((gemm_q4_attend_kernel<T, D, GR, NR, LOGITS>), grid, dim3(256), lds, s, a);
   CI_HIP_CHECK_LAUNCH();
-  if (a.splits > 1 || a.weights == 1) {
-    constexpr int ROWS = 256 / (D / 4);
-    const int join = a.splits > 1 ? (a.R + ROWS - 1) / ROWS : 0, weight = a.weights == 1 ? (a.max_len + 1023) / 1024 : 0;
-    hipLaunchKernelGGL((kv4_join_kernel<T, D>), dim3(join + weight, a.c.B * a.c.H), dim3(256), 0, s, a, join);
+  if (a.wanted || a.weights == 1) {
+    constexpr int ROWS = 64 / (D / 4);
+    const int join = a.wanted ? (a.R + ROWS - 1) / ROWS : 0, weight = a.weights == 1 ? (a.max_len + 255) / 256 : 0;
+    hipLaunchKernelGGL((kv4_join_kernel<T, D>), dim3(join + weight, a.c.B * a.c.H), dim3(64), 0, s, a, join);
     CI_HIP_CHECK_LAUNCH();
   }
   if (a.weights == 2) {

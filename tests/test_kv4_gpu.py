@@ -321,6 +321,33 @@ def test_attention_repeats_to_the_bit_on_another_stream_and_in_a_graph(lib):
             assert torch.equal(caches[0].pos, caches[1].pos) and torch.equal(counts[0][0], counts[1][0])
 
 
+def test_one_workspace_serves_calls_of_other_sizes(lib):
+    """Whatever the last call left in it."""
+    calls = []
+    for B, H, G, T, S, D, group, dtype in ((1, 2, 1, 900, 1, 64, 64, F16), (3, 40, 1, 700, 1, 128, 64, BF16),
+                                           (1, 1, 8, 3000, 1, 128, 128, F16), (1, 3, 1, 800, 40, 128, 32, F16),
+                                           (2, 2, 2, 1500, 100, 64, 32, BF16), (1, 2, 1, 20, 1, 64, 64, F32)):
+        cache, _, _ = _filled(lib, B, H, T, D, group, dtype, T)
+        calls.append((cache, _rand((B, S, H * G, D), dtype, S), _ints(*[T - 5 * b for b in range(B)])))
+    alone = [lib.kv4_attend(q, c, n, weight_out=torch.empty_like(c.weight)) for c, q, n in calls]
+    need = max(lib.kv4_attend_workspace_size(c, q.shape[1], q.shape[2], c.cap, True) for c, q, _ in calls)
+    ws = torch.full((need,), 0xff, dtype=torch.uint8, device=DEV)
+    for i in (0, 1, 2, 3, 4, 5, 2, 1, 0, 4, 3, 1, 5):
+        c, q, n = calls[i]
+        assert torch.equal(lib.kv4_attend(q, c, n, weight_out=torch.empty_like(c.weight), ws=ws), alone[i]), i
+        assert torch.equal(lib.kv4_attend(q, c, n, ws=ws), alone[i]), i
+
+
+def test_many_sentences_of_very_different_lengths(lib):
+    """Pieces of the slots are found by length: one long sentence among short ones, and more sentences than lanes."""
+    g = torch.Generator().manual_seed(3)
+    lens = torch.randint(0, 40, (70,), generator=g).tolist()
+    lens[33], lens[69], lens[5] = 2000, 700, 0
+    _check_attend(lib, 70, 1, 1, 2000, 1, 64, 64, F16, lens=lens)
+    _check_attend(lib, 4, 3, 4, 2500, 1, 128, 64, BF16, lens=[3, 2500, 0, 90])
+    _check_attend(lib, 3, 1, 2, 1500, 40, 64, 32, F16, lens=[1500, 20, 333])
+
+
 # ----------------------------------------------------------------------------------------------------- eviction
 
 def _check_evict(lib, B, H, T, D, group, budget, recent, lens=None, weight=None, pos=None, nxt=None, alias=True, max_len=None,
