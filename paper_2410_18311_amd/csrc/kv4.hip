@@ -1,6 +1,7 @@
 // Writing keys and values to a cache in 4 bits, reading them back, and evicting the slots that got the least weight (kv4.hpp).
 // All three are bound by the bytes they move, or, for single tokens, by their launches.
 #include <algorithm>
+#include <type_traits>
 
 #include "kv4.hpp"
 
@@ -168,6 +169,8 @@ __global__ __launch_bounds__(128) void kv4_read_kernel(Kv4 c, const int32_t* len
 
 // ---- eviction --------------------------------------------------------------------------------------------------------------------
 
+constexpr int kMovedHere = 256;  // moves of a head that the workgroup which plans them does itself
+
 struct EvictArgs {
   Kv4 c;
   const int32_t *lens, *next;
@@ -178,39 +181,70 @@ struct EvictArgs {
   int32_t *count, *holes, *movers;   // [B H], [B H, max_moves] twice
 };
 
-constexpr int kPlanThreads = 1024;
+// Inclusive sum over the lanes of a wave, without the LDS.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
+  auto add = [&](auto ctrl, auto rows) {
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+  };
+  constexpr std::integral_constant<int, 0xf> all{};
+  add(std::integral_constant<int, 0x111>{}, all);   // from 1, 2, 4 and 8 lanes below within sixteen
+  add(std::integral_constant<int, 0x112>{}, all);
+  add(std::integral_constant<int, 0x114>{}, all);
+  add(std::integral_constant<int, 0x118>{}, all);
+  add(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});   // the sums of the sixteens before
+  add(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
+  return v;
+}
 
-// Exclusive sum over the workgroup of a pair of counts below 2^32 in one word each; all threads take part.
-__device__ __forceinline__ uint64_t block_scan(uint64_t x, uint64_t* sums, uint64_t* total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint64_t v = x;
+// Exclusive sums over the workgroup; all threads take part.  sums: THREADS / 64 words that no other call uses.  Returns the total.
+template <int THREADS>
+__device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* sums, uint32_t* before) {
+  const uint32_t v = wave_scan(x);
+  const int wave = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) == 63) sums[wave] = v;
+  __syncthreads();
+  uint32_t lower = 0, all = 0;
 #pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const uint64_t u = __shfl_up(v, off, kWave);
-    if (lane >= off) v += u;
-  }
-  __syncthreads();
-  if (lane == 63) sums[wave] = v;
-  __syncthreads();
-  uint64_t before = 0, all = 0;
-  for (int w = 0; w < kPlanThreads / 64; ++w) {
-    const uint64_t s = sums[w];
-    before += w < wave ? s : 0;
+  for (int w = 0; w < THREADS / 64; ++w) {
+    const uint32_t s = sums[w];
+    lower += w < wave ? s : 0;
     all += s;
   }
-  *total = all;
-  return before + v - x;
+  *before = lower + v - x;
+  return all;
+}
+
+// A head's slot moved to another: sixteen lanes take the row of keys, the half-words of the values, the scales.
+template <int D, int GR>
+__device__ __forceinline__ void move_slot(const Kv4& c, size_t head, size_t to, size_t of, int n) {
+  constexpr int NG = D / GR;
+  const size_t cap = c.cap;
+  uint32_t* k = c.k + head * cap * (D / 8);
+  uint16_t* v = reinterpret_cast<uint16_t*>(c.v + head * cap * (D / 8));
+  uint32_t* s = (n < NG ? c.ks : c.vs) + (head * NG + n % NG) * cap;
+  auto half = [&](size_t slot, int f) { return (slot / 4 * 16 + n) * (D / 16) + 2 * ((D / 64) * ((slot & 3) >> 1) + f) + (slot & 1); };
+  const uint32_t kw = n < D / 8 ? k[of * (D / 8) + n] : 0, sw = n < 2 * NG ? s[of] : 0;
+  uint16_t vw[D / 64];
+#pragma unroll
+  for (int f = 0; f < D / 64; ++f) vw[f] = v[half(of, f)];
+  if (n < D / 8) k[to * (D / 8) + n] = kw;
+#pragma unroll
+  for (int f = 0; f < D / 64; ++f) v[half(to, f)] = vw[f];
+  if (n < 2 * NG) s[to] = sw;
 }
 
 // Which slots of a head stay, which move where.  Keys: the last `recent` positions first, then by weight, NaN last; equal keys by the
-// lower slot.  CACHED: the keys of a head are kept in the LDS.
-template <bool CACHED>
-__global__ __launch_bounds__(kPlanThreads) void kv4_plan_kernel(EvictArgs a) {
+// lower slot.  The budget-th key is found eleven bits at a time from histograms in the LDS; the recent ones, all alike, and zeros, of which
+// there may be many, are counted by wave, or every lane would wait for all others at one bin.  CACHED: the keys of a head are kept in
+// the LDS.  MOVE: the rows are moved here as well (few of them, and nobody reads a length that this launch writes).
+template <int THREADS, bool CACHED, int D, int GR, bool MOVE>
+__global__ __launch_bounds__(THREADS) void kv4_plan_kernel(EvictArgs a) {
   extern __shared__ uint32_t cache[];
-  __shared__ uint32_t hist[2048];
-  __shared__ uint64_t sums[kPlanThreads / 64];
-  __shared__ uint32_t chosen[2];
-  const int tid = threadIdx.x, b = blockIdx.x / a.c.H;
+  constexpr int kBins = 2048;
+  __shared__ __attribute__((aligned(16))) uint32_t hist[3][kBins];   // of the three passes; the last uses half of its
+  __shared__ uint32_t sums[6][THREADS / 64], chosen[3][2], recents;
+  constexpr uint32_t kRecent = 0xffffffffu, kZero = 0x80000000u;
+  const int tid = threadIdx.x, lane = tid & 63, h = blockIdx.x % a.c.H, b = blockIdx.x / a.c.H;
   const size_t head = blockIdx.x;
   const float* weight = a.c.weight + head * a.c.cap;
   const int32_t* pos = a.c.pos + head * a.c.cap;
@@ -218,124 +252,195 @@ __global__ __launch_bounds__(kPlanThreads) void kv4_plan_kernel(EvictArgs a) {
   int32_t* pos_out = a.pos_out + head * a.c.cap;
   const int len = min(max(a.lens[b], 0), a.max_len);
   const bool copy = weight_out != weight, copy_pos = pos_out != pos;
+  if (MOVE && h == 0 && tid == 0 && a.lens_out) a.lens_out[b] = min(len, a.budget);
   if (len <= a.budget) {
-    for (int t = tid; t < len; t += kPlanThreads) {
+    for (int t = tid; t < len; t += THREADS) {
       if (copy) weight_out[t] = weight[t];
       if (copy_pos) pos_out[t] = pos[t];
     }
-    if (tid == 0) a.count[head] = 0;
+    if (!MOVE && tid == 0) a.count[head] = 0;
     return;
   }
   const int64_t protect = (int64_t)a.next[b] - a.recent;
-  auto make_key = [&](int t) -> uint32_t {
-    if (pos[t] >= protect) return 0xffffffffu;
-    const float w = weight[t];
+  auto key_of = [&](float w, int p) -> uint32_t {
+    if (p >= protect) return kRecent;
     if (w != w) return 0u;
-    const uint32_t u = f2u(w + 0.0f);
+    const uint32_t u = f2u(w + 0.0f);   // one zero
     return u & 0x80000000u ? ~u : u | 0x80000000u;
   };
-  if (CACHED) {
-    for (int t = tid; t < len; t += kPlanThreads) cache[t] = make_key(t);
-    __syncthreads();
-  }
-  auto key_at = [&](int t) { return CACHED ? cache[t] : make_key(t); };
-
-  // the budget-th largest key, eleven bits at a time, and how many equal to it are kept
-  uint32_t prefix = 0, want = (uint32_t)a.budget;
+  auto key_at = [&](int t) { return CACHED ? cache[t] : key_of(weight[t], pos[t]); };
+  for (int i = tid; i < 3 * kBins / 4; i += THREADS) reinterpret_cast<uint4*>(hist)[i] = make_uint4(0, 0, 0, 0);
+  if (tid == 0) recents = 0;
+  __syncthreads();
+  // what does not depend on the choice goes out at once: slots that stay, and those cleared, unless their old values are yet to move
+  constexpr int AHEAD = 8;   // all loads of a round before its first store, which might be to the same place for all the compiler knows
+  for (int t0 = tid; t0 - tid < len; t0 += AHEAD * THREADS) {
+    float w[AHEAD];
+    int32_t p[AHEAD];
 #pragma unroll
-  for (int pass = 0; pass < 3; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : 2048;
-    for (int i = tid; i < bins; i += kPlanThreads) hist[i] = 0;
-    __syncthreads();
-    for (int t = tid; t < len; t += kPlanThreads) {
-      const uint32_t key = key_at(t);
-      if (pass == 0 || key >> (pass == 1 ? 21 : 10) == prefix) atomicAdd(&hist[key >> shift & (uint32_t)(bins - 1)], 1u);
+    for (int i = 0; i < AHEAD; ++i) {
+      const int t = min(t0 + i * THREADS, len - 1);
+      w[i] = weight[t];
+      p[i] = pos[t];
     }
-    __syncthreads();
-    // two bins a thread, from the largest down
-    const int i0 = bins - 1 - 2 * tid;
-    uint32_t c0 = 0, c1 = 0;
-    if (i0 > 0) c0 = hist[i0], c1 = hist[i0 - 1];
-    uint64_t total;
-    const uint64_t before = block_scan(c0 + c1, sums, &total);
-    if (before < want && before + c0 + c1 >= want) {
-      const bool second = before + c0 < want;
-      chosen[0] = (uint32_t)(second ? i0 - 1 : i0);
-      chosen[1] = want - (uint32_t)before - (second ? c0 : 0);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int t = t0 + i * THREADS;
+      const bool in = t < len;
+      const uint32_t key = key_of(w[i], p[i]);
+      if (CACHED && in) cache[t] = key;
+      const uint64_t all = __ballot(in && key == kRecent);
+      if (lane == 0 && all) atomicAdd(&recents, (uint32_t)__popcll(all));
+      if (in && copy) weight_out[t] = t < a.budget ? w[i] : 0.0f;
+      if (in && copy_pos) pos_out[t] = t < a.budget ? p[i] : -1;
     }
-    __syncthreads();
-    prefix = pass == 0 ? chosen[0] : prefix << (pass == 1 ? 11 : 10) | chosen[0];
-    want = chosen[1];
-    __syncthreads();
+  }
+  __syncthreads();
+
+  uint32_t prefix = 0, want = (uint32_t)a.budget;
+  if (recents >= want) {
+    prefix = kRecent;
+  } else {
+    want -= recents;
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+      const uint32_t mask = pass == 2 ? 1023u : 2047u;
+#pragma unroll 4
+      for (int t0 = 0; t0 < len; t0 += THREADS) {
+        const int t = t0 + tid;
+        const uint32_t key = t < len ? key_at(t) : kRecent;
+        const bool in = key != kRecent && (pass == 0 || key >> (pass == 1 ? 21 : 10) == prefix);
+        if (!__any(in)) continue;   // most rounds of the later passes
+        const uint64_t zeros = __ballot(in && key == kZero);
+        if (zeros && lane == 0) atomicAdd(&hist[pass][kZero >> shift & mask], (uint32_t)__popcll(zeros));
+        if (in && key != kZero) atomicAdd(&hist[pass][key >> shift & mask], 1u);
+      }
+      __syncthreads();
+      // a run of bins a thread, from the largest down
+      constexpr int RUN = kBins / THREADS;
+      const int i0 = kBins - RUN * (tid + 1);
+      uint32_t c[RUN], mine = 0, before;
+#pragma unroll
+      for (int i = 0; i < RUN; ++i) c[i] = hist[pass][i0 + RUN - 1 - i], mine += c[i];
+      block_scan<THREADS>(mine, sums[pass], &before);
+      if (before < want && before + mine >= want) {
+        int i = 0;
+#pragma unroll
+        for (int j = 0; j < RUN - 1; ++j)
+          if (i == j && before + c[j] < want) before += c[j], ++i;
+        chosen[pass][0] = (uint32_t)(i0 + RUN - 1 - i);
+        chosen[pass][1] = want - before;
+      }
+      __syncthreads();
+      prefix = pass == 0 ? chosen[pass][0] : prefix << (pass == 1 ? 11 : 10) | chosen[pass][0];
+      want = chosen[pass][1];
+    }
   }
 
-  // a run of slots a thread: the equal ones before it, then the holes and the slots that move
-  const int run = ((len + kPlanThreads - 1) / kPlanThreads) | 1;   // odd: the runs start in different banks
-  const int t0 = min(tid * run, len), t1 = min(t0 + run, len);
-  uint32_t equal = 0;
-  for (int t = t0; t < t1; ++t) equal += key_at(t) == prefix;
-  uint64_t total;
-  const uint32_t equal_before = (uint32_t)block_scan(equal, sums, &total);
-  auto walk = [&](auto&& hole, auto&& mover) {
+  // A stretch of slots a wave, 64 at a time in order: the equal ones before it, then the holes and the slots that move, counted by ballots.
+  constexpr int WAVES = THREADS / 64;
+  const int wave = tid >> 6, stretch = ((len + THREADS - 1) / THREADS) * 64;
+  const int t0 = wave * stretch, t1 = min(t0 + stretch, len);
+  const uint64_t lower = lanemask_lt();
+  auto over_waves = [&](uint32_t mine, uint32_t* of, uint32_t* all) {   // the sum over the waves before this one; a barrier
+    if (lane == 0) of[wave] = mine;
+    __syncthreads();
+    uint32_t sum = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      sum += w < wave ? of[w] : 0;
+      total += of[w];
+    }
+    *all = total;
+    return sum;
+  };
+  uint32_t equal = 0, total;
+#pragma unroll 4
+  for (int t = t0 + lane; t - lane < t1; t += 64) equal += (uint32_t)__popcll(__ballot(t < t1 && key_at(t) == prefix));
+  const uint32_t equal_before = over_waves(equal, sums[3], &total);
+  auto walk = [&](auto&& visit) {   // visit(slot, is a hole, moves)
     uint32_t e = equal_before;
-    for (int t = t0; t < t1; ++t) {
-      const uint32_t key = key_at(t);
-      const bool kept = key > prefix || (key == prefix && e < want);
-      e += key == prefix;
-      if (!kept && t < a.budget) hole(t);
-      if (kept && t >= a.budget) mover(t);
+#pragma unroll 4
+    for (int t = t0 + lane; t - lane < t1; t += 64) {
+      const uint32_t key = t < t1 ? key_at(t) : 0u;
+      const uint64_t same = __ballot(t < t1 && key == prefix);
+      const bool kept = key > prefix || (key == prefix && e + (uint32_t)__popcll(same & lower) < want);
+      e += (uint32_t)__popcll(same);
+      visit(t, t < t1 && !kept && t < a.budget, t < t1 && kept && t >= a.budget);
     }
   };
-  uint64_t mine = 0;
-  walk([&](int) { mine += 1; }, [&](int) { mine += 1ull << 32; });
-  const uint64_t at = block_scan(mine, sums, &total);
+  uint32_t n_holes = 0, n_movers = 0;
+  walk([&](int, bool hole, bool mover) {
+    n_holes += (uint32_t)__popcll(__ballot(hole));
+    n_movers += (uint32_t)__popcll(__ballot(mover));
+  });
+  uint32_t ih, im;
+  im = over_waves(n_movers, sums[4], &total);
+  ih = over_waves(n_holes, sums[5], &total);   // as many holes as slots that move
+  const int moves = (int)total;
+  // The lists, in the LDS where the histograms were if they fit there (16 bits a slot); rows that are not moved here need them in memory too.
+  constexpr int kListed = 3 * kBins * 4 / 4;   // moves whose lists of 16-bit slots fit
+  uint16_t* lists = reinterpret_cast<uint16_t*>(hist);
+  const bool small = CACHED && moves <= kListed;
   int32_t* holes = a.holes + head * a.max_moves;
   int32_t* movers = a.movers + head * a.max_moves;
-  uint32_t ih = (uint32_t)at, im = (uint32_t)(at >> 32);
-  walk([&](int t) { holes[ih++] = t; }, [&](int t) { movers[im++] = t; });
-  const int moves = (int)(uint32_t)total;   // as many holes as slots that move
-  if (tid == 0) a.count[head] = moves;
-  __syncthreads();   // the lists, and every read of a weight or position for a key
-  if (copy || copy_pos)
-    for (int t = tid; t < a.budget; t += kPlanThreads) {
-      if (copy) weight_out[t] = weight[t];
-      if (copy_pos) pos_out[t] = pos[t];
+  walk([&](int t, bool hole, bool mover) {
+    const uint64_t all_holes = __ballot(hole), all_movers = __ballot(mover);
+    const uint32_t to = ih + (uint32_t)__popcll(all_holes & lower), of = im + (uint32_t)__popcll(all_movers & lower);
+    if (hole) {
+      if (small) lists[to] = (uint16_t)t;
+      if (!MOVE) holes[to] = t;
     }
-  __syncthreads();
-  for (int i = tid; i < moves; i += kPlanThreads) {
-    const int to = holes[i], of = movers[i];
-    weight_out[to] = weight[of];
-    pos_out[to] = pos[of];
+    if (mover) {
+      if (small) lists[kListed + of] = (uint16_t)t;
+      if (!MOVE) movers[of] = t;
+    }
+    ih += (uint32_t)__popcll(all_holes);
+    im += (uint32_t)__popcll(all_movers);
+  });
+  if (!MOVE && tid == 0) a.count[head] = moves;
+  auto hole_at = [&](int i) { return small ? (int)lists[i] : holes[i]; };
+  auto mover_at = [&](int i) { return small ? (int)lists[kListed + i] : movers[i]; };
+  __syncthreads();   // the lists, every read of a weight or position for a key, and what the copies stored
+  if constexpr (MOVE)
+    for (int i = tid >> 4; i < moves; i += THREADS / 16) move_slot<D, GR>(a.c, head, hole_at(i), mover_at(i), tid & 15);
+  for (int i0 = tid; i0 < moves; i0 += 4 * THREADS) {
+    int to[4], p[4];
+    float w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int i = min(i0 + j * THREADS, moves - 1), of = mover_at(i);
+      to[j] = hole_at(i);
+      w[j] = weight[of];
+      p[j] = pos[of];
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (i0 + j * THREADS < moves) {
+        weight_out[to[j]] = w[j];
+        pos_out[to[j]] = p[j];
+      }
   }
+  if (copy && copy_pos) return;
   __syncthreads();
-  for (int t = a.budget + tid; t < len; t += kPlanThreads) {
-    weight_out[t] = 0.0f;
-    pos_out[t] = -1;
+  for (int t = a.budget + tid; t < len; t += THREADS) {
+    if (!copy) weight_out[t] = 0.0f;
+    if (!copy_pos) pos_out[t] = -1;
   }
 }
 
-// Sixteen lanes a move: a row of keys, the half-words of the values, the scales.  Sources lie from the budget on and places below it.
+// Sixteen lanes a move.  Sources lie from the budget on and places below it.
 template <int D, int GR>
 __global__ __launch_bounds__(256) void kv4_move_kernel(EvictArgs a) {
-  constexpr int NG = D / GR;
   const size_t head = blockIdx.y;
   if (blockIdx.x == 0 && head % a.c.H == 0 && threadIdx.x == 0 && a.lens_out) {
     const int b = (int)(head / a.c.H);
     a.lens_out[b] = min(min(max(a.lens[b], 0), a.max_len), a.budget);
   }
-  const int i = blockIdx.x * 16 + (threadIdx.x >> 4), n = threadIdx.x & 15;
+  const int i = blockIdx.x * 16 + (threadIdx.x >> 4);
   if (i >= a.count[head]) return;
-  const size_t to = a.holes[head * a.max_moves + i], of = a.movers[head * a.max_moves + i], cap = a.c.cap;
-  uint32_t* k = a.c.k + head * cap * (D / 8);
-  if (n < D / 8) k[to * (D / 8) + n] = k[of * (D / 8) + n];
-  uint16_t* v = reinterpret_cast<uint16_t*>(a.c.v + head * cap * (D / 8));
-  auto half = [&](size_t slot, int f) { return (slot / 4 * 16 + n) * (D / 16) + 2 * ((D / 64) * ((slot & 3) >> 1) + f) + (slot & 1); };
-#pragma unroll
-  for (int f = 0; f < D / 64; ++f) v[half(to, f)] = v[half(of, f)];
-  if (n < 2 * NG) {
-    uint32_t* s = (n < NG ? a.c.ks : a.c.vs) + (head * NG + n % NG) * cap;
-    s[to] = s[of];
-  }
+  move_slot<D, GR>(a.c, head, a.holes[head * a.max_moves + i], a.movers[head * a.max_moves + i], threadIdx.x & 15);
 }
 
 constexpr int kCachedKeys = 32768;
@@ -382,11 +487,34 @@ struct ReadLaunch {
   }
 };
 
-struct MoveLaunch {
+struct EvictLaunch {
   EvictArgs a;
   hipStream_t s;
+  bool here;
+  template <int THREADS, bool CACHED, int D, int GR, bool MOVE>
+  int plan() const {
+    auto* kernel = kv4_plan_kernel<THREADS, CACHED, D, GR, MOVE>;
+    const size_t lds = CACHED ? (size_t)a.max_len * sizeof(uint32_t) : 0;
+    static std::atomic<uint64_t> seen{0};
+    if (lds > 32768) {   // with the kernel's own, more than a launch may have unasked
+      const int rc = allow_dynamic_lds(seen, reinterpret_cast<const void*>(kernel), kCachedKeys * sizeof(uint32_t));
+      if (rc != CI_OK) return rc;
+    }
+    hipLaunchKernelGGL(kernel, dim3(a.c.B * a.c.H), dim3(THREADS), lds, s, a);
+    CI_HIP_CHECK_LAUNCH();
+    return CI_OK;
+  }
+  template <int D, int GR, bool MOVE>
+  int plan_any() const {
+    // a wave's share of the steps against the barriers' cost
+    if (a.max_len <= 2048) return plan<256, true, D, GR, MOVE>();
+    return a.max_len <= kCachedKeys ? plan<1024, true, D, GR, MOVE>() : plan<1024, false, D, GR, MOVE>();
+  }
   template <class T, int D, int GR>
   int operator()() const {
+    if (here) return plan_any<D, GR, true>();
+    const int rc = plan_any<D, GR, false>();
+    if (rc != CI_OK) return rc;
     hipLaunchKernelGGL((kv4_move_kernel<D, GR>), dim3((std::max(a.max_moves, 1) + 15) / 16, a.c.B * a.c.H), dim3(256), 0, s, a);
     CI_HIP_CHECK_LAUNCH();
     return CI_OK;
@@ -437,19 +565,10 @@ int launch_kv4_evict(const ci_kv4& c, const int32_t* lens, const int32_t* next, 
   a.count = reinterpret_cast<int32_t*>(ws);
   a.holes = a.count + words256(heads);
   a.movers = a.holes + words256(heads * a.max_moves);
-  if (max_len <= kCachedKeys) {
-    static std::atomic<uint64_t> seen{0};
-    const size_t lds = (size_t)max_len * sizeof(uint32_t);
-    if (lds > 40960) {   // with the kernel's own, more than a launch may have unasked
-      const int rc = allow_dynamic_lds(seen, reinterpret_cast<const void*>(kv4_plan_kernel<true>), kCachedKeys * sizeof(uint32_t));
-      if (rc != CI_OK) return rc;
-    }
-    hipLaunchKernelGGL(kv4_plan_kernel<true>, dim3((uint32_t)heads), dim3(kPlanThreads), lds, s, a);
-  } else {
-    hipLaunchKernelGGL(kv4_plan_kernel<false>, dim3((uint32_t)heads), dim3(kPlanThreads), 0, s, a);
-  }
-  CI_HIP_CHECK_LAUNCH();
-  return by_shape<F32>(c.D, c.group, MoveLaunch{a, s});
+  // In one launch where a workgroup's own moves are few, unless it would write lengths that others have yet to read.
+  const uintptr_t in = reinterpret_cast<uintptr_t>(lens), out = reinterpret_cast<uintptr_t>(lens_out);
+  const bool apart = !lens_out || out + c.B * sizeof(int32_t) <= in || in + c.B * sizeof(int32_t) <= out;
+  return by_shape<F32>(c.D, c.group, EvictLaunch{a, s, apart && a.max_moves <= kMovedHere});
 }
 
 }  // namespace ci
