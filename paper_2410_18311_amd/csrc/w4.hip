@@ -4,7 +4,7 @@
 // Layout.  Rows by 16 and columns by 128 make a block of 1 KB, which a wave loads with one instruction: lane 16 g + n holds row n, word j
 // the columns 32 j + 8 g .. + 7, so that the word is the matrix cores' operand (16 rows, 32 columns) once its codes are unpacked and
 // a group is a whole number of words.  Blocks lie along the columns; behind all of them, in the same order, the steps and lowest values of
-// the 16 rows, group by group.  Rows and columns that fill up the last blocks hold code, step and lowest value 0.
+// the 16 rows, row by row: a row's groups of a block are neighbours.  Rows and columns that fill up the last blocks hold code, step and lowest value 0.
 #include <algorithm>
 
 #include "q4.hpp"
@@ -76,7 +76,7 @@ __global__ __launch_bounds__(256) void w4_quantize_kernel(const typename D::T* w
       for (int e = 0; e < 8; ++e)
         if (row < R && c + e < C) word[j] |= q4_code(x[j][e], scale) << (4 * q4_nibble(e));
     }
-    if (g == s % 4) scales[(block * (4 / J) + s) * 16 + n] = scale;
+    if (g == s % 4) scales[(block * 16 + n) * (4 / J) + s] = scale;
   }
   *reinterpret_cast<uint4*>(codes + block * (kBlockBytes / 4) + lane * 4) = make_uint4(word[0], word[1], word[2], word[3]);
 }
@@ -92,7 +92,7 @@ __global__ __launch_bounds__(256) void w4_read_kernel(const uint32_t* codes, con
   const int col0 = (int)(block % nb) * kBlockCols;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const uint32_t word = codes[block * (kBlockBytes / 4) + lane * 4 + j], scale = scales[(block * (4 / J) + j / J) * 16 + n];
+    const uint32_t word = codes[block * (kBlockBytes / 4) + lane * 4 + j], scale = scales[(block * 16 + n) * (4 / J) + j / J];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const int c = col0 + 32 * j + 8 * g + e;
@@ -112,7 +112,7 @@ struct RowsArgs {
   void* y;
   int64_t ldy;
   int M, R, C, nb, tiles; // nb blocks of columns, tiles of 16 rows
-  int x_vectors, y_vectors, bias_dtype, y_dtype, act;
+  int x_vectors, x_bytes, bias_dtype, y_dtype, act;
 };
 
 // Eight elements of x from column c on as the pieces of an operand; zeros past the end.
@@ -166,74 +166,100 @@ __device__ __forceinline__ void store_as(void* p, int64_t i, float v, int dtype)
   else if (dtype == CI_F16) reinterpret_cast<_Float16*>(p)[i] = (_Float16)v;
   else reinterpret_cast<uint16_t*>(p)[i] = from_float<BF16>(v);
 }
-__device__ __forceinline__ void store4_as(void* p, int64_t i, const float (&v)[4], int dtype) {
-  if (dtype == CI_F32) {
-    *reinterpret_cast<float4*>(reinterpret_cast<float*>(p) + i) = make_float4(v[0], v[1], v[2], v[3]);
-    return;
-  }
-  uint2 u;
-  if (dtype == CI_F16) {
-    half2_t a, b;
-    a[0] = (_Float16)v[0]; a[1] = (_Float16)v[1]; b[0] = (_Float16)v[2]; b[1] = (_Float16)v[3];
-    u = make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b));
-  } else {
-    u = make_uint2(pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3]));
-  }
-  *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(p) + i) = u;
-}
+// Where the kernel has x from: rows in memory as they are (up to 16, 16-bit, read with the weights), the LDS as operands of the M rows that there
+// are ([word][piece][column octet g][row]), or operands that w4_x_kernel has laid out.
+enum { kXRows, kXLds, kXOperands };
 
 // A workgroup multiplies RT tiles of 16 weight rows (pairs of up and gate tiles where DUAL) with NT tiles of 16 rows of x; its waves take
-// the blocks of columns by turns and their sums are added at the end in the order of the waves.  XLDS: x is in the LDS, as operands of
-// the M rows that there are ([word][piece][column octet g][row]).
-template <class D, int G, int RT, int NT, bool DUAL, bool XLDS>
-__global__ __launch_bounds__(XLDS ? (D::VEC == 8 ? 1024 : 512) : 256) void gemm_q4_rows_kernel(RowsArgs a) {
+// the blocks of columns by turns and their sums are added at the end in the order of the waves.  A block is requested two turns ahead;
+// what would lie behind the last one is out of the descriptors' range, which costs no traffic and keeps the number of loads on their way
+// the same on every path.  Results come with a lane's four rows of x and one row of weights, so a group's two numbers are one load for
+// that row; ROWS: how many of the four are of rows that there are (one row of x stands in all sixteen places, so one is enough).
+template <class D, int G, int RT, int NT, bool DUAL, int X, int THREADS, int ROWS>
+__global__ __launch_bounds__(THREADS) void gemm_q4_rows_kernel(RowsArgs a) {
   constexpr int OP = Q4Type<D>::OP, PIECES = Q4Type<D>::PIECES;
   constexpr int J = G / 32, NG = 4 / J;   // words of a group, groups of a block
   constexpr int PF = 2;
+  static_assert(X != kXRows || (NT == 1 && PIECES == 1), "rows are read for one tile of 16-bit ones");
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
 
-  const uint32_t* code[RT];
-  const uint32_t* scale[RT];
+  __amdgpu_buffer_rsrc_t code[RT], scale[RT];
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     const int tile = min(DUAL ? (int)blockIdx.x * (RT / 2) + t / 2 : (int)blockIdx.x * RT + t, a.tiles - 1);
     const uint32_t* w = a.w[DUAL ? t & 1 : 0];
-    code[t] = w + (size_t)tile * a.nb * (kBlockBytes / 4) + lane * 4;
-    scale[t] = w + a.scales + (size_t)tile * a.nb * (NG * 16) + g * 4;
+    code[t] = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint32_t*>(w + (size_t)tile * a.nb * (kBlockBytes / 4)), 0, a.nb * kBlockBytes, 0x00020000);
+    scale[t] = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint32_t*>(w + a.scales + (size_t)tile * a.nb * (NG * 16)), 0, a.nb * NG * 64, 0x00020000);
   }
+  const auto xs = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(a.x), 0, a.x_bytes, 0x00020000);
+  const int xrow = min(n, a.M - 1);   // columns of the product past the last row of x repeat it
+  const int x_off = X == kXRows ? (int)(xrow * a.ldx * 2) + g * 16 : 0;
   struct Stage {
-    uint4 code[RT], scale[RT][NG];
+    uint4 code[RT], x[X == kXRows ? 4 : 1];
+    uint32_t scale[RT][NG];   // of the lane's row
   } st[PF];
   auto load = [&](Stage& s, int b) {
-    b = min(b, a.nb - 1);
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-      s.code[t] = ld16(code[t] + (size_t)b * (kBlockBytes / 4));
+      s.code[t] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(code[t], b * kBlockBytes + lane * 16, 0, 0));
+      const int at = b * (NG * 64) + n * (NG * 4);
+      if constexpr (NG == 1) {
+        s.scale[t][0] = __builtin_amdgcn_raw_buffer_load_b32(scale[t], at, 0, 0);
+      } else if constexpr (NG == 2) {
+        const auto two = __builtin_amdgcn_raw_buffer_load_b64(scale[t], at, 0, 0);
+        s.scale[t][0] = two[0], s.scale[t][1] = two[1];
+      } else {
+        const auto four = __builtin_amdgcn_raw_buffer_load_b128(scale[t], at, 0, 0);
 #pragma unroll
-      for (int i = 0; i < NG; ++i) s.scale[t][i] = ld16(scale[t] + (size_t)b * (NG * 16) + i * 16);
+        for (int i = 0; i < 4; ++i) s.scale[t][i] = four[i];
+      }
     }
+    if constexpr (X == kXRows)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s.x[j] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(xs, x_off + b * (kBlockCols * 2) + j * 64, 0, 0));
   };
 #pragma unroll
   for (int i = 0; i < PF; ++i) load(st[i], wave + i * waves);
 
-  if constexpr (XLDS) {
-    const int chunks = a.nb * 16;   // of eight columns
-    for (int i = threadIdx.x; i < chunks * a.M; i += blockDim.x) {
-      const int m = i / chunks, c = i % chunks;
-      uint4 p[PIECES];
-      x_pieces<D>(reinterpret_cast<const typename D::T*>(a.x) + m * a.ldx, c * 8, a.C, a.x_vectors, p);
+  if constexpr (X == kXLds) {
+    constexpr int AHEAD = 4;   // pieces on their way at a time
+    const int chunks = a.nb * 16, all = chunks * a.M;   // of eight columns
+    for (int i0 = threadIdx.x; i0 < all; i0 += AHEAD * blockDim.x) {
+      uint4 p[AHEAD][PIECES];
 #pragma unroll
-      for (int q = 0; q < PIECES; ++q)
-        reinterpret_cast<uint4*>(smem)[((c / 4 * PIECES + q) * 4 + c % 4) * a.M + m] = p[q];
+      for (int u = 0; u < AHEAD; ++u) {
+        const int i = min(i0 + u * (int)blockDim.x, all - 1);
+        x_pieces<D>(reinterpret_cast<const typename D::T*>(a.x) + i / chunks * a.ldx, i % chunks * 8, a.C, a.x_vectors, p[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const int i = i0 + u * (int)blockDim.x, m = i / chunks, c = i % chunks;
+        if (i < all)
+#pragma unroll
+          for (int q = 0; q < PIECES; ++q) reinterpret_cast<uint4*>(smem)[((c / 4 * PIECES + q) * 4 + c % 4) * a.M + m] = p[u][q];
+      }
     }
     __syncthreads();
   }
-  const int xrow = min(n, a.M - 1);   // XLDS: columns of the product past the last row of x repeat it
-  auto x_at = [&](int word, int q, int nt) {
-    if constexpr (XLDS) return reinterpret_cast<const uint4*>(smem)[((word * PIECES + q) * 4 + g) * a.M + xrow];
-    else return ld16(reinterpret_cast<const uint4*>(a.x) + ((size_t)(word * PIECES + q) * NT + nt) * 64 + lane);
+  auto x_at = [&](const Stage& s, int b, int j, int q, int nt) {
+    if constexpr (X == kXRows) {
+      (void)s;
+      uint4 x = s.x[j];
+      const int have = a.C - (b * kBlockCols + 32 * j + 8 * g);
+      if (b == a.nb - 1 && have < 8) {   // what follows the row is something else
+        uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = 2 * e < have ? w[e] : 0u;
+        x = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+      return x;
+    } else if constexpr (X == kXLds) {
+      return reinterpret_cast<const uint4*>(smem)[(((b * 4 + j) * PIECES + q) * 4 + g) * a.M + xrow];
+    } else {
+      return ld16(reinterpret_cast<const uint4*>(a.x) + ((size_t)((b * 4 + j) * PIECES + q) * NT + nt) * 64 + lane);
+    }
   };
 
   const Q4Magic magic = q4_magic<OP>();
@@ -270,22 +296,21 @@ __global__ __launch_bounds__(XLDS ? (D::VEC == 8 ? 1024 : 512) : 256) void gemm_
             for (int u = 0; u < NT; ++u)
 #pragma unroll
               for (int q = 0; q < PIECES; ++q) {
-                const uint4 x = x_at(b * 4 + j, q, u);
-                sx[u] = mfma_q4<OP>(ones, x, sx[u]);
+                const uint4 x = x_at(st[i], b, j, q, u);
+                sx[u] = mfma_q4<OP>(x, ones, sx[u]);
 #pragma unroll
-                for (int t = 0; t < RT; ++t) acc[t][u] = mfma_q4<OP>(w[t], x, acc[t][u]);
+                for (int t = 0; t < RT; ++t) acc[t][u] = mfma_q4<OP>(x, w[t], acc[t][u]);
               }
           }
 #pragma unroll
           for (int t = 0; t < RT; ++t) {
-            const uint32_t sc[4] = {st[i].scale[t][s].x, st[i].scale[t][s].y, st[i].scale[t][s].z, st[i].scale[t][s].w};
+            const uint32_t sc = st[i].scale[t][s];
+            const float rest = __builtin_fmaf(half_lo(sc), -kOffset<OP>, half_hi(sc));
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const float rest = __builtin_fmaf(half_lo(sc[r]), -kOffset<OP>, half_hi(sc[r]));
+            for (int u = 0; u < NT; ++u)
 #pragma unroll
-              for (int u = 0; u < NT; ++u)
-                sum[t][u][r] = __builtin_fmaf(half_lo(sc[r]), acc[t][u][r], __builtin_fmaf(rest, sx[u][r], sum[t][u][r]));
-            }
+              for (int r = 0; r < ROWS; ++r)
+                sum[t][u][r] = __builtin_fmaf(half_lo(sc), acc[t][u][r], __builtin_fmaf(rest, sx[u][r], sum[t][u][r]));
           }
         }
       }
@@ -295,86 +320,88 @@ __global__ __launch_bounds__(XLDS ? (D::VEC == 8 ? 1024 : 512) : 256) void gemm_
 
   // the waves' sums, lane by lane
   __syncthreads();
-  float4* part = reinterpret_cast<float4*>(smem);
+  float* part = reinterpret_cast<float*>(smem);   // [tile][tile of x][wave][row of x of the four][lane]
 #pragma unroll
   for (int t = 0; t < RT; ++t)
 #pragma unroll
     for (int u = 0; u < NT; ++u)
-      part[((t * NT + u) * waves + wave) * 64 + lane] = make_float4(sum[t][u][0], sum[t][u][1], sum[t][u][2], sum[t][u][3]);
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) part[(((t * NT + u) * waves + wave) * ROWS + r) * 64 + lane] = sum[t][u][r];
   __syncthreads();
-  constexpr int OUT = (DUAL ? RT / 2 : RT) * NT;
-  for (int i = threadIdx.x; i < OUT * 64; i += blockDim.x) {
-    const int l = i & 63, u = (i >> 6) % NT, t = (i >> 6) / NT;
-    auto total = [&](int tile, float (&v)[4]) {
-      float4 f = part[(tile * NT + u) * waves * 64 + l];
-      for (int w = 1; w < waves; ++w) {
-        const float4 h = part[((tile * NT + u) * waves + w) * 64 + l];
-        f.x += h.x; f.y += h.y; f.z += h.z; f.w += h.w;
-      }
-      v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
-    };
-    const int m = u * 16 + (l & 15), row = ((int)blockIdx.x * (DUAL ? RT / 2 : RT) + t) * 16 + (l >> 4) * 4;
+  constexpr int TILES = DUAL ? RT / 2 : RT;   // of results
+  // neighbouring threads have neighbouring rows of weights, and so neighbouring results
+  for (int i = threadIdx.x; i < TILES * NT * ROWS * 64; i += blockDim.x) {
+    const int col = i & 15, t = (i >> 4) % TILES, rest = (i >> 4) / TILES, gr = rest % 4, r = rest / 4 % ROWS, u = rest / 4 / ROWS;
+    const int m = u * 16 + 4 * gr + r, row = ((int)blockIdx.x * TILES + t) * 16 + col;
     if (m >= a.M || row >= a.R) continue;
-    float v[4];
-    total(DUAL ? 2 * t : t, v);
+    auto total = [&](int tile) {
+      float v = 0.0f;
+      for (int w = 0; w < waves; ++w) v += part[(((tile * NT + u) * waves + w) * ROWS + r) * 64 + 16 * gr + col];
+      return v;
+    };
+    float v = total(DUAL ? 2 * t : t);
     if constexpr (DUAL) {
-      float z[4];
-      total(2 * t + 1, z);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) v[r] *= silu(z[r]);
+      v *= silu(total(2 * t + 1));
     } else {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        if (a.bias && row + r < a.R) v[r] += load_as(a.bias, row + r, a.bias_dtype);
-        if (a.act == CI_ACT_RELU) v[r] = v[r] < 0.0f ? 0.0f : v[r];   // keeps a NaN
-      }
+      if (a.bias) v += load_as(a.bias, row, a.bias_dtype);
+      if (a.act == CI_ACT_RELU) v = v < 0.0f ? 0.0f : v;   // keeps a NaN
     }
-    const int64_t at = (int64_t)m * a.ldy + row;
-    if (a.y_vectors && row + 4 <= a.R) store4_as(a.y, at, v, a.y_dtype);
-    else
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (row + r < a.R) store_as(a.y, at + r, v[r], a.y_dtype);
+    store_as(a.y, (int64_t)m * a.ldy + row, v, a.y_dtype);
   }
 }
 
-constexpr size_t kXLds = 65536;   // x beside it leaves room for a second workgroup
+constexpr size_t kXInLds = 65536;   // what a launch may have unasked, and room for a second workgroup
 
 size_t x_bytes(int64_t rows, int64_t C, int dtype) { return (size_t)rows * col_blocks(C) * kBlockCols * 2 * (dtype == CI_F32 ? 3 : 1); }
-bool x_in_lds(int64_t M, int64_t C, int dtype) { return M <= 16 && x_bytes(M, C, dtype) <= kXLds; }
+int64_t x_span(int64_t M, int64_t C, int64_t ldx) { return ((M - 1) * ldx + C) * 2; }
+// Rows as they are: 16-bit, whole words at whole words, within a descriptor's reach.
+bool x_rows(const void* x, int64_t M, int64_t C, int64_t ldx, int dtype) {
+  return dtype != CI_F32 && M <= 16 && (reinterpret_cast<uintptr_t>(x) & 3u) == 0 && C % 2 == 0 && (M == 1 || ldx % 2 == 0) &&
+         ldx <= ((int64_t)1 << 26) &&
+         x_span(M, C, ldx) < ((int64_t)1 << 30);
+}
+bool x_in_lds(int64_t M, int64_t C, int dtype) { return M <= 16 && x_bytes(M, C, dtype) <= kXInLds; }
 
-template <class D, int G, int RT, int NT, bool DUAL, bool XLDS>
+template <class D, int G, int RT, int NT, bool DUAL, int X, int THREADS, int ROWS = 4>
 int launch_rows(const RowsArgs& a, int waves, hipStream_t s) {
   const int per = DUAL ? RT / 2 : RT;
   size_t lds = (size_t)waves * RT * NT * 1024;
-  if (XLDS) lds = std::max(lds, x_bytes(a.M, a.C, D::VEC == 8 ? CI_F16 : CI_F32));
-  hipLaunchKernelGGL((gemm_q4_rows_kernel<D, G, RT, NT, DUAL, XLDS>), dim3((a.tiles + per - 1) / per), dim3(waves * 64), lds, s, a);
+  if (X == kXLds) lds = std::max(lds, x_bytes(a.M, a.C, D::VEC == 8 ? CI_F16 : CI_F32));
+  hipLaunchKernelGGL((gemm_q4_rows_kernel<D, G, RT, NT, DUAL, X, THREADS, ROWS>), dim3((a.tiles + per - 1) / per), dim3(waves * 64), lds, s, a);
   CI_HIP_CHECK_LAUNCH();
   return CI_OK;
 }
 
+template <class D, int G, bool DUAL, int X, int THREADS, int ROWS>
+int launch_few(const RowsArgs& a, int waves, hipStream_t s) {
+  if constexpr (DUAL) return launch_rows<D, G, 2, 1, true, X, THREADS, ROWS>(a, waves, s);
+  else if (a.tiles >= 1024) return launch_rows<D, G, 2, 1, false, X, THREADS, ROWS>(a, waves, s);
+  else return launch_rows<D, G, 1, 1, false, X, THREADS, ROWS>(a, waves, s);
+}
+
 template <class D, int G, bool DUAL>
-int launch_shape(const RowsArgs& a, bool x_lds, hipStream_t s) {
-  if (x_lds) {
-    // waves for two a SIMD on the whole chip, and no more than there are blocks
+int launch_shape(const RowsArgs& a, int x, hipStream_t s) {
+  if (x != kXOperands) {
+    // waves for two a SIMD on the whole chip, and no more than there are blocks or, of groups of 32 and fp32 rows, registers
+    constexpr int MOST = D::VEC == 8 && G > 32 ? 16 : 8;
     int waves = 4;
-    while (waves < (D::VEC == 8 ? 16 : 8) && (int64_t)a.tiles * waves < 4096 && waves * 2 <= a.nb) waves *= 2;
-    if constexpr (DUAL) return launch_rows<D, G, 2, 1, true, true>(a, waves, s);
-    else if (a.tiles >= 1024) return launch_rows<D, G, 2, 1, false, true>(a, waves, s);
-    else return launch_rows<D, G, 1, 1, false, true>(a, waves, s);
+    while (waves < MOST && (int64_t)a.tiles * waves < 2048 && waves * 2 <= a.nb) waves *= 2;
+    if (a.M == 1)
+      return waves == 4 ? launch_few<D, G, DUAL, kXLds, 256, 1>(a, waves, s) : launch_few<D, G, DUAL, kXLds, MOST * 64, 1>(a, waves, s);
+    return launch_few<D, G, DUAL, kXLds, MOST * 64, 4>(a, waves, s);
   }
-  if (a.M <= 16) return launch_rows<D, G, 2, 1, DUAL, false>(a, 4, s);
-  if (a.M <= 32) return launch_rows<D, G, 2, 2, DUAL, false>(a, 4, s);
-  return launch_rows<D, G, 2, 4, DUAL, false>(a, 4, s);
+  if (a.M <= 16) return launch_rows<D, G, 2, 1, DUAL, kXOperands, 256>(a, 4, s);
+  if (a.M <= 32) return launch_rows<D, G, 2, 2, DUAL, kXOperands, 256>(a, 4, s);
+  return launch_rows<D, G, 2, 4, DUAL, kXOperands, 256>(a, 4, s);
 }
 
 template <class D>
-int launch_type(const RowsArgs& a, int group, bool x_lds, hipStream_t s) {
+int launch_type(const RowsArgs& a, int group, int x, hipStream_t s) {
   const bool dual = a.act == CI_ACT_SWIGLU;
   switch (group) {
-    case 32: return dual ? launch_shape<D, 32, true>(a, x_lds, s) : launch_shape<D, 32, false>(a, x_lds, s);
-    case 64: return dual ? launch_shape<D, 64, true>(a, x_lds, s) : launch_shape<D, 64, false>(a, x_lds, s);
-    default: return dual ? launch_shape<D, 128, true>(a, x_lds, s) : launch_shape<D, 128, false>(a, x_lds, s);
+    case 32: return dual ? launch_shape<D, 32, true>(a, x, s) : launch_shape<D, 32, false>(a, x, s);
+    case 64: return dual ? launch_shape<D, 64, true>(a, x, s) : launch_shape<D, 64, false>(a, x, s);
+    default: return dual ? launch_shape<D, 128, true>(a, x, s) : launch_shape<D, 128, false>(a, x, s);
   }
 }
 
@@ -450,9 +477,9 @@ int launch_w4_matvec(const void* x, int64_t M, int64_t ldx, int x_dtype, const v
   a.nb = (int)col_blocks(C);
   a.tiles = (int)row_tiles(R);
   a.x_vectors = aligned16(x) && ldx * elem_bytes(x_dtype) % 16 == 0;
-  a.y_vectors = reinterpret_cast<uintptr_t>(y) % (4 * elem_bytes(y_dtype)) == 0 && ldy % 4 == 0;
-  const bool x_lds = x_in_lds(M, C, x_dtype);
-  if (!x_lds) {
+  const int where = x_in_lds(M, C, x_dtype) ? kXLds : kXOperands;
+  a.x_bytes = where == kXRows ? (int)x_span(M, C, ldx) : 0;
+  if (where == kXOperands) {
     const int NT = M <= 16 ? 1 : M <= 32 ? 2 : 4, words = a.nb * 4;
     const dim3 grid((words * NT + 3) / 4);
     uint4* out = reinterpret_cast<uint4*>(ws);
@@ -466,9 +493,9 @@ int launch_w4_matvec(const void* x, int64_t M, int64_t ldx, int x_dtype, const v
     a.x = ws;
   }
   switch (x_dtype) {
-    case CI_F32: return launch_type<F32>(a, group, x_lds, s);
-    case CI_F16: return launch_type<F16>(a, group, x_lds, s);
-    default: return launch_type<BF16>(a, group, x_lds, s);
+    case CI_F32: return launch_type<F32>(a, group, where, s);
+    case CI_F16: return launch_type<F16>(a, group, where, s);
+    default: return launch_type<BF16>(a, group, where, s);
   }
 }
 
