@@ -166,7 +166,7 @@ __device__ __forceinline__ void store_as(void* p, int64_t i, float v, int dtype)
   else if (dtype == CI_F16) reinterpret_cast<_Float16*>(p)[i] = (_Float16)v;
   else reinterpret_cast<uint16_t*>(p)[i] = from_float<BF16>(v);
 }
-// Where the kernel has x from: rows in memory as they are (up to 16, 16-bit, read with the weights), the LDS as operands of the M rows that there
+// Where the kernel has x from: rows in memory as they are (16-bit, requested with the weights), the LDS as operands of the M rows that there
 // are ([word][piece][column octet g][row]), or operands that w4_x_kernel has laid out.
 enum { kXRows, kXLds, kXOperands };
 
@@ -174,12 +174,13 @@ enum { kXRows, kXLds, kXOperands };
 // the blocks of columns by turns and their sums are added at the end in the order of the waves.  A block is requested two turns ahead;
 // what would lie behind the last one is out of the descriptors' range, which costs no traffic and keeps the number of loads on their way
 // the same on every path.  Results come with a lane's four rows of x and one row of weights, so a group's two numbers are one load for
-// that row; ROWS: how many of the four are of rows that there are (one row of x stands in all sixteen places, so one is enough).
+// that row; ROWS: how many of the four are of rows that there are: up to 4 ROWS rows of x stand ROWS to a lane, and the other places repeat them.
 template <class D, int G, int RT, int NT, bool DUAL, int X, int THREADS, int ROWS>
 __global__ __launch_bounds__(THREADS) void gemm_q4_rows_kernel(RowsArgs a) {
   constexpr int OP = Q4Type<D>::OP, PIECES = Q4Type<D>::PIECES;
   constexpr int J = G / 32, NG = 4 / J;   // words of a group, groups of a block
   constexpr int PF = 2;
+  constexpr bool kStaged = X == kXRows || (X == kXOperands && NT * PIECES * RT <= 8);   // x is requested with the weights, registers permitting
   static_assert(X != kXRows || (NT == 1 && PIECES == 1), "rows are read for one tile of 16-bit ones");
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
@@ -194,10 +195,13 @@ __global__ __launch_bounds__(THREADS) void gemm_q4_rows_kernel(RowsArgs a) {
     scale[t] = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint32_t*>(w + a.scales + (size_t)tile * a.nb * (NG * 16)), 0, a.nb * NG * 64, 0x00020000);
   }
   const auto xs = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(a.x), 0, a.x_bytes, 0x00020000);
-  const int xrow = min(n, a.M - 1);   // columns of the product past the last row of x repeat it
-  const int x_off = X == kXRows ? (int)(xrow * a.ldx * 2) + g * 16 : 0;
+  static_assert(NT == 1 || ROWS == 4, "tiles of x but a single one are full");
+  const int xrow = min(ROWS * (n >> 2) + min(n & 3, ROWS - 1), a.M - 1);   // the row of x in place n of a single tile
+  int x_off[NT];
+#pragma unroll
+  for (int u = 0; u < NT; ++u) x_off[u] = (int)(xrow * a.ldx * 2) + g * 16;
   struct Stage {
-    uint4 code[RT], x[X == kXRows ? 4 : 1];
+    uint4 code[RT], x[kStaged ? NT * 4 * PIECES : 1];
     uint32_t scale[RT][NG];   // of the lane's row
   } st[PF];
   auto load = [&](Stage& s, int b) {
@@ -216,9 +220,16 @@ __global__ __launch_bounds__(THREADS) void gemm_q4_rows_kernel(RowsArgs a) {
         for (int i = 0; i < 4; ++i) s.scale[t][i] = four[i];
       }
     }
-    if constexpr (X == kXRows)
+    if constexpr (kStaged)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) s.x[j] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(xs, x_off + b * (kBlockCols * 2) + j * 64, 0, 0));
+      for (int u = 0; u < NT; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int q = 0; q < PIECES; ++q) {
+            const int at = X == kXRows ? x_off[u] + b * (kBlockCols * 2) + j * 64 : (((b * 4 + j) * PIECES + q) * NT + u) * 1024 + lane * 16;
+            s.x[(u * 4 + j) * PIECES + q] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(xs, at, 0, 0));
+          }
   };
 #pragma unroll
   for (int i = 0; i < PF; ++i) load(st[i], wave + i * waves);
@@ -245,8 +256,7 @@ __global__ __launch_bounds__(THREADS) void gemm_q4_rows_kernel(RowsArgs a) {
   }
   auto x_at = [&](const Stage& s, int b, int j, int q, int nt) {
     if constexpr (X == kXRows) {
-      (void)s;
-      uint4 x = s.x[j];
+      uint4 x = s.x[nt * 4 + j];
       const int have = a.C - (b * kBlockCols + 32 * j + 8 * g);
       if (b == a.nb - 1 && have < 8) {   // what follows the row is something else
         uint32_t w[4] = {x.x, x.y, x.z, x.w};
@@ -257,6 +267,8 @@ __global__ __launch_bounds__(THREADS) void gemm_q4_rows_kernel(RowsArgs a) {
       return x;
     } else if constexpr (X == kXLds) {
       return reinterpret_cast<const uint4*>(smem)[(((b * 4 + j) * PIECES + q) * 4 + g) * a.M + xrow];
+    } else if constexpr (kStaged) {
+      return s.x[(nt * 4 + j) * PIECES + q];
     } else {
       return ld16(reinterpret_cast<const uint4*>(a.x) + ((size_t)((b * 4 + j) * PIECES + q) * NT + nt) * 64 + lane);
     }
@@ -332,7 +344,7 @@ __global__ __launch_bounds__(THREADS) void gemm_q4_rows_kernel(RowsArgs a) {
   // neighbouring threads have neighbouring rows of weights, and so neighbouring results
   for (int i = threadIdx.x; i < TILES * NT * ROWS * 64; i += blockDim.x) {
     const int col = i & 15, t = (i >> 4) % TILES, rest = (i >> 4) / TILES, gr = rest % 4, r = rest / 4 % ROWS, u = rest / 4 / ROWS;
-    const int m = u * 16 + 4 * gr + r, row = ((int)blockIdx.x * TILES + t) * 16 + col;
+    const int m = u * 16 + ROWS * gr + r, row = ((int)blockIdx.x * TILES + t) * 16 + col;
     if (m >= a.M || row >= a.R) continue;
     auto total = [&](int tile) {
       float v = 0.0f;
@@ -362,7 +374,7 @@ bool x_rows(const void* x, int64_t M, int64_t C, int64_t ldx, int dtype) {
 }
 bool x_in_lds(int64_t M, int64_t C, int dtype) { return M <= 16 && x_bytes(M, C, dtype) <= kXInLds; }
 
-template <class D, int G, int RT, int NT, bool DUAL, int X, int THREADS, int ROWS = 4>
+template <class D, int G, int RT, int NT, bool DUAL, int X, int THREADS, int ROWS>
 int launch_rows(const RowsArgs& a, int waves, hipStream_t s) {
   const int per = DUAL ? RT / 2 : RT;
   size_t lds = (size_t)waves * RT * NT * 1024;
@@ -372,27 +384,36 @@ int launch_rows(const RowsArgs& a, int waves, hipStream_t s) {
   return CI_OK;
 }
 
-template <class D, int G, bool DUAL, int X, int THREADS, int ROWS>
-int launch_few(const RowsArgs& a, int waves, hipStream_t s) {
-  if constexpr (DUAL) return launch_rows<D, G, 2, 1, true, X, THREADS, ROWS>(a, waves, s);
-  else if (a.tiles >= 1024) return launch_rows<D, G, 2, 1, false, X, THREADS, ROWS>(a, waves, s);
-  else return launch_rows<D, G, 1, 1, false, X, THREADS, ROWS>(a, waves, s);
+template <class D, int G, bool DUAL, int X, int ROWS>
+int launch_few(const RowsArgs& a, hipStream_t s) {
+  // Eight waves to a compute unit, if there are as many blocks, and no more to a workgroup than registers leave room for (groups of 32, fp32).
+  // Pairs of tiles share what is read of x, where there are enough of them for the chip.
+  constexpr int MOST = D::VEC == 8 && G > 32 && X == kXLds ? 16 : 8;
+  const int RT = DUAL || a.tiles >= 900 ? 2 : 1, groups = DUAL ? a.tiles : (a.tiles + RT - 1) / RT;
+  int waves = 4;
+  while (waves < MOST && groups * waves < 2000 && waves * 2 <= a.nb) waves *= 2;
+  if constexpr (DUAL) {
+    return waves == 4 ? launch_rows<D, G, 2, 1, true, X, 256, ROWS>(a, waves, s) : launch_rows<D, G, 2, 1, true, X, MOST * 64, ROWS>(a, waves, s);
+  } else if (RT == 2) {
+    return launch_rows<D, G, 2, 1, false, X, 512, ROWS>(a, waves, s);   // never more than eight waves
+  } else {
+    return waves == 4 ? launch_rows<D, G, 1, 1, false, X, 256, ROWS>(a, waves, s) : launch_rows<D, G, 1, 1, false, X, MOST * 64, ROWS>(a, waves, s);
+  }
+}
+template <class D, int G, bool DUAL, int X>
+int launch_by_rows(const RowsArgs& a, hipStream_t s) {
+  if (a.M <= 4) return launch_few<D, G, DUAL, X, 1>(a, s);
+  return a.M <= 8 ? launch_few<D, G, DUAL, X, 2>(a, s) : launch_few<D, G, DUAL, X, 4>(a, s);
 }
 
 template <class D, int G, bool DUAL>
 int launch_shape(const RowsArgs& a, int x, hipStream_t s) {
-  if (x != kXOperands) {
-    // waves for two a SIMD on the whole chip, and no more than there are blocks or, of groups of 32 and fp32 rows, registers
-    constexpr int MOST = D::VEC == 8 && G > 32 ? 16 : 8;
-    int waves = 4;
-    while (waves < MOST && (int64_t)a.tiles * waves < 2048 && waves * 2 <= a.nb) waves *= 2;
-    if (a.M == 1)
-      return waves == 4 ? launch_few<D, G, DUAL, kXLds, 256, 1>(a, waves, s) : launch_few<D, G, DUAL, kXLds, MOST * 64, 1>(a, waves, s);
-    return launch_few<D, G, DUAL, kXLds, MOST * 64, 4>(a, waves, s);
-  }
-  if (a.M <= 16) return launch_rows<D, G, 2, 1, DUAL, kXOperands, 256>(a, 4, s);
-  if (a.M <= 32) return launch_rows<D, G, 2, 2, DUAL, kXOperands, 256>(a, 4, s);
-  return launch_rows<D, G, 2, 4, DUAL, kXOperands, 256>(a, 4, s);
+  if (x == kXLds) return launch_by_rows<D, G, DUAL, kXLds>(a, s);
+  if constexpr (D::VEC == 8)
+    if (x == kXRows) return launch_by_rows<D, G, DUAL, kXRows>(a, s);
+  if (a.M <= 16) return launch_rows<D, G, 2, 1, DUAL, kXOperands, 256, 4>(a, 4, s);
+  if (a.M <= 32) return launch_rows<D, G, 2, 2, DUAL, kXOperands, 256, 4>(a, 4, s);
+  return launch_rows<D, G, 2, 4, DUAL, kXOperands, 256, 4>(a, 4, s);
 }
 
 template <class D>
@@ -477,8 +498,8 @@ int launch_w4_matvec(const void* x, int64_t M, int64_t ldx, int x_dtype, const v
   a.nb = (int)col_blocks(C);
   a.tiles = (int)row_tiles(R);
   a.x_vectors = aligned16(x) && ldx * elem_bytes(x_dtype) % 16 == 0;
-  const int where = x_in_lds(M, C, x_dtype) ? kXLds : kXOperands;
-  a.x_bytes = where == kXRows ? (int)x_span(M, C, ldx) : 0;
+  const int where = x_in_lds(M, C, x_dtype) ? kXLds : x_rows(x, M, C, ldx, x_dtype) ? kXRows : kXOperands;
+  a.x_bytes = where == kXRows ? (int)x_span(M, C, ldx) : where == kXOperands ? (int)w4_matvec_ws_bytes(M, C, x_dtype) : 0;
   if (where == kXOperands) {
     const int NT = M <= 16 ? 1 : M <= 32 ? 2 : 4, words = a.nb * 4;
     const dim3 grid((words * NT + 3) / 4);
