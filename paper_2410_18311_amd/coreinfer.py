@@ -115,12 +115,26 @@ for _name, (_res, _args) in _SIGNATURES.items():
 
 EXPORTS = tuple(_SIGNATURES)
 
-# the per-token call, with addresses as integers: the C module if it was built for this interpreter, or the same through ctypes
+# the per-token calls, with addresses as integers: the C module if it was built for this interpreter, or the same through ctypes
 if os.path.exists(BINDING_PATH):
     from . import _binding  # linked against the library that is now loaded
     _decode_call = _binding.ffn_decode
+    _w4_matvec_call, _kv4_append_call, _kv4_read_call = _binding.w4_matvec, _binding.kv4_append, _binding.kv4_read
+    _kv4_attend_call, _kv4_evict_call = _binding.kv4_attend, _binding.kv4_evict
 else:
     _binding = None
+    _prototype = lambda name, *args: ctypes.CFUNCTYPE(_int, *args)((name, _lib))  # noqa: E731
+    _w4_matvec_call = _prototype("coreinfer_w4_matvec", *_SIGNATURES["coreinfer_w4_matvec"][1])
+    _kv4_read_call = _prototype("coreinfer_kv4_read", _vp, *_SIGNATURES["coreinfer_kv4_read"][1][1:])
+    _kv4_evict_call = _prototype("coreinfer_kv4_evict", _vp, *_SIGNATURES["coreinfer_kv4_evict"][1][1:])
+    _kv4_append_c = _prototype("coreinfer_kv4_append", _vp, *_SIGNATURES["coreinfer_kv4_append"][1][1:])
+    _kv4_attend_c = _prototype("coreinfer_kv4_attend", _vp, *_SIGNATURES["coreinfer_kv4_attend"][1][1:])
+
+    def _kv4_append_call(cache, k, v, S, s0, s1, s2, *rest):
+        return _kv4_append_c(cache, k, v, S, (_i64 * 3)(s0, s1, s2), *rest)
+
+    def _kv4_attend_call(cache, q, S, Hq, s0, s1, s2, *rest):
+        return _kv4_attend_c(cache, q, S, Hq, (_i64 * 3)(s0, s1, s2), *rest)
     _decode_call = ctypes.CFUNCTYPE(_int, _vp, _i64, _vp, _int, _int, _vp, _vp, _sz, _vp)(("coreinfer_ffn_decode", _lib))
 
 raw = _lib  # the bare C entry points, for tests of the error paths
@@ -660,7 +674,7 @@ class W4:
     """Weights [R, C] in 4 bits, in groups along C (w4_quantize)."""
 
     def __init__(self, packed: torch.Tensor, R: int, C: int, group: int):
-        self.packed, self.R, self.C, self.group = packed, R, C, group
+        self.packed, self.R, self.C, self.group, self.ptr = packed, R, C, group, packed.data_ptr()
 
 
 def w4_size(R: int, C: int, group: int) -> int:
@@ -705,24 +719,26 @@ def w4_matvec(x: torch.Tensor, w: W4, gate: Optional[W4] = None, bias: Optional[
               y: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
               out_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
     """coreinfer_w4_matvec on x [M, C] (or [C]): act(x W^T + bias), "swiglu" with `gate`: SiLU(x G^T) * (x W^T)."""
-    x2 = x if x.dim() == 2 else x.unsqueeze(0)
-    M, C = x2.shape
-    assert C == w.C and x2.stride(1) == 1
-    assert gate is None or (gate.R, gate.C, gate.group) == (w.R, w.C, w.group)
-    assert bias is None or (bias.numel() == w.R and bias.is_contiguous())
+    R, C = w.R, w.C
+    M, (ldx, last) = (x.shape[0], x.stride()) if x.dim() == 2 else (1, (C, x.stride(0)))
+    assert x.shape[-1] == C and last == 1
+    assert gate is None or (gate.R, gate.C, gate.group) == (R, C, w.group)
+    assert bias is None or (bias.numel() == R and bias.is_contiguous())
     if y is None:
-        y = torch.empty((M, w.R), dtype=out_dtype or x.dtype, device=x.device)
-    y2 = y if y.dim() == 2 else y.unsqueeze(0)
-    assert y2.shape == (M, w.R) and y2.stride(1) == 1
-    if ws is None:
+        y = torch.empty((M, R) if x.dim() == 2 else (R,), dtype=out_dtype or x.dtype, device=x.device)
+    ldy, last = y.stride() if y.dim() == 2 else (R, y.stride(0))
+    assert y.shape[-1] == R and y.numel() == M * R and last == 1
+    x_type, y_type = DTYPE_CODE[x.dtype], DTYPE_CODE[y.dtype]
+    if ws is None and (M > 4 or M * C > 8192):   # fewer need none
         need = w4_matvec_workspace_size(M, C, x.dtype)
         ws = _workspace(need, x) if need else None
-    _check(_lib.coreinfer_w4_matvec(_ptr(x2), M, x2.stride(0) if M > 1 else C, DTYPE_CODE[x.dtype], _ptr(w.packed),
-                                    None if gate is None else _ptr(gate.packed), _ptr(bias),
-                                    0 if bias is None else DTYPE_CODE[bias.dtype], _W4_ACT[act], w.R, C, w.group, _ptr(y2),
-                                    y2.stride(0) if M > 1 else w.R, DTYPE_CODE[y2.dtype], _ptr(ws),
-                                    0 if ws is None else ws.numel(), _stream(x)), "coreinfer_w4_matvec")
-    return y.squeeze(0) if x.dim() == 1 and y.dim() == 2 else y
+    status = _w4_matvec_call(x.data_ptr(), M, ldx if M > 1 else C, x_type, w.ptr, None if gate is None else gate.ptr,
+                             None if bias is None else bias.data_ptr(), 0 if bias is None else DTYPE_CODE[bias.dtype],
+                             _W4_ACT[act], R, C, w.group, y.data_ptr(), ldy if M > 1 else R, y_type,
+                             None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _stream(x))
+    if status != CI_OK:
+        raise CoreInferError(status, "coreinfer_w4_matvec")
+    return y
 
 
 class Kv4Cache:
@@ -732,6 +748,7 @@ class Kv4Cache:
         self.k, self.v, self.k_scale, self.v_scale, self.weight, self.pos = k, v, k_scale, v_scale, weight, pos
         self.B, self.H, self.cap, self.D, self.group = shape
         self.desc = ci_kv4(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(weight), _ptr(pos), *shape)
+        self.ptr = ctypes.addressof(self.desc)
 
 
 def kv4_cache(B: int, H: int, cap: int, D: int, group: int = 64, weights: bool = True, device="cuda") -> Kv4Cache:
@@ -750,20 +767,19 @@ def _check_lens(cache: Kv4Cache, *lens: Optional[torch.Tensor]):
         assert t is None or (t.dtype == torch.int32 and t.numel() == cache.B and t.is_contiguous())
 
 
-def _strides(t: torch.Tensor):
-    return (_i64 * 3)(*t.stride()[:3])
-
-
 def kv4_append(cache: Kv4Cache, k: torch.Tensor, v: torch.Tensor, lens: torch.Tensor, start: Optional[torch.Tensor] = None,
                next_pos: Optional[torch.Tensor] = None) -> None:
     """coreinfer_kv4_append: k, v [B, S, H, D] (any strides, the same for both, channels contiguous) become the last S of
     the lens[b] slots of each sentence."""
-    assert k.shape == v.shape and k.dtype == v.dtype and k.dim() == 4 and k.stride() == v.stride() and k.stride(3) == 1
-    B, S, H, D = k.shape
+    B, S, H, D = shape = k.shape
+    stride = k.stride()
+    assert v.shape == shape and v.dtype == k.dtype and v.stride() == stride and stride[3] == 1
     assert (B, H, D) == (cache.B, cache.H, cache.D)
     _check_lens(cache, lens, start, next_pos)
-    _check(_lib.coreinfer_kv4_append(ctypes.byref(cache.desc), _ptr(k), _ptr(v), S, _strides(k), DTYPE_CODE[k.dtype],
-                                     _ptr(start), _ptr(lens), _ptr(next_pos), _stream(k)), "coreinfer_kv4_append")
+    status = _kv4_append_call(cache.ptr, k.data_ptr(), v.data_ptr(), S, stride[0], stride[1], stride[2], DTYPE_CODE[k.dtype],
+                              _ptr(start), lens.data_ptr(), _ptr(next_pos), _stream(k))
+    if status != CI_OK:
+        raise CoreInferError(status, "coreinfer_kv4_append")
 
 
 def kv4_read(cache: Kv4Cache, lens: torch.Tensor, first: int, count: int, dtype: torch.dtype,
@@ -777,8 +793,9 @@ def kv4_read(cache: Kv4Cache, lens: torch.Tensor, first: int, count: int, dtype:
     for t in (k, v):
         assert t.shape == shape and t.dtype == dtype and t.is_contiguous()
     _check_lens(cache, lens)
-    _check(_lib.coreinfer_kv4_read(ctypes.byref(cache.desc), _ptr(lens), first, count, _ptr(k), _ptr(v), DTYPE_CODE[dtype],
-                                   _stream(k)), "coreinfer_kv4_read")
+    status = _kv4_read_call(cache.ptr, lens.data_ptr(), first, count, k.data_ptr(), v.data_ptr(), DTYPE_CODE[dtype], _stream(k))
+    if status != CI_OK:
+        raise CoreInferError(status, "coreinfer_kv4_read")
     return k, v
 
 
@@ -794,21 +811,24 @@ def kv4_attend(q: torch.Tensor, cache: Kv4Cache, lens: torch.Tensor, scale: Opti
                weight_out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
     """coreinfer_kv4_attend: q [B, S, Hq, D], the last S tokens of each sentence, over the cache.  scale: 1 / sqrt(D) by
     default; max_len: the most any of lens is (the cache's capacity by default; the launches are sized by it)."""
-    B, S, Hq, D = q.shape
-    assert (B, D) == (cache.B, cache.D) and q.stride(3) == 1
+    B, S, Hq, D = shape = q.shape
+    stride, dtype = q.stride(), q.dtype
+    assert (B, D) == (cache.B, cache.D) and stride[3] == 1
     _check_lens(cache, lens)
     max_len = cache.cap if max_len is None else max_len
     if out is None:
-        out = torch.empty((B, S, Hq, D), dtype=q.dtype, device=q.device)
-    assert out.shape == q.shape and out.dtype == q.dtype and out.is_contiguous()
+        out = torch.empty(shape, dtype=dtype, device=q.device)
+    assert out.shape == shape and out.dtype == dtype and out.is_contiguous()
     assert lse is None or (lse.shape == (B, S, Hq) and lse.dtype == torch.float32 and lse.is_contiguous())
     assert weight_out is None or (weight_out.shape == (B, cache.H, cache.cap) and weight_out.dtype == torch.float32 and
                                   weight_out.is_contiguous())
     if ws is None:
         ws = _workspace(kv4_attend_workspace_size(cache, S, Hq, max_len, weight_out is not None), q)
-    _check(_lib.coreinfer_kv4_attend(ctypes.byref(cache.desc), _ptr(q), S, Hq, _strides(q), DTYPE_CODE[q.dtype],
-                                     D ** -0.5 if scale is None else scale, _ptr(lens), max_len, _ptr(out), _ptr(lse),
-                                     _ptr(weight_out), _ptr(ws), ws.numel(), _stream(q)), "coreinfer_kv4_attend")
+    status = _kv4_attend_call(cache.ptr, q.data_ptr(), S, Hq, stride[0], stride[1], stride[2], DTYPE_CODE[dtype],
+                              D ** -0.5 if scale is None else float(scale), lens.data_ptr(), max_len, out.data_ptr(), _ptr(lse),
+                              _ptr(weight_out), ws.data_ptr(), ws.numel(), _stream(q))
+    if status != CI_OK:
+        raise CoreInferError(status, "coreinfer_kv4_attend")
     return out
 
 
@@ -834,6 +854,7 @@ def kv4_evict(cache: Kv4Cache, lens: torch.Tensor, next_pos: torch.Tensor, budge
         assert t is None or (t.shape == (cache.B, cache.H, cache.cap) and t.dtype == dtype and t.is_contiguous())
     if ws is None:
         ws = _workspace(kv4_evict_workspace_size(cache, max_len, budget), lens)
-    _check(_lib.coreinfer_kv4_evict(ctypes.byref(cache.desc), _ptr(lens), _ptr(next_pos), max_len, budget, recent,
-                                    _ptr(weight_out), _ptr(pos_out), _ptr(lens_out), _ptr(ws), ws.numel(), _stream(lens)),
-           "coreinfer_kv4_evict")
+    status = _kv4_evict_call(cache.ptr, lens.data_ptr(), next_pos.data_ptr(), max_len, budget, recent, _ptr(weight_out),
+                             _ptr(pos_out), lens_out.data_ptr(), ws.data_ptr(), ws.numel(), _stream(lens))
+    if status != CI_OK:
+        raise CoreInferError(status, "coreinfer_kv4_evict")

@@ -1,9 +1,11 @@
-/* The per-token call of the Python binding without ctypes, whose conversion of nine arguments costs the host more than the
+/* The per-token calls of the Python binding without ctypes, whose conversion of nine arguments costs the host more than the
  * checks and the choice of a kernel behind them (a call that fails the first check: 0.42 us, 0.06 so, on one host, 1.25 and 0.12 on
  * another).  A decode call of a small layer is bound by the host: 128 x 205 fp32 4.8 -> 4.1 us, a prompt and 16 tokens of 256 x 1024
  * 137 -> 126. */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
+#include <stdint.h>
+#include <string.h>
 
 #include "coreinfer.h"
 
@@ -36,7 +38,111 @@ static PyObject* ffn_decode(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   return PyLong_FromLong(status);
 }
 
-static PyMethodDef methods[] = {{"ffn_decode", (PyCFunction)(void (*)(void))ffn_decode, METH_FASTCALL, NULL}, {NULL, NULL, 0, NULL}};
+/* The 4-bit operators' calls: their C arguments in order, addresses and numbers alike as integers (or None), three element strides one
+ * by one.  Everything fits long long; scale is a float. */
+static int values(const char* name, PyObject* const* a, Py_ssize_t n, Py_ssize_t want, long long* v) {
+  Py_ssize_t i;
+  if (n != want) {
+    PyErr_Format(PyExc_TypeError, "%s: %zd arguments", name, want);
+    return 0;
+  }
+  for (i = 0; i < n; ++i) {
+    if (a[i] == Py_None) {
+      v[i] = 0;
+    } else if (PyFloat_Check(a[i])) {
+      const double d = PyFloat_AS_DOUBLE(a[i]);
+      memcpy(&v[i], &d, sizeof d);
+    } else {
+      v[i] = PyLong_AsLongLong(a[i]);
+      if (v[i] == -1 && PyErr_Occurred()) return 0;
+    }
+  }
+  return 1;
+}
+#define P(i) ((void*)(intptr_t)v[i])
+#define I(i) ((int)v[i])
+
+/* x, M, ldx, x_dtype, w, gate, bias, bias_dtype, act, R, C, group, y, ldy, y_dtype, ws, ws_bytes, stream */
+static PyObject* w4_matvec(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  long long v[18];
+  int status;
+  (void)self;
+  if (!values("w4_matvec", a, n, 18, v)) return NULL;
+  Py_BEGIN_ALLOW_THREADS
+  status = coreinfer_w4_matvec(P(0), v[1], v[2], I(3), P(4), P(5), P(6), I(7), I(8), v[9], v[10], I(11), P(12), v[13], I(14), P(15),
+                               (size_t)v[16], P(17));
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+/* cache, k, v, S, strides b, s, h, dtype, start, lens, next, stream */
+static PyObject* kv4_append(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  long long v[12];
+  int64_t stride[3];
+  int status;
+  (void)self;
+  if (!values("kv4_append", a, n, 12, v)) return NULL;
+  stride[0] = v[4];
+  stride[1] = v[5];
+  stride[2] = v[6];
+  Py_BEGIN_ALLOW_THREADS
+  status = coreinfer_kv4_append((const ci_kv4*)P(0), P(1), P(2), v[3], stride, I(7), (const int32_t*)P(8), (const int32_t*)P(9),
+                                (const int32_t*)P(10), P(11));
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+/* cache, lens, first, count, k, v, dtype, stream */
+static PyObject* kv4_read(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  long long v[8];
+  int status;
+  (void)self;
+  if (!values("kv4_read", a, n, 8, v)) return NULL;
+  Py_BEGIN_ALLOW_THREADS
+  status = coreinfer_kv4_read((const ci_kv4*)P(0), (const int32_t*)P(1), v[2], v[3], P(4), P(5), I(6), P(7));
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+/* cache, q, S, Hq, strides b, s, h, dtype, scale (a float), lens, max_len, out, lse, weight_out, ws, ws_bytes, stream */
+static PyObject* kv4_attend(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  long long v[17];
+  int64_t stride[3];
+  double scale;
+  int status;
+  (void)self;
+  if (!values("kv4_attend", a, n, 17, v)) return NULL;
+  if (!PyFloat_Check(a[8])) {
+    PyErr_SetString(PyExc_TypeError, "kv4_attend: scale is a float");
+    return NULL;
+  }
+  memcpy(&scale, &v[8], sizeof scale);
+  stride[0] = v[4];
+  stride[1] = v[5];
+  stride[2] = v[6];
+  Py_BEGIN_ALLOW_THREADS
+  status = coreinfer_kv4_attend((const ci_kv4*)P(0), P(1), v[2], v[3], stride, I(7), (float)scale, (const int32_t*)P(9), v[10], P(11),
+                                (float*)P(12), (float*)P(13), P(14), (size_t)v[15], P(16));
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+/* cache, lens, next, max_len, budget, recent, weight_out, pos_out, lens_out, ws, ws_bytes, stream */
+static PyObject* kv4_evict(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  long long v[12];
+  int status;
+  (void)self;
+  if (!values("kv4_evict", a, n, 12, v)) return NULL;
+  Py_BEGIN_ALLOW_THREADS
+  status = coreinfer_kv4_evict((const ci_kv4*)P(0), (const int32_t*)P(1), (const int32_t*)P(2), v[3], v[4], v[5], (float*)P(6),
+                               (int32_t*)P(7), (int32_t*)P(8), P(9), (size_t)v[10], P(11));
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+#define CALL(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, NULL}
+static PyMethodDef methods[] = {CALL(ffn_decode), CALL(w4_matvec), CALL(kv4_append), CALL(kv4_read), CALL(kv4_attend), CALL(kv4_evict),
+                                {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__binding(void) { return PyModule_Create(&module); }
