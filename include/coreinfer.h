@@ -535,6 +535,7 @@ int coreinfer_kv4_sizes(int64_t B, int64_t H, int64_t cap, int D, int group, siz
  * have theirs at the end of the S; slots outside 0 .. cap - 1 are not written either.
  * weight of a written slot becomes 0, pos (where the cache has them) next[b] - S + i;
  * next [B]: the sentence's tokens so far, evicted ones included, NULL = lens.
+ * 1 <= S <= CI_MAX_TOKENS.
  */
 int coreinfer_kv4_append(const ci_kv4* cache, const void* k, const void* v, int64_t S, const int64_t* stride, int dtype,
                          const int32_t* start, const int32_t* lens, const int32_t* next, void* stream);

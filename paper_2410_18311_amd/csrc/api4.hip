@@ -107,7 +107,7 @@ int coreinfer_kv4_append(const ci_kv4* cache, const void* k, const void* v, int6
   if (!type_ok(dtype)) return CI_ERR_BAD_DTYPE;
   const int rc = cache_status(cache);
   if (rc != CI_OK) return rc;
-  if (!k || !v || !stride || !lens || S < 1 || S > CI_MAX_CACHE_SLOTS) return CI_ERR_INVALID_ARG;
+  if (!k || !v || !stride || !lens || S < 1 || S > CI_MAX_TOKENS) return CI_ERR_INVALID_ARG;
   if (!strides_ok(stride) || !elem_aligned(k, dtype) || !elem_aligned(v, dtype) || !word_aligned(start) || !word_aligned(lens) ||
       !word_aligned(next))
     return CI_ERR_BAD_LAYOUT;

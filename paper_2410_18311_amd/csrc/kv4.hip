@@ -19,56 +19,69 @@ struct AppendArgs {
 };
 
 // A workgroup has 16 slots of a head: one wave their keys, the other their values.  A slot's D channels are held by D / 8 neighbouring lanes.
+// Workgroups that run together have neighbouring heads, whose rows are neighbours in memory.
 template <class T, int D, int GR>
 __global__ __launch_bounds__(128) void kv4_append_kernel(AppendArgs a) {
   constexpr int LPT = D / 8, TP = 64 / LPT, PASSES = 16 / TP, NG = D / GR;
   __shared__ __attribute__((aligned(16))) uint8_t code[16][D];  // of the values, on the way to their quads
-  const int lane = threadIdx.x & 63, h = blockIdx.y, b = blockIdx.z;
+  const int lane = threadIdx.x & 63, h = blockIdx.x, b = blockIdx.z;
   const bool values = threadIdx.x >= 64;
   const int64_t len = a.lens[b], from = len - a.S;   // slot of the first token
   const int64_t start = a.start ? a.start[b] : 0;
   const int64_t first = max(max(from, start), (int64_t)0), last = min(len, (int64_t)a.c.cap);
-  const int64_t slot0 = (first / 16 + blockIdx.x) * 16;
+  const int64_t slot0 = (first / 16 + blockIdx.y) * 16;
   if (slot0 >= last) return;   // the whole workgroup
   const size_t head = (size_t)b * a.c.H + h;
   const typename T::T* src = reinterpret_cast<const typename T::T*>(values ? a.v : a.k) + b * a.s_b + h * a.s_h;
   uint32_t* scales = (values ? a.c.vs : a.c.ks) + head * NG * a.c.cap;
   const int d0 = (lane % LPT) * 8;
+  // all rows on their way before the first is used; slots that are not written read a neighbour's
+  uint4 raw[PASSES][8 / T::VEC];
+  auto any_in = [&](int p) { return slot0 + (p + 1) * TP > first && slot0 + p * TP < last; };
 #pragma unroll
   for (int p = 0; p < PASSES; ++p) {
+    if (!any_in(p)) continue;
+    const int64_t slot = min(max(slot0 + p * TP + lane / LPT, first), last - 1);
+    const typename T::T* row = src + (slot - from) * a.s_s + d0;
+    if (a.vectors) {
+#pragma unroll
+      for (int i = 0; i < 8 / T::VEC; ++i) raw[p][i] = ld16(row + i * T::VEC);
+    } else {
+      typename T::T e[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) e[i] = row[i];
+      __builtin_memcpy(raw[p], e, sizeof(e));
+    }
+  }
+#pragma unroll
+  for (int p = 0; p < PASSES; ++p) {
+    if (!any_in(p)) continue;   // nothing of its places in the LDS is used
     const int at = p * TP + lane / LPT;
     const int64_t slot = slot0 + at;
     const bool in = slot >= first && slot < last;
     float x[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = 0.0f;
-    if (in) {
-      const typename T::T* row = src + (slot - from) * a.s_s + d0;
-      if (a.vectors) {
-        float f[T::VEC];
+    for (int i = 0; i < 8 / T::VEC; ++i) {
+      float f[T::VEC];
+      unpack<T>(raw[p][i], f);
 #pragma unroll
-        for (int i = 0; i < 8 / T::VEC; ++i) {
-          unpack<T>(ld16(row + i * T::VEC), f);
-#pragma unroll
-          for (int e = 0; e < T::VEC; ++e) x[i * T::VEC + e] = f[e];
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = to_float<T>(row[e]);
-      }
+      for (int e = 0; e < T::VEC; ++e) x[i * T::VEC + e] = f[e];
     }
     float lo = x[0], hi = x[0];
 #pragma unroll
     for (int e = 1; e < 8; ++e) lo = min_nan(lo, x[e]), hi = max_nan(hi, x[e]);
-#pragma unroll
-    for (int off = 1; off < GR / 8; off <<= 1) {
-      lo = min_nan(lo, __shfl_xor(lo, off, kWave));
-      hi = max_nan(hi, __shfl_xor(hi, off, kWave));
-    }
+    // over the lanes of a group, by moves within sixteen lanes: the neighbour, the other pair, the other four, the other eight
+    auto both = [&](auto ctrl) {
+      lo = min_nan(lo, u2f((uint32_t)__builtin_amdgcn_mov_dpp((int)f2u(lo), decltype(ctrl)::value, 0xf, 0xf, true)));
+      hi = max_nan(hi, u2f((uint32_t)__builtin_amdgcn_mov_dpp((int)f2u(hi), decltype(ctrl)::value, 0xf, 0xf, true)));
+    };
+    both(std::integral_constant<int, 0xb1>{});
+    both(std::integral_constant<int, 0x4e>{});
+    if constexpr (GR >= 64) both(std::integral_constant<int, 0x141>{});
+    if constexpr (GR >= 128) both(std::integral_constant<int, 0x140>{});
     const uint32_t scale = q4_scale(lo, hi);
     uint32_t n[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) n[e] = q4_code(x[e], scale);
+    q4_codes(x, scale, n);
     if (in && d0 % GR == 0) scales[(size_t)(d0 / GR) * a.c.cap + slot] = scale;
     if (values) {
       *reinterpret_cast<uint2*>(&code[at][d0]) = make_uint2(n[0] | n[1] << 8 | n[2] << 16 | n[3] << 24,
@@ -465,7 +478,7 @@ struct AppendLaunch {
   hipStream_t s;
   template <class T, int D, int GR>
   int operator()() const {
-    hipLaunchKernelGGL((kv4_append_kernel<T, D, GR>), dim3((a.S + 14) / 16 + 1, a.c.H, a.c.B), dim3(128), 0, s, a);
+    hipLaunchKernelGGL((kv4_append_kernel<T, D, GR>), dim3(a.c.H, (a.S + 14) / 16 + 1, a.c.B), dim3(128), 0, s, a);
     CI_HIP_CHECK_LAUNCH();
     return CI_OK;
   }

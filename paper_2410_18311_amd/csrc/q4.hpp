@@ -120,12 +120,28 @@ __device__ __forceinline__ uint32_t q4_code(float x, uint32_t scale) {
   const float n = rintf((x - half_hi(scale)) / step);
   return (uint32_t)fminf(fmaxf(n, 0.0f), 15.0f);
 }
+// The codes of eight elements of a group.  A product with the reciprocal is within 2^-20 of the quotient for what counts (up to 16), so only
+// where it lies that close to the middle between two codes do the divisions decide; a fifth of the instructions otherwise.
+__device__ __forceinline__ void q4_codes(const float (&x)[8], uint32_t scale, uint32_t (&n)[8]) {
+  const float step = half_lo(scale), low = half_hi(scale), inv = __builtin_amdgcn_rcpf(step);
+  bool close = false;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float q = (x[e] - low) * inv, r = rintf(q);
+    close |= fabsf(fabsf(q - r) - 0.5f) < 8e-6f;
+    n[e] = step > 0.0f ? (uint32_t)fminf(fmaxf(r, 0.0f), 15.0f) : 0u;
+  }
+  if (__any(close)) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) n[e] = q4_code(x[e], scale);
+  }
+}
 __device__ __forceinline__ float q4_value(uint32_t code, uint32_t scale) {
   return __builtin_fmaf(half_lo(scale), (float)code, half_hi(scale));
 }
-// Extremes that a NaN takes over.
-__device__ __forceinline__ float min_nan(float a, float b) { return a < b || a != a ? a : b; }
-__device__ __forceinline__ float max_nan(float a, float b) { return a > b || a != a ? a : b; }
+// Extremes that a NaN takes over, in one instruction.
+__device__ __forceinline__ float min_nan(float a, float b) { return __builtin_elementwise_minimum(a, b); }
+__device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
 }  // namespace
 }  // namespace ci

@@ -72,9 +72,11 @@ __global__ __launch_bounds__(256) void w4_quantize_kernel(const typename D::T* w
     for (int j = s * J; j < s * J + J; ++j) {
       const int c = col0 + 32 * j + 8 * g;
       word[j] = 0;
+      uint32_t n8[8];
+      q4_codes(x[j], scale, n8);
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (row < R && c + e < C) word[j] |= q4_code(x[j][e], scale) << (4 * q4_nibble(e));
+        if (row < R && c + e < C) word[j] |= n8[e] << (4 * q4_nibble(e));
     }
     if (g == s % 4) scales[(block * 16 + n) * (4 / J) + s] = scale;
   }
