@@ -535,7 +535,7 @@ int coreinfer_kv4_sizes(int64_t B, int64_t H, int64_t cap, int D, int group, siz
  * have theirs at the end of the S; slots outside 0 .. cap - 1 are not written either.
  * weight of a written slot becomes 0, pos (where the cache has them) next[b] - S + i;
  * next [B]: the sentence's tokens so far, evicted ones included, NULL = lens.
- * 1 <= S <= CI_MAX_TOKENS.
+ * 1 <= S <= 2^19.
  */
 int coreinfer_kv4_append(const ci_kv4* cache, const void* k, const void* v, int64_t S, const int64_t* stride, int dtype,
                          const int32_t* start, const int32_t* lens, const int32_t* next, void* stream);
@@ -565,7 +565,7 @@ int coreinfer_kv4_read(const ci_kv4* cache, const int32_t* lens, int64_t first, 
  * two bf16 pieces (fp32 q: three).  The order of the sums is fixed.
  * ws: coreinfer_kv4_attend_workspace_size bytes, 16-byte aligned (weights != 0: for
  * calls with weight_out).  Calls that share a workspace must not overlap in time.
- * Limits: S * (Hq / H) <= 2^20.
+ * Limits: Hq / H <= 4096, S * (Hq / H) <= 2^20.
  */
 int coreinfer_kv4_attend_workspace_size(int64_t B, int64_t H, int D, int64_t S, int64_t Hq, int64_t max_len, int weights,
                                         size_t* bytes);

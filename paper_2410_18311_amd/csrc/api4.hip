@@ -107,7 +107,7 @@ int coreinfer_kv4_append(const ci_kv4* cache, const void* k, const void* v, int6
   if (!type_ok(dtype)) return CI_ERR_BAD_DTYPE;
   const int rc = cache_status(cache);
   if (rc != CI_OK) return rc;
-  if (!k || !v || !stride || !lens || S < 1 || S > CI_MAX_TOKENS) return CI_ERR_INVALID_ARG;
+  if (!k || !v || !stride || !lens || S < 1 || S > (1 << 19)) return CI_ERR_INVALID_ARG;
   if (!strides_ok(stride) || !elem_aligned(k, dtype) || !elem_aligned(v, dtype) || !word_aligned(start) || !word_aligned(lens) ||
       !word_aligned(next))
     return CI_ERR_BAD_LAYOUT;
@@ -128,7 +128,8 @@ int coreinfer_kv4_attend_workspace_size(int64_t B, int64_t H, int D, int64_t S, 
                                         size_t* bytes) {
   const int rc = shape_status(B, H, 32, D, 32);
   if (rc != CI_OK) return rc;
-  if (!bytes || S < 1 || S > (1 << 20) || Hq < H || Hq > ((int64_t)1 << 32) || Hq % H != 0 || S * (Hq / H) > (1 << 20) || max_len < 1 ||
+  if (!bytes || S < 1 || S > (1 << 20) || Hq < H || Hq > ((int64_t)1 << 32) || Hq % H != 0 || Hq / H > 4096 ||
+      S * (Hq / H) > (1 << 20) || max_len < 1 ||
       max_len > CI_MAX_CACHE_SLOTS)
     return CI_ERR_INVALID_ARG;
   *bytes = kv4_attend_ws_bytes(B * H, D, S, Hq / H, max_len, weights != 0);

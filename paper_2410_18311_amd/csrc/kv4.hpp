@@ -33,11 +33,12 @@ struct Kv4Attend {
   float* weight_out;
   const int32_t* lens;
   int S, G, R, max_len;   // R = S G rows of a head of the cache
+  uint32_t inverse_G;     // 2^32 / G, rounded up
   float scale;            // of the logits, with log2(e)
   int q_vectors;
   // Work of the launch: `blocks` workgroups (times those along the rows) share the slots of all sentences; see Shares.  wanted 0: one workgroup a head.
   int blocks, wanted, least;
-  int row_tiles, token_waves, NR;  // tiles of 16 rows; waves of a workgroup along the slots (4 or 1); tiles of 16 rows a wave
+  int row_tiles, token_waves;      // tiles of 16 rows; waves of a workgroup along the slots (4 or 1: then along the tiles)
   int weights;                     // 0 none, 1 from stored logits, 2 from logits computed again
   int2* place;  // [B]: a sentence's first piece and how many it has
   // partial results [blocks, row_tiles 16] twice and [blocks, row_tiles 16, D]; log-sums [B H, R]; logits [B H, R, whole steps of slots]

@@ -10,7 +10,7 @@ constexpr int kCus = 256;   // of an MI355X; a workspace query knows no device
 constexpr double kLog2e = 1.4426950408889634;
 
 struct AttendPlan {
-  int R, row_tiles, NR, token_waves, blocks, wanted, least, weights;
+  int R, row_tiles, token_waves, blocks, wanted, least, weights;
   size_t place, m, l, o, z, logits, bytes;   // places in the workspace
 };
 
@@ -19,14 +19,12 @@ AttendPlan attend_plan(int64_t heads, int D, int64_t S, int64_t G, int64_t max_l
   p.R = (int)(S * G);
   p.row_tiles = (p.R + 15) / 16;
   p.weights = !weights ? 0 : p.R <= 16 ? 1 : 2;
-  p.NR = p.R <= 16 ? 1 : 2;
-  const int wave_tiles = (p.row_tiles + p.NR - 1) / p.NR;
-  p.token_waves = wave_tiles >= 4 ? 1 : 4;
-  const int64_t row_blocks = p.token_waves == 4 ? wave_tiles : (wave_tiles + 3) / 4;
+  p.token_waves = p.row_tiles >= 4 ? 1 : 4;
+  const int64_t row_blocks = p.token_waves == 4 ? p.row_tiles : (p.row_tiles + 3) / 4;
   const int64_t steps = (max_len + 31) / 32, blocks = heads * row_blocks;
-  // Three workgroups a compute unit where waves share the slots (what the registers leave room for), one where they share the rows; no
+  // Three workgroups a compute unit (what the registers leave room for), two where waves share the rows (whose partial results are many); no
   // piece below two steps a wave, respectively 16 steps.
-  const int64_t wanted = (p.token_waves == 4 ? 3 : 1) * kCus;
+  const int64_t wanted = (p.token_waves == 4 ? 3 : 2) * kCus;
   p.least = p.token_waves == 4 ? 8 : 16;
   p.wanted = blocks * 2 > wanted || steps <= p.least ? 0 : (int)(wanted / row_blocks);
   p.blocks = (int)heads + p.wanted;
@@ -69,6 +67,7 @@ int launch_kv4_attend(const ci_kv4& c, const void* q, int64_t S, int64_t G, cons
   a.lens = lens;
   a.S = (int)S;
   a.G = (int)G;
+  a.inverse_G = (uint32_t)((((uint64_t)1 << 32) + G - 1) / G);
   a.R = p.R;
   a.max_len = (int)max_len;
   a.scale = (float)(scale * kLog2e);
@@ -86,7 +85,6 @@ int launch_kv4_attend(const ci_kv4& c, const void* q, int64_t S, int64_t G, cons
   a.least = p.least;
   a.row_tiles = p.row_tiles;
   a.token_waves = p.token_waves;
-  a.NR = p.NR;
   a.weights = p.weights;
   switch (dtype) {
     case CI_F32: return launch_kv4_attend_type<F32>(a, c.D, c.group, s);

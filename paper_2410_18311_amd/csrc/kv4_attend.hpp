@@ -32,29 +32,47 @@ __device__ __forceinline__ uint4 ld_row(const uint32_t* p) {
   return make_uint4(u.x, u.y, 0, 0);
 }
 
-// The rows of a tile as operands, zero rows nowhere: rows past the last repeat it.  sums: of the row's channels by group, minus-offset.
-template <class T, int D, int GR>
-__device__ __forceinline__ void load_rows(const Kv4Attend& a, int b, int h, int row, uint4 (&q)[D / 32][Q4Type<T>::PIECES],
-                                          float (&sums)[D / GR]) {
-  constexpr int OP = Q4Type<T>::OP, PIECES = Q4Type<T>::PIECES;
-  const int g = (threadIdx.x & 63) >> 4, s = row / a.G, i = row % a.G;
+// The token of a row: row / G, rows and G being below 2^20 and 2^12.
+__device__ __forceinline__ int row_token(const Kv4Attend& a, int row) { return a.G == 1 ? row : (int)__umulhi((uint32_t)row, a.inverse_G); }
+
+// A lane's channels of a row of q as they are in memory: eight of each 32.
+template <class T, int D>
+struct RawRow {
+  uint4 raw[D / 32][8 / T::VEC];
+};
+template <class T, int D>
+__device__ __forceinline__ void load_raw(const Kv4Attend& a, int b, int h, int row, RawRow<T, D>& r) {
+  const int g = (threadIdx.x & 63) >> 4, s = row_token(a, row), i = row - s * a.G;
   const typename T::T* src = reinterpret_cast<const typename T::T*>(a.q) + b * a.q_b + s * a.q_s + (int64_t)(h * a.G + i) * a.q_h + 8 * g;
+  if (a.q_vectors) {
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+      for (int e = 0; e < 8 / T::VEC; ++e) r.raw[j][e] = ld16(src + 32 * j + e * T::VEC);
+  } else {
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) {
+      typename T::T x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = src[32 * j + e];
+      __builtin_memcpy(r.raw[j], x, sizeof(x));
+    }
+  }
+}
+// The same as operands, and the sums of the row's channels by group.
+template <class T, int D, int GR>
+__device__ __forceinline__ void make_rows(const RawRow<T, D>& r, uint4 (&q)[D / 32][Q4Type<T>::PIECES], float (&sums)[D / GR]) {
+  constexpr int OP = Q4Type<T>::OP, PIECES = Q4Type<T>::PIECES;
 #pragma unroll
   for (int j = 0; j < D / 32; ++j) {
     if constexpr (T::VEC == 8) {
-      if (a.q_vectors) q[j][0] = ld16(src + 32 * j);
-      else {
-        uint32_t p[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          p[e] = (uint32_t)__builtin_bit_cast(uint16_t, src[32 * j + 2 * e]) |
-                 (uint32_t)__builtin_bit_cast(uint16_t, src[32 * j + 2 * e + 1]) << 16;
-        q[j][0] = make_uint4(p[0], p[1], p[2], p[3]);
-      }
+      q[j][0] = r.raw[j][0];
     } else {
+      float x[8];
+      __builtin_memcpy(x, r.raw[j], sizeof(x));
       uint32_t p[4][3];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) split_bf16<3>(src[32 * j + 2 * e], src[32 * j + 2 * e + 1], p[e]);
+      for (int e = 0; e < 4; ++e) split_bf16<3>(x[2 * e], x[2 * e + 1], p[e]);
 #pragma unroll
       for (int c = 0; c < 3; ++c) q[j][c] = make_uint4(p[0][c], p[1][c], p[2][c], p[3][c]);
     }
@@ -71,25 +89,30 @@ __device__ __forceinline__ void load_rows(const Kv4Attend& a, int b, int h, int 
   }
 }
 
-// Logits (without the scale) of 16 slots, four to a lane, and the rows of q.
+// Logits (without the scale) of 16 slots, four to a lane, and the rows of q.  rest: the lowest value less the codes' offset in steps.
 template <class T, int D, int GR>
-__device__ __forceinline__ f32x4q logits_of(const uint4 (&k)[D / 32], const uint4 (&scale)[D / GR],
+__device__ __forceinline__ void rests_of(const uint4 (&scale)[D / GR], float (&rest)[D / GR][4]) {
+#pragma unroll
+  for (int f = 0; f < D / GR; ++f)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      rest[f][r] = __builtin_fmaf(half_lo(word_of(scale[f], r)), -kOffset<Q4Type<T>::OP>, half_hi(word_of(scale[f], r)));
+}
+template <class T, int D, int GR>
+__device__ __forceinline__ f32x4q logits_of(const uint4 (&k)[D / 32], const uint4 (&scale)[D / GR], const float (&rest)[D / GR][4],
                                             const uint4 (&q)[D / 32][Q4Type<T>::PIECES], const float (&sums)[D / GR]) {
   constexpr int OP = Q4Type<T>::OP, PIECES = Q4Type<T>::PIECES;
   f32x4q x = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
   for (int f = 0; f < D / GR; ++f) {
-    const float c0 = -kOffset<OP> * sums[f];
-    f32x4q acc = {c0, c0, c0, c0};
+    f32x4q acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int j = f * (GR / 32); j < (f + 1) * (GR / 32); ++j)
 #pragma unroll
       for (int c = 0; c < PIECES; ++c) acc = mfma_q4<OP>(k[j], q[j][c], acc);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const uint32_t s = word_of(scale[f], r);
-      x[r] = __builtin_fmaf(half_lo(s), acc[r], __builtin_fmaf(half_hi(s), sums[f], x[r]));
-    }
+    for (int r = 0; r < 4; ++r)
+      x[r] = __builtin_fmaf(half_lo(word_of(scale[f], r)), acc[r], __builtin_fmaf(rest[f][r], sums[f], x[r]));
   }
   return x;
 }
@@ -97,7 +120,7 @@ __device__ __forceinline__ f32x4q logits_of(const uint4 (&k)[D / 32], const uint
 // Four results of neighbouring channels.
 template <class T>
 __device__ __forceinline__ void store_out(const Kv4Attend& a, int D, int b, int h, int row, int d, const f32x4q& v) {
-  const int s = row / a.G, i = row % a.G;
+  const int s = row_token(a, row), i = row - s * a.G;
   typename T::T* dst = reinterpret_cast<typename T::T*>(a.out) + (((int64_t)b * a.S + s) * a.c.H * a.G + h * a.G + i) * D + d;
   if constexpr (T::VEC == 4) {
     *reinterpret_cast<float4*>(dst) = make_float4(v[0], v[1], v[2], v[3]);
@@ -115,12 +138,12 @@ __device__ __forceinline__ void store_out(const Kv4Attend& a, int D, int b, int 
 }
 
 // Slots that a row sees: those before the limit.
-__device__ __forceinline__ int row_limit(const Kv4Attend& a, int len, int row) { return min(len, len - a.S + row / a.G + 1); }
+__device__ __forceinline__ int row_limit(const Kv4Attend& a, int len, int row) { return min(len, len - a.S + row_token(a, row) + 1); }
 // log2 of a row's sum over slots; +infinity where it sees none, so that every probability against it is 0.
 __device__ __forceinline__ float log_sum(float m, float l) { return l == 0.0f ? INFINITY : m + __builtin_amdgcn_logf(l); }
 __device__ __forceinline__ void store_lse(const Kv4Attend& a, int b, int h, int row, float z) {
   if (!a.lse) return;
-  const int s = row / a.G, i = row % a.G;
+  const int s = row_token(a, row), i = row - s * a.G;
   // natural logarithm; -infinity for a row that sees nothing
   a.lse[((int64_t)b * a.S + s) * a.c.H * a.G + h * a.G + i] = z == INFINITY ? -INFINITY : z * 0.69314718055994531f;
 }
@@ -224,13 +247,13 @@ __device__ __forceinline__ void join_pieces(const float* m, const float* l, size
 }
 
 // Waves of a SIMD that the registers are to leave room for.
-template <class T, int D, int GR, int NR> constexpr int kAttendWaves = NR > 1 ? 1 : D / GR == 4 || T::VEC == 4 ? 2 : 3;
+template <class T, int D, int GR> constexpr int kAttendWaves = D / GR == 4 || T::VEC == 4 ? 2 : 3;
 
-template <class T, int D, int GR, int NR, bool LOGITS>
-__global__ __launch_bounds__(256, (kAttendWaves<T, D, GR, NR>)) void gemm_q4_attend_kernel(Kv4Attend a) {
+template <class T, int D, int GR, bool LOGITS>
+__global__ __launch_bounds__(256, (kAttendWaves<T, D, GR>)) void gemm_q4_attend_kernel(Kv4Attend a) {
   constexpr int OP = Q4Type<T>::OP, OPV = AttendType<T>::OPV, PIECES = Q4Type<T>::PIECES, P = AttendType<T>::P;
   constexpr int NG = D / GR, JK = D / 32, JV = D / 16;
-  __shared__ float ml[2][4][NR][16];
+  __shared__ float ml[2][4][16];
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -242,14 +265,13 @@ __global__ __launch_bounds__(256, (kAttendWaves<T, D, GR, NR>)) void gemm_q4_att
   if (b >= a.c.B) return;
   const int h = ((int)blockIdx.x - first) % a.c.H, split = ((int)blockIdx.x - first) / a.c.H, bh = b * a.c.H + h;
   const bool joined = a.token_waves == 4;
-  const int tile0 = (joined ? (int)blockIdx.y : (int)blockIdx.y * 4 + wave) * NR;
-  const int row0 = tile0 * 16;
+  const int row0 = (joined ? (int)blockIdx.y : (int)blockIdx.y * 4 + wave) * 16, row = min(row0 + n, a.R - 1);   // rows past the last repeat it
   if (!joined && row0 >= a.R) return;   // no barrier follows
   const int len = min(max(a.lens[b], 0), a.max_len);
   const int pieces = a.wanted == 0 ? 1 : shares.count((len + 31) / 32);
   if (a.wanted && (int)blockIdx.x == first && blockIdx.y == 0 && threadIdx.x == 0) a.place[b] = make_int2(first, pieces);   // for the join
 
-  const int low_limit = row_limit(a, len, row0), high_limit = row_limit(a, len, min(row0 + 16 * NR, a.R) - 1);
+  const int low_limit = row_limit(a, len, row0), high_limit = row_limit(a, len, min(row0 + 16, a.R) - 1);
 
   // where the lane's share of a step lies
   const uint32_t* kp = a.c.k + ((size_t)bh * a.c.cap + n) * (D / 8) + g * (D / 32);
@@ -287,215 +309,182 @@ __global__ __launch_bounds__(256, (kAttendWaves<T, D, GR, NR>)) void gemm_q4_att
     load_keys(step0);
     load_values(step0);
   }
-  uint4 q[NR][JK][PIECES];
-  float sums[NR][NG];
-  int limit[NR];
-#pragma unroll
-  for (int u = 0; u < NR; ++u) {
-    const int row = min(row0 + 16 * u + n, a.R - 1);
-    load_rows<T, D, GR>(a, b, h, row, q[u], sums[u]);
-    limit[u] = row_limit(a, len, row);
+  uint4 q[JK][PIECES];
+  float sums[NG];
+  {
+    RawRow<T, D> raw;
+    load_raw<T, D>(a, b, h, row, raw);
+    make_rows<T, D, GR>(raw, q, sums);
   }
+  const int limit = row_limit(a, len, row);
 
-  f32x4q o[NR][JV], one[NR][NG];
-  float m[NR], l[NR], low[NR][NG];
+  f32x4q o[JV], one[NG];
+  float m = -INFINITY, l = 0.0f, low[NG];
 #pragma unroll
-  for (int u = 0; u < NR; ++u) {
-    m[u] = -INFINITY;
-    l[u] = 0.0f;
+  for (int f = 0; f < NG; ++f) one[f] = f32x4q{0.0f, 0.0f, 0.0f, 0.0f}, low[f] = 0.0f;
 #pragma unroll
-    for (int f = 0; f < NG; ++f) one[u][f] = f32x4q{0.0f, 0.0f, 0.0f, 0.0f}, low[u][f] = 0.0f;
-#pragma unroll
-    for (int j = 0; j < JV; ++j) o[u][j] = f32x4q{0.0f, 0.0f, 0.0f, 0.0f};
-  }
+  for (int j = 0; j < JV; ++j) o[j] = f32x4q{0.0f, 0.0f, 0.0f, 0.0f};
 
   for (int step = step0; step < steps; step += stride) {
     const int t0 = step * 32, after = min(step + stride, steps - 1);
     const bool partial = t0 + 32 > low_limit;
-    float xs[NR][8];
+    float x[8];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       uint4 kop[JK];
 #pragma unroll
       for (int j = 0; j < JK; ++j) kop[j] = q4_operand<OP>(word_of(k[i], j), mk);
+      float rest[NG][4];
+      rests_of<T, D, GR>(ks[i], rest);
+      const f32x4q y = logits_of<T, D, GR>(kop, ks[i], rest, q, sums);
 #pragma unroll
-      for (int u = 0; u < NR; ++u) {
-        const f32x4q y = logits_of<T, D, GR>(kop, ks[i], q[u], sums[u]);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) xs[u][4 * i + r] = y[r];
-      }
+      for (int r = 0; r < 4; ++r) x[4 * i + r] = y[r];
     }
     load_keys(after);
-    uint4 piece[NR][NG][P];
+    if (partial) {
 #pragma unroll
-    for (int u = NR - 1; u >= 0; --u) {   // later rows see more
-      float (&x)[8] = xs[u];
-      if (partial) {
+      for (int i = 0; i < 8; ++i)
+        if (t0 + 16 * (i / 4) + 4 * g + i % 4 >= limit) x[i] = -INFINITY;
+      // no probability of a slot that the row does not see meets its step and lowest value, which may be anything
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (t0 + 16 * (i / 4) + 4 * g + i % 4 >= limit[u]) x[i] = -INFINITY;
-        // no probability of a slot that the row does not see meets its step and lowest value, which may be anything
+      for (int i = 0; i < 2; ++i) {
+        const int see = limit - (t0 + 16 * i + 4 * g);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int see = limit[u] - (t0 + 16 * i + 4 * g);
-#pragma unroll
-          for (int f = 0; f < NG; ++f) {
-            vs[i][f].x = see > 0 ? vs[i][f].x : 0;
-            vs[i][f].y = see > 1 ? vs[i][f].y : 0;
-            vs[i][f].z = see > 2 ? vs[i][f].z : 0;
-            vs[i][f].w = see > 3 ? vs[i][f].w : 0;
-          }
-        }
-      }
-      if constexpr (LOGITS) {   // one tile of rows
-        if (n < a.R) {
-          float4* dst = reinterpret_cast<float4*>(a.logits + ((size_t)bh * a.R + n) * ((a.max_len + 31) / 32 * 32) + t0 + 4 * g);
-          dst[0] = make_float4(x[0] * a.scale, x[1] * a.scale, x[2] * a.scale, x[3] * a.scale);
-          dst[4] = make_float4(x[4] * a.scale, x[5] * a.scale, x[6] * a.scale, x[7] * a.scale);
-        }
-      }
-      float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))) * a.scale;
-      if (__any(top > m[u] + 8.0f)) {
-        top = fmaxf(top, __shfl_xor(top, 16, kWave));
-        top = fmaxf(top, __shfl_xor(top, 32, kWave));
-        top = fmaxf(top, m[u]);
-        const float f = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[u] - top);
-        m[u] = top;
-        l[u] *= f;
-#pragma unroll
-        for (int e = 0; e < NG; ++e) {
-          low[u][e] *= f;
-          one[u][e] *= f;
-        }
-#pragma unroll
-        for (int j = 0; j < JV; ++j) o[u][j] *= f;
-      }
-      const float base = m[u] == -INFINITY ? 0.0f : m[u];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale, -base));
-        l[u] += x[i];
-      }
-#pragma unroll
-      for (int f = 0; f < NG; ++f) {
-        uint32_t p[4][P];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t s0 = word_of(vs[i / 2][f], 2 * (i % 2)), s1 = word_of(vs[i / 2][f], 2 * (i % 2) + 1);
-          low[u][f] = __builtin_fmaf(half_hi(s0), x[2 * i], low[u][f]);
-          low[u][f] = __builtin_fmaf(half_hi(s1), x[2 * i + 1], low[u][f]);
-          split_bf16<P>(half_lo(s0) * x[2 * i], half_lo(s1) * x[2 * i + 1], p[i]);
-        }
-#pragma unroll
-        for (int c = 0; c < P; ++c) {
-          piece[u][f][c] = make_uint4(p[0][c], p[1][c], p[2][c], p[3][c]);
-          if constexpr (OPV != kOpExact) one[u][f] = mfma_q4<OPV>(ones, piece[u][f][c], one[u][f]);
+        for (int f = 0; f < NG; ++f) {
+          vs[i][f].x = see > 0 ? vs[i][f].x : 0;
+          vs[i][f].y = see > 1 ? vs[i][f].y : 0;
+          vs[i][f].z = see > 2 ? vs[i][f].z : 0;
+          vs[i][f].w = see > 3 ? vs[i][f].w : 0;
         }
       }
     }
-    // channels 16 j + n of eight slots: bits 4 i of the words of half f of each pair of slots
+    if constexpr (LOGITS) {   // one tile of rows
+      if (n < a.R) {
+        float4* dst = reinterpret_cast<float4*>(a.logits + ((size_t)bh * a.R + n) * ((a.max_len + 31) / 32 * 32) + t0 + 4 * g);
+        dst[0] = make_float4(x[0] * a.scale, x[1] * a.scale, x[2] * a.scale, x[3] * a.scale);
+        dst[4] = make_float4(x[4] * a.scale, x[5] * a.scale, x[6] * a.scale, x[7] * a.scale);
+      }
+    }
+    float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))) * a.scale;
+    if (__any(top > m + 8.0f)) {
+      top = fmaxf(top, __shfl_xor(top, 16, kWave));
+      top = fmaxf(top, __shfl_xor(top, 32, kWave));
+      top = fmaxf(top, m);
+      const float f = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - top);
+      m = top;
+      l *= f;
 #pragma unroll
-    for (int f = 0; f < D / 64; ++f) {
-      uint4 vop[4];
-      uint32_t w[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = word_of(v[i / 2], (D / 64) * (i % 2) + f);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint32_t e[4];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          if constexpr (OPV == kOpBF16) {
-            e[c] = ((w[c] >> (4 * i)) & mv.mask) | mv.magic;
-          } else {
-            const uint32_t two = (w[c] >> (4 * i)) & 0x000f000fu;
-            e[c] = __builtin_amdgcn_perm(f2u((float)(two >> 16)), f2u((float)(two & 0xffffu)), 0x07060302u);
-          }
-        }
-        vop[i] = make_uint4(e[0], e[1], e[2], e[3]);
+      for (int e = 0; e < NG; ++e) {
+        low[e] *= f;
+        one[e] *= f;
       }
 #pragma unroll
-      for (int u = 0; u < NR; ++u)
+      for (int j = 0; j < JV; ++j) o[j] *= f;
+    }
+    const float base = m == -INFINITY ? 0.0f : m;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 8; ++i) {
+      x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale, -base));
+      l += x[i];
+    }
+    // group by group: the probabilities times the group's steps, in pieces, and their products with the group's channels
 #pragma unroll
-          for (int c = 0; c < P; ++c) o[u][4 * f + i] = mfma_q4<OPV>(vop[i], piece[u][(4 * f + i) * 16 / GR][c], o[u][4 * f + i]);
+    for (int e = 0; e < NG; ++e) {
+      uint4 piece[P];
+      uint32_t p[4][P];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t s0 = word_of(vs[i / 2][e], 2 * (i % 2)), s1 = word_of(vs[i / 2][e], 2 * (i % 2) + 1);
+        low[e] = __builtin_fmaf(half_hi(s0), x[2 * i], low[e]);
+        low[e] = __builtin_fmaf(half_hi(s1), x[2 * i + 1], low[e]);
+        split_bf16<P>(half_lo(s0) * x[2 * i], half_lo(s1) * x[2 * i + 1], p[i]);
+      }
+#pragma unroll
+      for (int c = 0; c < P; ++c) {
+        piece[c] = make_uint4(p[0][c], p[1][c], p[2][c], p[3][c]);
+        if constexpr (OPV != kOpExact) one[e] = mfma_q4<OPV>(ones, piece[c], one[e]);
+      }
+      // channels 16 j + n of eight slots: bits 4 (j % 4) of the words of half j / 4 of each pair of slots
+#pragma unroll
+      for (int j = e * (GR / 16); j < (e + 1) * (GR / 16); ++j) {
+        uint32_t b[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const uint32_t w = word_of(v[c / 2], (D / 64) * (c % 2) + j / 4);
+          if constexpr (OPV == kOpBF16) {
+            b[c] = ((w >> (4 * (j % 4))) & mv.mask) | mv.magic;
+          } else {
+            const uint32_t two = (w >> (4 * (j % 4))) & 0x000f000fu;
+            b[c] = __builtin_amdgcn_perm(f2u((float)(two >> 16)), f2u((float)(two & 0xffffu)), 0x07060302u);
+          }
+        }
+        const uint4 vop = make_uint4(b[0], b[1], b[2], b[3]);
+#pragma unroll
+        for (int c = 0; c < P; ++c) o[j] = mfma_q4<OPV>(vop, piece[c], o[j]);
+      }
     }
     load_values(after);
   }
 
   // sums over the lanes of a row, and the constants that entered with the codes
+  l += __shfl_xor(l, 16, kWave);
+  l += __shfl_xor(l, 32, kWave);
 #pragma unroll
-  for (int u = 0; u < NR; ++u) {
-    l[u] += __shfl_xor(l[u], 16, kWave);
-    l[u] += __shfl_xor(l[u], 32, kWave);
-#pragma unroll
-    for (int f = 0; f < NG; ++f) {
-      low[u][f] += __shfl_xor(low[u][f], 16, kWave);
-      low[u][f] += __shfl_xor(low[u][f], 32, kWave);
-      if constexpr (OPV != kOpExact) low[u][f] = __builtin_fmaf(-kOffset<OPV>, one[u][f][0], low[u][f]);
-    }
-#pragma unroll
-    for (int j = 0; j < JV; ++j) o[u][j] += low[u][j * 16 / GR];
+  for (int f = 0; f < NG; ++f) {
+    low[f] += __shfl_xor(low[f], 16, kWave);
+    low[f] += __shfl_xor(low[f], 32, kWave);
+    if constexpr (OPV != kOpExact) low[f] = __builtin_fmaf(-kOffset<OPV>, one[f][0], low[f]);
   }
+#pragma unroll
+  for (int j = 0; j < JV; ++j) o[j] += low[j * 16 / GR];
   const size_t part = (size_t)blockIdx.x * a.row_tiles * 16;
   if (!joined) {
+    if (row0 + n >= a.R) return;
+    if (pieces > 1) {
+      if (g == 0) a.m[part + row] = m, a.l[part + row] = l;
 #pragma unroll
-    for (int u = 0; u < NR; ++u) {
-      const int row = row0 + 16 * u + n;
-      if (row >= a.R) continue;
-      if (pieces > 1) {
-        if (g == 0) a.m[part + row] = m[u], a.l[part + row] = l[u];
+      for (int j = 0; j < JV; ++j)
+        *reinterpret_cast<float4*>(a.o + (part + row) * D + 16 * j + 4 * g) = make_float4(o[j][0], o[j][1], o[j][2], o[j][3]);
+    } else {
+      const float inv = l == 0.0f ? 0.0f : 1.0f / l, z = log_sum(m, l);
 #pragma unroll
-        for (int j = 0; j < JV; ++j)
-          *reinterpret_cast<float4*>(a.o + (part + row) * D + 16 * j + 4 * g) = make_float4(o[u][j][0], o[u][j][1], o[u][j][2], o[u][j][3]);
-      } else {
-        const float inv = l[u] == 0.0f ? 0.0f : 1.0f / l[u], z = log_sum(m[u], l[u]);
-#pragma unroll
-        for (int j = 0; j < JV; ++j) store_out<T>(a, D, b, h, row, 16 * j + 4 * g, o[u][j] * inv);
-        if (g == 0) {
-          store_lse(a, b, h, row, z);
-          if (a.weights) a.z[(size_t)bh * a.R + row] = z;
-        }
+      for (int j = 0; j < JV; ++j) store_out<T>(a, D, b, h, row, 16 * j + 4 * g, o[j] * inv);
+      if (g == 0) {
+        store_lse(a, b, h, row, z);
+        if (a.weights) a.z[(size_t)bh * a.R + row] = z;
       }
     }
     return;
   }
 
   // the waves' sums
-  float4* shared = reinterpret_cast<float4*>(smem);   // [wave][u][j][lane]
-  if (g == 0)
-#pragma unroll
-    for (int u = 0; u < NR; ++u) ml[0][wave][u][n] = m[u], ml[1][wave][u][n] = l[u];
+  float4* shared = reinterpret_cast<float4*>(smem);   // [wave][j][lane]
+  if (g == 0) ml[0][wave][n] = m, ml[1][wave][n] = l;
   __syncthreads();
-#pragma unroll
-  for (int u = 0; u < NR; ++u) {
+  if (row0 + n < a.R) {
     float top = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[0][w][u][n]);
-    const float f = m[u] == -INFINITY ? (l[u] != l[u] ? l[u] : 0.0f) : __builtin_amdgcn_exp2f(m[u] - top);   // a row of NaNs stays one
-    if (row0 + 16 * u + n < a.R)
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[0][w][n]);
+    const float f = m == -INFINITY ? (l != l ? l : 0.0f) : __builtin_amdgcn_exp2f(m - top);   // a row of NaNs stays one
 #pragma unroll
-      for (int j = 0; j < JV; ++j)
-        shared[((wave * NR + u) * JV + j) * 64 + lane] = make_float4(o[u][j][0] * f, o[u][j][1] * f, o[u][j][2] * f, o[u][j][3] * f);
+    for (int j = 0; j < JV; ++j)
+      shared[(wave * JV + j) * 64 + lane] = make_float4(o[j][0] * f, o[j][1] * f, o[j][2] * f, o[j][3] * f);
   }
   __syncthreads();
-  const int rows = min(NR * 16, a.R - row0);
-  for (int i = threadIdx.x; i < rows * (D / 4); i += 256) {
-    const int r = i / (D / 4), d = i % (D / 4) * 4, u = r / 16, col = r % 16, row = row0 + r;
-    const int at = (u * JV + d / 16) * 64 + d % 16 / 4 * 16 + col;
+  for (int i = threadIdx.x; i < min(16, a.R - row0) * (D / 4); i += 256) {
+    const int col = i / (D / 4), d = i % (D / 4) * 4, row = row0 + col, at = d / 16 * 64 + d % 16 / 4 * 16 + col;
     float top = -INFINITY, total = 0.0f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[0][w][u][col]);
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[0][w][col]);
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      const float mw = ml[0][w][u][col], lw = ml[1][w][u][col];
+      const float mw = ml[0][w][col], lw = ml[1][w][col];
       total += mw == -INFINITY ? lw : lw * __builtin_amdgcn_exp2f(mw - top);   // no maximum: 0, or NaN
     }
     f32x4q v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      const float4 s = shared[w * NR * JV * 64 + at];
+      const float4 s = shared[w * JV * 64 + at];
       v[0] += s.x; v[1] += s.y; v[2] += s.z; v[3] += s.w;
     }
     if (pieces > 1) {
@@ -613,21 +602,32 @@ __global__ __launch_bounds__(256) void gemm_q4_weights_kernel(Kv4Attend a) {
 #pragma unroll
     for (int f = 0; f < NG; ++f) ks[i][f] = ld16(ksp + (size_t)f * a.c.cap + 16 * i);
   }
+  float rest[2][NG][4];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) rests_of<T, D, GR>(ks[i], rest[i]);
   float w[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
   const int first = max(0, t0 - (len - a.S)) * a.G / 16;   // rows of earlier tiles see none of these slots
-  for (int tile = first; tile < a.row_tiles && tile * 16 < a.R; ++tile) {
+  RawRow<T, D> raw;
+  float z;
+  auto request = [&](int tile) {
     const int row = min(tile * 16 + n, a.R - 1);
+    load_raw<T, D>(a, b, h, row, raw);
+    z = a.z[(size_t)bh * a.R + row];
+  };
+  if (first < a.row_tiles) request(first);
+  for (int tile = first; tile < a.row_tiles; ++tile) {
     uint4 q[JK][PIECES];
     float sums[NG];
-    load_rows<T, D, GR>(a, b, h, row, q, sums);
-    const float z = tile * 16 + n < a.R ? a.z[(size_t)bh * a.R + row] : INFINITY;
-    const int limit = row_limit(a, len, row);
+    make_rows<T, D, GR>(raw, q, sums);
+    const float zr = tile * 16 + n < a.R ? z : INFINITY;
+    const int limit = row_limit(a, len, min(tile * 16 + n, a.R - 1));
+    request(min(tile + 1, a.row_tiles - 1));   // ahead of its use
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const f32x4q x = logits_of<T, D, GR>(kop[i], ks[i], q, sums);
+      const f32x4q x = logits_of<T, D, GR>(kop[i], ks[i], rest[i], q, sums);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.scale, -z));
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], a.scale, -zr));
         w[4 * i + r] += t0 + 16 * i + 4 * g + r < limit ? p : 0.0f;
       }
     }
@@ -645,12 +645,12 @@ __global__ __launch_bounds__(256) void gemm_q4_weights_kernel(Kv4Attend a) {
     }
 }
 
-template <class T, int D, int GR, int NR, bool LOGITS>
+template <class T, int D, int GR, bool LOGITS>
 int launch_attend(const Kv4Attend& a, hipStream_t s) {
-  const int tiles = (a.R + 15) / 16, per = a.token_waves == 4 ? NR : 4 * NR;
+  const int tiles = (a.R + 15) / 16, per = a.token_waves == 4 ? 1 : 4;
   const dim3 grid(a.blocks, (tiles + per - 1) / per);
-  const size_t lds = a.token_waves == 4 ? (size_t)4 * NR * D * 64 : 0;
-  hipLaunchKernelGGL((gemm_q4_attend_kernel<T, D, GR, NR, LOGITS>), grid, dim3(256), lds, s, a);
+  const size_t lds = a.token_waves == 4 ? (size_t)4 * D * 64 : 0;
+  hipLaunchKernelGGL((gemm_q4_attend_kernel<T, D, GR, LOGITS>), grid, dim3(256), lds, s, a);
   CI_HIP_CHECK_LAUNCH();
   if (a.wanted || a.weights == 1) {
     constexpr int ROWS = 64 / (D / 4);
@@ -667,8 +667,7 @@ int launch_attend(const Kv4Attend& a, hipStream_t s) {
 
 template <class T, int D, int GR>
 int launch_attend_rows(const Kv4Attend& a, hipStream_t s) {
-  if (a.weights == 1) return launch_attend<T, D, GR, 1, true>(a, s);
-  return a.NR == 2 ? launch_attend<T, D, GR, 2, false>(a, s) : launch_attend<T, D, GR, 1, false>(a, s);
+  return a.weights == 1 ? launch_attend<T, D, GR, true>(a, s) : launch_attend<T, D, GR, false>(a, s);
 }
 
 }  // namespace

@@ -95,7 +95,8 @@ def test_cache_calls_refuse_their_arguments(lib):
     bad_stride = (ctypes.c_int64 * 3)(-1, 512, 128)
     cases = {
         "append": [(dict(dt=9), "DTYPE"), (dict(k=None), "INVALID"), (dict(v=None), "INVALID"), (dict(lens=None), "INVALID"),
-                   (dict(S=0), "INVALID"), (dict(st=None), "INVALID"), (dict(st=bad_stride), "LAYOUT"), (dict(k=F + 1), "LAYOUT"),
+                   (dict(S=0), "INVALID"), (dict(S=(1 << 19) + 1), "INVALID"),
+                   (dict(st=None), "INVALID"), (dict(st=bad_stride), "LAYOUT"), (dict(k=F + 1), "LAYOUT"),
                    (dict(start=F + 2), "LAYOUT"), (dict(nxt=F + 1), "LAYOUT"), (dict(lens=F + 1), "LAYOUT")],
         "read": [(dict(dt=-1), "DTYPE"), (dict(lens=None), "INVALID"), (dict(first=-1), "INVALID"), (dict(count=0), "INVALID"),
                  (dict(first=60, count=5), "INVALID"), (dict(count=65), "INVALID"), (dict(k=None), "INVALID"),
