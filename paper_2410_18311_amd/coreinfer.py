@@ -786,12 +786,10 @@ def kv4_read(cache: Kv4Cache, lens: torch.Tensor, first: int, count: int, dtype:
              k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None):
     """coreinfer_kv4_read: the values of slots first .. first + count - 1, (k, v) [B, H, count, D]; zeros from lens on."""
     shape = (cache.B, cache.H, count, cache.D)
-    if k is None:
-        k = torch.empty(shape, dtype=dtype, device=cache.k.device)
-    if v is None:
-        v = torch.empty(shape, dtype=dtype, device=cache.k.device)
     for t in (k, v):
-        assert t.shape == shape and t.dtype == dtype and t.is_contiguous()
+        assert t is None or (t.shape == shape and t.dtype == dtype and t.is_contiguous())
+    k = torch.empty(shape, dtype=dtype, device=lens.device) if k is None else k
+    v = torch.empty(shape, dtype=dtype, device=lens.device) if v is None else v
     _check_lens(cache, lens)
     status = _kv4_read_call(cache.ptr, lens.data_ptr(), first, count, k.data_ptr(), v.data_ptr(), DTYPE_CODE[dtype], _stream(k))
     if status != CI_OK:

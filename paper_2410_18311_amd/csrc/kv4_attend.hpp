@@ -40,24 +40,25 @@ template <class T, int D>
 struct RawRow {
   uint4 raw[D / 32][8 / T::VEC];
 };
-template <class T, int D>
-__device__ __forceinline__ void load_raw(const Kv4Attend& a, int b, int h, int row, RawRow<T, D>& r) {
-  const int g = (threadIdx.x & 63) >> 4, s = row_token(a, row), i = row - s * a.G;
-  const typename T::T* src = reinterpret_cast<const typename T::T*>(a.q) + b * a.q_b + s * a.q_s + (int64_t)(h * a.G + i) * a.q_h + 8 * g;
+template <class T>
+__device__ __forceinline__ void load_channels(const Kv4Attend& a, int b, int h, int row, int channel, uint4 (&to)[8 / T::VEC]) {
+  const int s = row_token(a, row), i = row - s * a.G;
+  const typename T::T* src = reinterpret_cast<const typename T::T*>(a.q) + b * a.q_b + s * a.q_s + (int64_t)(h * a.G + i) * a.q_h + channel;
   if (a.q_vectors) {
 #pragma unroll
-    for (int j = 0; j < D / 32; ++j)
-#pragma unroll
-      for (int e = 0; e < 8 / T::VEC; ++e) r.raw[j][e] = ld16(src + 32 * j + e * T::VEC);
+    for (int e = 0; e < 8 / T::VEC; ++e) to[e] = ld16(src + e * T::VEC);
   } else {
+    typename T::T x[8];
 #pragma unroll
-    for (int j = 0; j < D / 32; ++j) {
-      typename T::T x[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = src[32 * j + e];
-      __builtin_memcpy(r.raw[j], x, sizeof(x));
-    }
+    for (int e = 0; e < 8; ++e) x[e] = src[e];
+    __builtin_memcpy(to, x, sizeof(x));
   }
+}
+template <class T, int D>
+__device__ __forceinline__ void load_raw(const Kv4Attend& a, int b, int h, int row, RawRow<T, D>& r) {
+  const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+  for (int j = 0; j < D / 32; ++j) load_channels<T>(a, b, h, row, 32 * j + 8 * g, r.raw[j]);
 }
 // The same as operands, and the sums of the row's channels by group.
 template <class T, int D, int GR>
@@ -580,19 +581,24 @@ __global__ __launch_bounds__(64) void kv4_join_kernel(Kv4Attend a, int join_bloc
 }
 
 // Weights of many rows: the logits are computed again, 32 slots a wave against all rows that see them, and every slot's sum stays in its
-// lane until the end, so there is no order to depend on and nothing of S x T is stored.
+// lane until the end, so there is no order to depend on and nothing of S x T is stored.  The rows go through the LDS, each wave fetching
+// a quarter of a tile of 16 for all four: every wave fetching its own is bound by the L2 (512 rows, 2048 slots, 32 heads: 36 us; of 16 slots
+// a wave 64).
 template <class T, int D, int GR>
 __global__ __launch_bounds__(256) void gemm_q4_weights_kernel(Kv4Attend a) {
-  constexpr int OP = Q4Type<T>::OP, PIECES = Q4Type<T>::PIECES, NG = D / GR, JK = D / 32;
+  constexpr int OP = Q4Type<T>::OP, PIECES = Q4Type<T>::PIECES, NG = D / GR, JK = D / 32, V = 8 / T::VEC;
+  __shared__ uint4 tile_of_q[2][JK][V][64];
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int bh = blockIdx.x, b = bh / a.c.H, h = bh % a.c.H;
+  const int heads = a.c.B * a.c.H, bh = blockIdx.x % heads, b = bh / a.c.H, h = bh % a.c.H;   // heads fastest: a head's rows stay in one L2
   const int len = min(max(a.lens[b], 0), a.max_len);
-  const int t0 = ((int)blockIdx.y * 4 + wave) * 32;
-  if (t0 >= len) return;
+  const int t_block = (int)(blockIdx.x / heads) * 128, t0 = t_block + wave * 32;
+  if (t_block >= len) return;   // the whole workgroup; t0 + 32 may pass len, but not a multiple of 32 that holds it, so not the capacity
+  const bool idle = t0 >= len;
   const Q4Magic mk = q4_magic<OP>();
-  const uint32_t* kp = a.c.k + ((size_t)bh * a.c.cap + t0 + n) * (D / 8) + g * (D / 32);
-  const uint32_t* ksp = a.c.ks + (size_t)bh * NG * a.c.cap + t0 + 4 * g;
+  const int from = idle ? t_block : t0;
+  const uint32_t* kp = a.c.k + ((size_t)bh * a.c.cap + from + n) * (D / 8) + g * (D / 32);
+  const uint32_t* ksp = a.c.ks + (size_t)bh * NG * a.c.cap + from + 4 * g;
   uint4 kop[2][JK], ks[2][NG];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -606,22 +612,32 @@ __global__ __launch_bounds__(256) void gemm_q4_weights_kernel(Kv4Attend a) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) rests_of<T, D, GR>(ks[i], rest[i]);
   float w[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-  const int first = max(0, t0 - (len - a.S)) * a.G / 16;   // rows of earlier tiles see none of these slots
-  RawRow<T, D> raw;
-  float z;
+  const int first = max(0, t_block - (len - a.S)) * a.G / 16;   // rows of earlier tiles see none of these slots
+  uint4 mine[V];
+  float z = 0.0f;
   auto request = [&](int tile) {
     const int row = min(tile * 16 + n, a.R - 1);
-    load_raw<T, D>(a, b, h, row, raw);
+    if (JK == 4 || wave < JK) load_channels<T>(a, b, h, row, 32 * wave + 8 * g, mine);
     z = a.z[(size_t)bh * a.R + row];
   };
   if (first < a.row_tiles) request(first);
   for (int tile = first; tile < a.row_tiles; ++tile) {
+    const int at = tile & 1;   // two places by turns: one barrier a tile
+    if (JK == 4 || wave < JK)
+#pragma unroll
+      for (int v = 0; v < V; ++v) tile_of_q[at][wave][v][lane] = mine[v];
+    const float zr = tile * 16 + n < a.R ? z : INFINITY;
+    __syncthreads();
+    request(min(tile + 1, a.row_tiles - 1));   // ahead of its use
+    RawRow<T, D> raw;
+#pragma unroll
+    for (int j = 0; j < JK; ++j)
+#pragma unroll
+      for (int v = 0; v < V; ++v) raw.raw[j][v] = tile_of_q[at][j][v][lane];
     uint4 q[JK][PIECES];
     float sums[NG];
     make_rows<T, D, GR>(raw, q, sums);
-    const float zr = tile * 16 + n < a.R ? z : INFINITY;
-    const int limit = row_limit(a, len, min(tile * 16 + n, a.R - 1));
-    request(min(tile + 1, a.row_tiles - 1));   // ahead of its use
+    const int limit = idle ? 0 : row_limit(a, len, min(tile * 16 + n, a.R - 1));
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const f32x4q x = logits_of<T, D, GR>(kop[i], ks[i], rest[i], q, sums);
@@ -659,7 +675,8 @@ int launch_attend(const Kv4Attend& a, hipStream_t s) {
     CI_HIP_CHECK_LAUNCH();
   }
   if (a.weights == 2) {
-    hipLaunchKernelGGL((gemm_q4_weights_kernel<T, D, GR>), dim3(a.c.B * a.c.H, (a.max_len + 127) / 128), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((gemm_q4_weights_kernel<T, D, GR>), dim3((uint32_t)(a.c.B * a.c.H) * ((a.max_len + 127) / 128)), dim3(256), 0,
+                       s, a);
     CI_HIP_CHECK_LAUNCH();
   }
   return CI_OK;
