@@ -90,6 +90,23 @@ __device__ __forceinline__ void make_rows(const RawRow<T, D>& r, uint4 (&q)[D / 
   }
 }
 
+// Channels 16 j + n of eight slots as an operand: bits 4 (j % 4) of the words of half j / 4 of each pair of slots.
+template <int OP, int D>
+__device__ __forceinline__ uint4 value_operand(const uint4 (&v)[2], int j, const Q4Magic& magic) {
+  uint32_t e[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const uint32_t w = word_of(v[c / 2], (D / 64) * (c % 2) + j / 4) >> (4 * (j % 4));
+    if constexpr (OP == kOpBF16) {
+      e[c] = (w & magic.mask) | magic.magic;
+    } else {
+      const uint32_t two = w & 0x000f000fu;
+      e[c] = __builtin_amdgcn_perm(f2u((float)(two >> 16)), f2u((float)(two & 0xffffu)), 0x07060302u);
+    }
+  }
+  return make_uint4(e[0], e[1], e[2], e[3]);
+}
+
 // Logits (without the scale) of 16 slots, four to a lane, and the rows of q.  rest: the lowest value less the codes' offset in steps.
 template <class T, int D, int GR>
 __device__ __forceinline__ void rests_of(const uint4 (&scale)[D / GR], float (&rest)[D / GR][4]) {
@@ -250,8 +267,14 @@ __device__ __forceinline__ void join_pieces(const float* m, const float* l, size
 // Waves of a SIMD that the registers are to leave room for.
 template <class T, int D, int GR> constexpr int kAttendWaves = D / GR == 4 || T::VEC == 4 ? 2 : 3;
 
-template <class T, int D, int GR, bool LOGITS>
+// How the four waves of a workgroup share the work: one tile of rows and different slots, their sums joined at the end (storing the logits for
+// the weights or not), or the same slots and different tiles; then the cache goes through the LDS as operands, each wave fetching and
+// unpacking a quarter of a step for all four.
+enum { kSlots, kSlotsAndLogits, kTiles };
+
+template <class T, int D, int GR, int SHARE>
 __global__ __launch_bounds__(256, (kAttendWaves<T, D, GR>)) void gemm_q4_attend_kernel(Kv4Attend a) {
+  constexpr bool LOGITS = SHARE == kSlotsAndLogits, JOINED = SHARE != kTiles;
   constexpr int OP = Q4Type<T>::OP, OPV = AttendType<T>::OPV, PIECES = Q4Type<T>::PIECES, P = AttendType<T>::P;
   constexpr int NG = D / GR, JK = D / 32, JV = D / 16;
   __shared__ float ml[2][4][16];
@@ -265,23 +288,24 @@ __global__ __launch_bounds__(256, (kAttendWaves<T, D, GR>)) void gemm_q4_attend_
   first = __builtin_amdgcn_readfirstlane(first);
   if (b >= a.c.B) return;
   const int h = ((int)blockIdx.x - first) % a.c.H, split = ((int)blockIdx.x - first) / a.c.H, bh = b * a.c.H + h;
-  const bool joined = a.token_waves == 4;
-  const int row0 = (joined ? (int)blockIdx.y : (int)blockIdx.y * 4 + wave) * 16, row = min(row0 + n, a.R - 1);   // rows past the last repeat it
-  if (!joined && row0 >= a.R) return;   // no barrier follows
+  const int row0 = (JOINED ? (int)blockIdx.y : (int)blockIdx.y * 4 + wave) * 16, row = min(row0 + n, a.R - 1);   // rows past the last repeat it
   const int len = min(max(a.lens[b], 0), a.max_len);
   const int pieces = a.wanted == 0 ? 1 : shares.count((len + 31) / 32);
   if (a.wanted && (int)blockIdx.x == first && blockIdx.y == 0 && threadIdx.x == 0) a.place[b] = make_int2(first, pieces);   // for the join
 
-  const int low_limit = row_limit(a, len, row0), high_limit = row_limit(a, len, min(row0 + 16, a.R) - 1);
+  // slots that all rows of the wave see, and those that any row of the waves that go together sees
+  const int low_limit = row_limit(a, len, min(row0, a.R - 1));
+  const int high_limit = row_limit(a, len, min(JOINED ? row0 + 16 : ((int)blockIdx.y + 1) * 64, a.R) - 1);
 
+  const Q4Magic mk = q4_magic<OP>(), mv = q4_magic<OPV>();
   // where the lane's share of a step lies
   const uint32_t* kp = a.c.k + ((size_t)bh * a.c.cap + n) * (D / 8) + g * (D / 32);
   const uint32_t* vp = a.c.v + ((size_t)bh * (a.c.cap / 4) + g) * (D / 2) + n * (D / 32);
   const uint32_t* ksp = a.c.ks + (size_t)bh * NG * a.c.cap + 4 * g;
   const uint32_t* vsp = a.c.vs + (size_t)bh * NG * a.c.cap + 4 * g;
-  // Keys and values are each requested again as soon as they have been used: the keys' way is behind the softmax and the values' product, and
-  // the other way round, with one set of registers.  (A ring in LDS with twice as much on its way was no faster.)
   uint4 k[2], ks[2][NG], v[2], vs[2][NG];
+  // Slots: keys and values are each requested again as soon as they have been used: the keys' way is behind the softmax and the values' product,
+  // and the other way round, with one set of registers.  (A ring in LDS with twice as much on its way was no faster.)
   auto load_keys = [&](int step) {
     const int t = step * 32;   // t + 32 <= cap, which is whole steps
 #pragma unroll
@@ -300,15 +324,52 @@ __global__ __launch_bounds__(256, (kAttendWaves<T, D, GR>)) void gemm_q4_attend_
       for (int f = 0; f < NG; ++f) vs[i][f] = ld16(vsp + (size_t)f * a.c.cap + t + 16 * i);
     }
   };
+  // Tiles: waves 0 and 1 fetch 16 slots' keys each, 2 and 3 half of the values' channels each, and 16 NG lanes of wave 0 all scales.
+  uint4 raw_codes[2], scales;
+  constexpr int OPERANDS = 2 * JK + JV;
+  uint4 (*operands)[OPERANDS][64] = reinterpret_cast<uint4 (*)[OPERANDS][64]>(smem);   // [2 places][keys of two tiles, values]
+  uint4 (*scales_of)[2][2][NG][4] = reinterpret_cast<uint4 (*)[2][2][NG][4]>(smem + 2 * OPERANDS * 1024);
+  auto fetch = [&](int step) {
+    const int t = step * 32;
+    if (wave < 2) {
+      raw_codes[0] = ld_row<D>(kp + (size_t)(t + 16 * wave) * (D / 8));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) raw_codes[i] = ld_row<D>(vp + (size_t)(t / 4 + 4 * i) * (D / 2));
+    }
+    if (threadIdx.x < 16 * NG) {
+      const int which = threadIdx.x / (8 * NG), i = threadIdx.x / (4 * NG) % 2, f = threadIdx.x / 4 % NG, quad = threadIdx.x % 4;
+      scales = ld16((which ? a.c.vs : a.c.ks) + ((size_t)bh * NG + f) * a.c.cap + t + 16 * i + 4 * quad);
+    }
+  };
+  auto exchange = [&](int place) {
+    if (wave < 2) {
+#pragma unroll
+      for (int j = 0; j < JK; ++j) operands[place][wave * JK + j][lane] = q4_operand<OP>(word_of(raw_codes[0], j), mk);
+    } else {
+#pragma unroll
+      for (int j = 0; j < JV; ++j)
+        if (j / (JV / 2) == wave - 2) operands[place][2 * JK + j][lane] = value_operand<OPV, D>(raw_codes, j, mv);
+    }
+    if (threadIdx.x < 16 * NG) (&scales_of[place][0][0][0][0])[threadIdx.x] = scales;
+    __syncthreads();   // two places by turns: one barrier a step
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int f = 0; f < NG; ++f) ks[i][f] = scales_of[place][0][i][f][g], vs[i][f] = scales_of[place][1][i][f][g];
+  };
   const int begin = split ? split * shares.chunk : 0;   // one piece: the chunk may be anything
-  const int step0 = begin + (joined ? wave : 0), stride = joined ? 4 : 1;
+  const int step0 = begin + (JOINED ? wave : 0), stride = JOINED ? 4 : 1;
   const int end = pieces == 1 ? 1 << 30 : begin + shares.chunk, steps = min(end, (max(high_limit, 0) + 31) / 32);
-  const Q4Magic mk = q4_magic<OP>(), mv = q4_magic<OPV>();
   const uint4 ones = make_uint4(kOnes<OPV>, kOnes<OPV>, kOnes<OPV>, kOnes<OPV>);
 
   if (step0 < steps) {
-    load_keys(step0);
-    load_values(step0);
+    if constexpr (JOINED) {
+      load_keys(step0);
+      load_values(step0);
+    } else {
+      fetch(step0);
+    }
   }
   uint4 q[JK][PIECES];
   float sums[NG];
@@ -329,19 +390,23 @@ __global__ __launch_bounds__(256, (kAttendWaves<T, D, GR>)) void gemm_q4_attend_
   for (int step = step0; step < steps; step += stride) {
     const int t0 = step * 32, after = min(step + stride, steps - 1);
     const bool partial = t0 + 32 > low_limit;
+    if constexpr (!JOINED) {
+      exchange(step & 1);
+      fetch(after);
+    }
     float x[8];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       uint4 kop[JK];
 #pragma unroll
-      for (int j = 0; j < JK; ++j) kop[j] = q4_operand<OP>(word_of(k[i], j), mk);
+      for (int j = 0; j < JK; ++j) kop[j] = JOINED ? q4_operand<OP>(word_of(k[i], j), mk) : operands[step & 1][i * JK + j][lane];
       float rest[NG][4];
       rests_of<T, D, GR>(ks[i], rest);
       const f32x4q y = logits_of<T, D, GR>(kop, ks[i], rest, q, sums);
 #pragma unroll
       for (int r = 0; r < 4; ++r) x[4 * i + r] = y[r];
     }
-    load_keys(after);
+    if constexpr (JOINED) load_keys(after);
     if (partial) {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
@@ -405,26 +470,14 @@ __global__ __launch_bounds__(256, (kAttendWaves<T, D, GR>)) void gemm_q4_attend_
         piece[c] = make_uint4(p[0][c], p[1][c], p[2][c], p[3][c]);
         if constexpr (OPV != kOpExact) one[e] = mfma_q4<OPV>(ones, piece[c], one[e]);
       }
-      // channels 16 j + n of eight slots: bits 4 (j % 4) of the words of half j / 4 of each pair of slots
 #pragma unroll
       for (int j = e * (GR / 16); j < (e + 1) * (GR / 16); ++j) {
-        uint32_t b[4];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const uint32_t w = word_of(v[c / 2], (D / 64) * (c % 2) + j / 4);
-          if constexpr (OPV == kOpBF16) {
-            b[c] = ((w >> (4 * (j % 4))) & mv.mask) | mv.magic;
-          } else {
-            const uint32_t two = (w >> (4 * (j % 4))) & 0x000f000fu;
-            b[c] = __builtin_amdgcn_perm(f2u((float)(two >> 16)), f2u((float)(two & 0xffffu)), 0x07060302u);
-          }
-        }
-        const uint4 vop = make_uint4(b[0], b[1], b[2], b[3]);
+        const uint4 vop = JOINED ? value_operand<OPV, D>(v, j, mv) : operands[step & 1][2 * JK + j][lane];
 #pragma unroll
         for (int c = 0; c < P; ++c) o[j] = mfma_q4<OPV>(vop, piece[c], o[j]);
       }
     }
-    load_values(after);
+    if constexpr (JOINED) load_values(after);
   }
 
   // sums over the lanes of a row, and the constants that entered with the codes
@@ -439,7 +492,7 @@ __global__ __launch_bounds__(256, (kAttendWaves<T, D, GR>)) void gemm_q4_attend_
 #pragma unroll
   for (int j = 0; j < JV; ++j) o[j] += low[j * 16 / GR];
   const size_t part = (size_t)blockIdx.x * a.row_tiles * 16;
-  if (!joined) {
+  if constexpr (!JOINED) {
     if (row0 + n >= a.R) return;
     if (pieces > 1) {
       if (g == 0) a.m[part + row] = m, a.l[part + row] = l;
@@ -661,12 +714,12 @@ __global__ __launch_bounds__(256) void gemm_q4_weights_kernel(Kv4Attend a) {
     }
 }
 
-template <class T, int D, int GR, bool LOGITS>
+template <class T, int D, int GR, int SHARE>
 int launch_attend(const Kv4Attend& a, hipStream_t s) {
-  const int tiles = (a.R + 15) / 16, per = a.token_waves == 4 ? 1 : 4;
+  const int tiles = (a.R + 15) / 16, per = SHARE == kTiles ? 4 : 1;
   const dim3 grid(a.blocks, (tiles + per - 1) / per);
-  const size_t lds = a.token_waves == 4 ? (size_t)4 * D * 64 : 0;
-  hipLaunchKernelGGL((gemm_q4_attend_kernel<T, D, GR, LOGITS>), grid, dim3(256), lds, s, a);
+  const size_t lds = SHARE == kTiles ? 2 * (D / 8) * 1024 + 2 * 16 * (D / GR) * 16 : 4 * D * 64;   // D / 16 operands each
+  hipLaunchKernelGGL((gemm_q4_attend_kernel<T, D, GR, SHARE>), grid, dim3(256), lds, s, a);
   CI_HIP_CHECK_LAUNCH();
   if (a.wanted || a.weights == 1) {
     constexpr int ROWS = 64 / (D / 4);
@@ -684,7 +737,8 @@ int launch_attend(const Kv4Attend& a, hipStream_t s) {
 
 template <class T, int D, int GR>
 int launch_attend_rows(const Kv4Attend& a, hipStream_t s) {
-  return a.weights == 1 ? launch_attend<T, D, GR, true>(a, s) : launch_attend<T, D, GR, false>(a, s);
+  if (a.token_waves == 1) return launch_attend<T, D, GR, kTiles>(a, s);
+  return a.weights == 1 ? launch_attend<T, D, GR, kSlotsAndLogits>(a, s) : launch_attend<T, D, GR, kSlots>(a, s);
 }
 
 }  // namespace
