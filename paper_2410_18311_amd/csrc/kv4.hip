@@ -1,5 +1,7 @@
 // Writing keys and values to a cache in 4 bits, reading them back, and evicting the slots that got the least weight (kv4.hpp).
-// All three are bound by the bytes they move, or, for single tokens, by their launches.
+// Reading is bound by its bytes (8 x 40 heads x 1024 slots, 220 MB: 46 us, 4.8 TB/s); writing by the packing's instructions from a few
+// hundred tokens on (1023 tokens of 32 heads 12.4 us), and by latency below (one token of 8 x 72 heads 4.0 us); eviction by the chain of barriers
+// in which a head's slots are chosen (1025 slots 13 us with the one move, 8192 slots 21 us and 18 for the moves).
 #include <algorithm>
 #include <type_traits>
 

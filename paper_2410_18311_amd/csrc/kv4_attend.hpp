@@ -1,15 +1,19 @@
 // Attention over a cache in 4 bits (kv4.hpp): out = softmax(scale q k^T, causal) v for S rows of each query head, one token or a prompt's
 // chunk, in one pass over the cache with a running maximum and sum.
 //
-// A wave takes tiles of 16 rows (the S G rows that share a head of the cache, G query heads to each) and steps of 32 slots.  The logits come out
+// A wave takes a tile of 16 rows (of the S G rows that share a head of the cache, G query heads to each) and steps of 32 slots.  The logits come out
 // of the matrix cores with slots down and rows across, four slots to a lane: just the layout in which the probabilities enter the product with
-// the values, so nothing is exchanged between lanes and nothing but the sums of waves passes through the LDS.  Steps and lowest values enter in
+// the values, so nothing is exchanged between lanes.  Steps and lowest values enter in
 // fp32: logit = step (q . codes) + low (sum q), and the probabilities are multiplied by the values' steps before they are split into
-// bf16 pieces (16 bits of them for 16-bit results, 24 for fp32).  The running maximum is raised only when a logit passes it by 2^8, which a
-// first look at the lane's own eight logits decides; the sums hold that range in fp32.
+// bf16 pieces (16 bits of them for 16-bit results, 24 for fp32; one piece would cost fp16 results as much as their own rounding).  The
+// running maximum is raised only when a logit passes it by 2^8, which a first look at the lane's own eight logits decides; the sums hold
+// that range in fp32.
 //
-// Bound: the cache's bytes where few rows meet many slots; 256 vector instructions a step (unpacking, the softmax, the pieces), which
-// is 10 TB/s of cache, leave room for that.  With 16 rows and more, the instructions.
+// Few rows: the waves of a workgroup take different steps and their sums are joined, and the slots of all sentences are shared out by length
+// over three workgroups a compute unit, joined by a second launch.  Bound by the cache's bytes: eight sentences of up to 65536 slots,
+// 259 MB, 56 us and 7 of the join (4.6 TB/s); where there are few of them by two launches' latency: 4096 slots of 40 heads 12 and 5 us.
+// Many rows: the waves take different tiles and share a step's operands.  Bound by vector instructions, 27 a logit and row: 512 rows over 2048 slots of 32
+// heads 58 us, and 28 for the slots' weights, for which the logits are computed again.
 #pragma once
 
 #include "kv4.hpp"
