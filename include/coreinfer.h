@@ -495,7 +495,7 @@ int coreinfer_w4_read(const void* packed, int64_t R, int64_t C, int group, void*
  * ldy >= R) may be of different types, so that the hidden values between two
  * products stay in fp32; both are aligned to their elements.  16-bit x is multiplied
  * as it is, fp32 x in three bf16 pieces (24 bits); sums in fp32, in a fixed order.
- * A row of x with an infinity or a NaN gives NaN.
+ * A row of x with an infinity or a NaN gives NaN.  y must not overlap x.
  * ws: coreinfer_w4_matvec_workspace_size bytes, 16-byte aligned; NULL where
  * that is 0 (one row, and as many as fit 64 KB).
  */
@@ -585,7 +585,8 @@ int coreinfer_kv4_attend(const ci_kv4* cache, const void* q, int64_t S, int64_t 
  *   weight_out, pos_out [B, H, cap]: of the new contents; slots from the budget to
  *     lens[b] - 1 get weight 0 and pos -1, others are left.  May be
  *     cache->weight and cache->pos.
- *   lens_out [B] or NULL: min(lens[b], budget); may be lens.
+ *   lens_out [B] or NULL: min(lens[b], budget); may be lens (apart from lens and next, calls
+ *     of few moves take one launch instead of two).
  * The order of slots is no longer that of positions, which attention does not ask for.
  * ws: coreinfer_kv4_evict_workspace_size bytes, 16-byte aligned.
  * 1 <= budget, 0 <= recent <= budget, 1 <= max_len <= cap.

@@ -580,10 +580,12 @@ int launch_kv4_evict(const ci_kv4& c, const int32_t* lens, const int32_t* next, 
   a.count = reinterpret_cast<int32_t*>(ws);
   a.holes = a.count + words256(heads);
   a.movers = a.holes + words256(heads * a.max_moves);
-  // In one launch where a workgroup's own moves are few, unless it would write lengths that others have yet to read.
-  const uintptr_t in = reinterpret_cast<uintptr_t>(lens), out = reinterpret_cast<uintptr_t>(lens_out);
-  const bool apart = !lens_out || out + c.B * sizeof(int32_t) <= in || in + c.B * sizeof(int32_t) <= out;
-  return by_shape<F32>(c.D, c.group, EvictLaunch{a, s, apart && a.max_moves <= kMovedHere});
+  // In one launch where a workgroup's own moves are few, unless it would write what others have yet to read.
+  auto apart = [&](const int32_t* in) {
+    const uintptr_t from = reinterpret_cast<uintptr_t>(in), to = reinterpret_cast<uintptr_t>(lens_out), bytes = c.B * sizeof(int32_t);
+    return !lens_out || to + bytes <= from || from + bytes <= to;
+  };
+  return by_shape<F32>(c.D, c.group, EvictLaunch{a, s, apart(lens) && apart(next) && a.max_moves <= kMovedHere});
 }
 
 }  // namespace ci

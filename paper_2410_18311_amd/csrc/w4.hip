@@ -2,7 +2,7 @@
 // up, gate and down matrices of deployed core neurons; a token reads 0.28 of the bytes of 16-bit weights (groups of 64).
 //
 // Bound by those bytes where there are enough of them: a gated 13824 x 5120 product of one row, 80 MB, 15.1 us (5.3 TB/s, a large
-// copy's rate); 14746 x 9216 of eight rows, 77 MB, 19.5 us.  Small ones are bound by latency: 4096 x 6554 (14 MB) 7.2 us, 1024 x 256 4.2 us.
+// copy's rate); 14746 x 9216 of eight rows, 77 MB, 18.0 us.  Small ones are bound by latency: 4096 x 6554 (14 MB) 7.2 us, 1024 x 256 4.2 us.
 // From 32 rows on by what is read of x: 64 rows of the gated product 63 us.
 //
 // Layout.  Rows by 16 and columns by 128 make a block of 1 KB, which a wave loads with one instruction: lane 16 g + n holds row n, word j
@@ -393,13 +393,16 @@ int launch_rows(const RowsArgs& a, int waves, hipStream_t s) {
 template <class D, int G, bool DUAL, int X, int ROWS>
 int launch_few(const RowsArgs& a, hipStream_t s) {
   // Eight waves to a compute unit, if there are as many blocks, and no more to a workgroup than registers leave room for (groups of 32, fp32).
-  // Pairs of tiles share what is read of x, where there are enough of them for the chip.
+  // Pairs of tiles share what is read of x, where there are enough of them for the chip, fours where that comes from memory (14746 x 9216, eight
+  // rows: 20.0 us in pairs, 18.2 in fours).
   constexpr int MOST = D::VEC == 8 && G > 32 && X == kXLds ? 16 : 8;
   const int RT = DUAL || a.tiles >= 900 ? 2 : 1, groups = DUAL ? a.tiles : (a.tiles + RT - 1) / RT;
   int waves = 4;
   while (waves < MOST && groups * waves < 2000 && waves * 2 <= a.nb) waves *= 2;
   if constexpr (DUAL) {
     return waves == 4 ? launch_rows<D, G, 2, 1, true, X, 256, ROWS>(a, waves, s) : launch_rows<D, G, 2, 1, true, X, MOST * 64, ROWS>(a, waves, s);
+  } else if (X == kXRows && RT == 2) {
+    return launch_rows<D, G, 4, 1, false, X, 512, ROWS>(a, 8, s);   // rows this long are more than eight blocks
   } else if (RT == 2) {
     return launch_rows<D, G, 2, 1, false, X, 512, ROWS>(a, waves, s);   // never more than eight waves
   } else {

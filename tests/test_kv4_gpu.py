@@ -423,6 +423,23 @@ def test_eviction_goes_by_positions_where_slots_are_out_of_order(lib):
     _check_evict(lib, 2, 2, T, 64, 32, 120, 60, pos=pos, nxt=[5000, 0])      # none and all
 
 
+def test_eviction_writes_lengths_over_what_it_reads(lib):
+    """lens_out over lens or over the positions, with few and with many moves: every head goes by what was there before."""
+    B, H, T = 2, 70, 300
+    for budget in (299, 20):
+        got = []
+        for over in ("apart", "lens", "next"):
+            cache, _, _ = _filled(lib, B, H, T, 64, 64, F16, 1)
+            cache.weight[:, :, :T] = _rand((B, H, T), F32, 2).abs()
+            n, nx, left = _ints(T, T - 1), _ints(T, T), _ints(0, 0)
+            out = {"apart": left, "lens": n, "next": nx}[over]
+            lib.kv4_evict(cache, n, nx, budget, 10, max_len=T, lens_out=out)
+            assert out.tolist() == [min(T, budget), min(T - 1, budget)]
+            got.append((cache.pos.clone(), cache.weight.clone()))
+        for pos, weight in got[1:]:
+            assert torch.equal(pos, got[0][0]) and torch.equal(weight, got[0][1])
+
+
 @pytest.mark.parametrize("T", [9000, 33000])
 def test_eviction_of_long_caches(lib, T):
     """From 40960 bytes of keys on the launch asks for its LDS, beyond 32768 slots the keys are formed again."""

@@ -112,6 +112,7 @@ def test_several_rows(lib, M, dtype, act, group):
     (1, 16390, 520, 64, "none", F16), (1, 20000, 128, 32, "relu", BF16),      # two tiles of rows a workgroup
     (8, 64, 9216, 64, "relu", F16), (16, 40, 4104, 128, "swiglu", BF16),      # x does not fit beside two workgroups
     (1, 24, 36864, 64, "none", F16), (3, 48, 11008, 128, "none", F32),        # long rows
+    (16, 14410, 2056, 64, "relu", BF16),                                       # fours of tiles beside rows in memory
     (1, 24, 70000, 128, "none", BF16), (64, 100, 2056, 32, "swiglu", F16)])
 def test_the_ways_that_sizes_choose(lib, M, R, C, group, act, dtype):
     _check(lib, M, R, C, group, act, dtype, seed=7)
