@@ -1,7 +1,7 @@
 // Writing keys and values to a cache in 4 bits, reading them back, and evicting the slots that got the least weight (kv4.hpp).
 // Reading is bound by its bytes (8 x 40 heads x 1024 slots, 220 MB: 46 us, 4.8 TB/s); writing by the packing's instructions from a few
 // hundred tokens on (1023 tokens of 32 heads 12.4 us), and by latency below (one token of 8 x 72 heads 4.0 us); eviction by the chain of barriers
-// in which a head's slots are chosen (1025 slots 13 us with the one move, 8192 slots 21 us and 18 for the moves).
+// in which a head's slots are chosen (one of 1025 slots 6 us with its move, 6144 of 8192 21 us and 18 for the moves).
 #include <algorithm>
 #include <type_traits>
 
@@ -184,6 +184,7 @@ __global__ __launch_bounds__(128) void kv4_read_kernel(Kv4 c, const int32_t* len
 
 // ---- eviction --------------------------------------------------------------------------------------------------------------------
 
+constexpr int kFew = 4;
 constexpr int kMovedHere = 256;  // moves of a head that the workgroup which plans them does itself
 
 struct EvictArgs {
@@ -209,6 +210,23 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
   add(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});   // the sums of the sixteens before
   add(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
   return v;
+}
+
+// The least (LEAST) or greatest of a wave's values, in every lane.
+template <bool LEAST>
+__device__ __forceinline__ uint32_t wave_extreme(uint32_t v) {
+  auto with = [&](auto ctrl, auto rows) {
+    const uint32_t u = (uint32_t)__builtin_amdgcn_update_dpp(LEAST ? -1 : 0, (int)v, decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+    v = LEAST ? min(v, u) : max(v, u);
+  };
+  constexpr std::integral_constant<int, 0xf> all{};
+  with(std::integral_constant<int, 0x111>{}, all);
+  with(std::integral_constant<int, 0x112>{}, all);
+  with(std::integral_constant<int, 0x114>{}, all);
+  with(std::integral_constant<int, 0x118>{}, all);
+  with(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});
+  with(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
+  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
 }
 
 // Exclusive sums over the workgroup; all threads take part.  sums: THREADS / 64 words that no other call uses.  Returns the total.
@@ -251,8 +269,10 @@ __device__ __forceinline__ void move_slot(const Kv4& c, size_t head, size_t to, 
 // Which slots of a head stay, which move where.  Keys: the last `recent` positions first, then by weight, NaN last; equal keys by the
 // lower slot.  The budget-th key is found eleven bits at a time from histograms in the LDS; the recent ones, all alike, and zeros, of which
 // there may be many, are counted by wave, or every lane would wait for all others at one bin.  CACHED: the keys of a head are kept in
-// the LDS.  MOVE: the rows are moved here as well (few of them, and nobody reads a length that this launch writes).
-template <int THREADS, bool CACHED, int D, int GR, bool MOVE>
+// the LDS.  MOVE: the rows are moved here as well (few of them, and nobody reads a length that this launch writes).  FEW: no more than
+// kFew slots can leave, as in a cache that is cut at every step, so these are looked for one by one (one of 1025 slots of 320 heads: 6 us
+// instead of 13).
+template <int THREADS, bool CACHED, int D, int GR, bool MOVE, bool FEW>
 __global__ __launch_bounds__(THREADS) void kv4_plan_kernel(EvictArgs a) {
   extern __shared__ uint32_t cache[];
   constexpr int kBins = 2048;
@@ -312,109 +332,163 @@ __global__ __launch_bounds__(THREADS) void kv4_plan_kernel(EvictArgs a) {
   }
   __syncthreads();
 
-  uint32_t prefix = 0, want = (uint32_t)a.budget;
-  if (recents >= want) {
-    prefix = kRecent;
-  } else {
-    want -= recents;
-#pragma unroll
-    for (int pass = 0; pass < 3; ++pass) {
-      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
-      const uint32_t mask = pass == 2 ? 1023u : 2047u;
-#pragma unroll 4
-      for (int t0 = 0; t0 < len; t0 += THREADS) {
-        const int t = t0 + tid;
-        const uint32_t key = t < len ? key_at(t) : kRecent;
-        const bool in = key != kRecent && (pass == 0 || key >> (pass == 1 ? 21 : 10) == prefix);
-        if (!__any(in)) continue;   // most rounds of the later passes
-        const uint64_t zeros = __ballot(in && key == kZero);
-        if (zeros && lane == 0) atomicAdd(&hist[pass][kZero >> shift & mask], (uint32_t)__popcll(zeros));
-        if (in && key != kZero) atomicAdd(&hist[pass][key >> shift & mask], 1u);
-      }
-      __syncthreads();
-      // a run of bins a thread, from the largest down
-      constexpr int RUN = kBins / THREADS;
-      const int i0 = kBins - RUN * (tid + 1);
-      uint32_t c[RUN], mine = 0, before;
-#pragma unroll
-      for (int i = 0; i < RUN; ++i) c[i] = hist[pass][i0 + RUN - 1 - i], mine += c[i];
-      block_scan<THREADS>(mine, sums[pass], &before);
-      if (before < want && before + mine >= want) {
-        int i = 0;
-#pragma unroll
-        for (int j = 0; j < RUN - 1; ++j)
-          if (i == j && before + c[j] < want) before += c[j], ++i;
-        chosen[pass][0] = (uint32_t)(i0 + RUN - 1 - i);
-        chosen[pass][1] = want - before;
-      }
-      __syncthreads();
-      prefix = pass == 0 ? chosen[pass][0] : prefix << (pass == 1 ? 11 : 10) | chosen[pass][0];
-      want = chosen[pass][1];
-    }
-  }
-
-  // A stretch of slots a wave, 64 at a time in order: the equal ones before it, then the holes and the slots that move, counted by ballots.
-  constexpr int WAVES = THREADS / 64;
-  const int wave = tid >> 6, stretch = ((len + THREADS - 1) / THREADS) * 64;
-  const int t0 = wave * stretch, t1 = min(t0 + stretch, len);
-  const uint64_t lower = lanemask_lt();
-  auto over_waves = [&](uint32_t mine, uint32_t* of, uint32_t* all) {   // the sum over the waves before this one; a barrier
-    if (lane == 0) of[wave] = mine;
-    __syncthreads();
-    uint32_t sum = 0, total = 0;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-      sum += w < wave ? of[w] : 0;
-      total += of[w];
-    }
-    *all = total;
-    return sum;
-  };
-  uint32_t equal = 0, total;
-#pragma unroll 4
-  for (int t = t0 + lane; t - lane < t1; t += 64) equal += (uint32_t)__popcll(__ballot(t < t1 && key_at(t) == prefix));
-  const uint32_t equal_before = over_waves(equal, sums[3], &total);
-  auto walk = [&](auto&& visit) {   // visit(slot, is a hole, moves)
-    uint32_t e = equal_before;
-#pragma unroll 4
-    for (int t = t0 + lane; t - lane < t1; t += 64) {
-      const uint32_t key = t < t1 ? key_at(t) : 0u;
-      const uint64_t same = __ballot(t < t1 && key == prefix);
-      const bool kept = key > prefix || (key == prefix && e + (uint32_t)__popcll(same & lower) < want);
-      e += (uint32_t)__popcll(same);
-      visit(t, t < t1 && !kept && t < a.budget, t < t1 && kept && t >= a.budget);
-    }
-  };
-  uint32_t n_holes = 0, n_movers = 0;
-  walk([&](int, bool hole, bool mover) {
-    n_holes += (uint32_t)__popcll(__ballot(hole));
-    n_movers += (uint32_t)__popcll(__ballot(mover));
-  });
-  uint32_t ih, im;
-  im = over_waves(n_movers, sums[4], &total);
-  ih = over_waves(n_holes, sums[5], &total);   // as many holes as slots that move
-  const int moves = (int)total;
-  // The lists, in the LDS where the histograms were if they fit there (16 bits a slot); rows that are not moved here need them in memory too.
-  constexpr int kListed = 3 * kBins * 4 / 4;   // moves whose lists of 16-bit slots fit
+  // lists of the moves: in the LDS, where the histograms were, if they fit there (16 bits a slot)
+  constexpr int kListed = 3 * kBins * 4 / 4, WAVES = THREADS / 64;
   uint16_t* lists = reinterpret_cast<uint16_t*>(hist);
-  const bool small = CACHED && moves <= kListed;
   int32_t* holes = a.holes + head * a.max_moves;
   int32_t* movers = a.movers + head * a.max_moves;
-  walk([&](int t, bool hole, bool mover) {
-    const uint64_t all_holes = __ballot(hole), all_movers = __ballot(mover);
-    const uint32_t to = ih + (uint32_t)__popcll(all_holes & lower), of = im + (uint32_t)__popcll(all_movers & lower);
-    if (hole) {
-      if (small) lists[to] = (uint16_t)t;
-      if (!MOVE) holes[to] = t;
+  const int wave = tid >> 6;
+  int moves;
+  bool small;
+  if constexpr (FEW) {
+    static_assert(CACHED && MOVE, "keys in the LDS, rows moved here");
+    __shared__ uint32_t least[2][WAVES][2];   // by turns: one barrier a slot
+    int gone[kFew];
+#pragma unroll
+    for (int r = 0; r < kFew; ++r) {
+      gone[r] = -1;
+      if (r >= len - a.budget) continue;
+      uint32_t key = kRecent, place = 0;   // of the last of the least, its number counted from one
+      for (int t = tid; t < len; t += THREADS) {
+        bool left = false;
+#pragma unroll
+        for (int q = 0; q < r; ++q) left |= t == gone[q];
+        const uint32_t k = cache[t];
+        if (!left && k <= key) key = k, place = (uint32_t)t + 1;
+      }
+      const uint32_t wave_key = wave_extreme<true>(key), wave_place = wave_extreme<false>(key == wave_key ? place : 0u);
+      if (lane == 0) least[r & 1][wave][0] = wave_key, least[r & 1][wave][1] = wave_place;
+      __syncthreads();
+      key = kRecent, place = 0;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        const uint32_t k = least[r & 1][w][0], at = least[r & 1][w][1];
+        place = k < key ? at : k == key ? max(place, at) : place;
+        key = min(key, k);
+      }
+      gone[r] = (int)place - 1;
     }
-    if (mover) {
-      if (small) lists[kListed + of] = (uint16_t)t;
-      if (!MOVE) movers[of] = t;
+    // the holes in ascending order, and the slots from the budget on that have not left
+    small = true;
+    moves = 0;
+#pragma unroll
+    for (int r = 0; r < kFew; ++r) {
+      if (gone[r] < 0 || gone[r] >= a.budget) continue;
+      int before = 0;
+#pragma unroll
+      for (int q = 0; q < kFew; ++q) before += gone[q] >= 0 && gone[q] < gone[r];
+      if (tid == 0) lists[before] = (uint16_t)gone[r];
+      ++moves;
     }
-    ih += (uint32_t)__popcll(all_holes);
-    im += (uint32_t)__popcll(all_movers);
-  });
-  if (!MOVE && tid == 0) a.count[head] = moves;
+    int of = 0;
+    for (int t = a.budget; t < len; ++t) {
+      bool left = false;
+#pragma unroll
+      for (int q = 0; q < kFew; ++q) left |= t == gone[q];
+      if (left) continue;
+      if (tid == 0) lists[kListed + of] = (uint16_t)t;
+      ++of;
+    }
+  } else {
+    uint32_t prefix = 0, want = (uint32_t)a.budget;
+    if (recents >= want) {
+      prefix = kRecent;
+    } else {
+      want -= recents;
+#pragma unroll
+      for (int pass = 0; pass < 3; ++pass) {
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+        const uint32_t mask = pass == 2 ? 1023u : 2047u;
+#pragma unroll 4
+        for (int t0 = 0; t0 < len; t0 += THREADS) {
+          const int t = t0 + tid;
+          const uint32_t key = t < len ? key_at(t) : kRecent;
+          const bool in = key != kRecent && (pass == 0 || key >> (pass == 1 ? 21 : 10) == prefix);
+          if (!__any(in)) continue;   // most rounds of the later passes
+          const uint64_t zeros = __ballot(in && key == kZero);
+          if (zeros && lane == 0) atomicAdd(&hist[pass][kZero >> shift & mask], (uint32_t)__popcll(zeros));
+          if (in && key != kZero) atomicAdd(&hist[pass][key >> shift & mask], 1u);
+        }
+        __syncthreads();
+        // a run of bins a thread, from the largest down
+        constexpr int RUN = kBins / THREADS;
+        const int i0 = kBins - RUN * (tid + 1);
+        uint32_t c[RUN], mine = 0, before;
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) c[i] = hist[pass][i0 + RUN - 1 - i], mine += c[i];
+        block_scan<THREADS>(mine, sums[pass], &before);
+        if (before < want && before + mine >= want) {
+          int i = 0;
+#pragma unroll
+          for (int j = 0; j < RUN - 1; ++j)
+            if (i == j && before + c[j] < want) before += c[j], ++i;
+          chosen[pass][0] = (uint32_t)(i0 + RUN - 1 - i);
+          chosen[pass][1] = want - before;
+        }
+        __syncthreads();
+        prefix = pass == 0 ? chosen[pass][0] : prefix << (pass == 1 ? 11 : 10) | chosen[pass][0];
+        want = chosen[pass][1];
+      }
+    }
+
+    // A stretch of slots a wave, 64 at a time in order: the equal ones before it, then the holes and the slots that move, counted by ballots.
+    const int stretch = ((len + THREADS - 1) / THREADS) * 64;
+    const int t0 = wave * stretch, t1 = min(t0 + stretch, len);
+    const uint64_t lower = lanemask_lt();
+    auto over_waves = [&](uint32_t mine, uint32_t* of, uint32_t* all) {   // the sum over the waves before this one; a barrier
+      if (lane == 0) of[wave] = mine;
+      __syncthreads();
+      uint32_t sum = 0, total = 0;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        sum += w < wave ? of[w] : 0;
+        total += of[w];
+      }
+      *all = total;
+      return sum;
+    };
+    uint32_t equal = 0, total;
+#pragma unroll 4
+    for (int t = t0 + lane; t - lane < t1; t += 64) equal += (uint32_t)__popcll(__ballot(t < t1 && key_at(t) == prefix));
+    const uint32_t equal_before = over_waves(equal, sums[3], &total);
+    auto walk = [&](auto&& visit) {   // visit(slot, is a hole, moves)
+      uint32_t e = equal_before;
+#pragma unroll 4
+      for (int t = t0 + lane; t - lane < t1; t += 64) {
+        const uint32_t key = t < t1 ? key_at(t) : 0u;
+        const uint64_t same = __ballot(t < t1 && key == prefix);
+        const bool kept = key > prefix || (key == prefix && e + (uint32_t)__popcll(same & lower) < want);
+        e += (uint32_t)__popcll(same);
+        visit(t, t < t1 && !kept && t < a.budget, t < t1 && kept && t >= a.budget);
+      }
+    };
+    uint32_t n_holes = 0, n_movers = 0;
+    walk([&](int, bool hole, bool mover) {
+      n_holes += (uint32_t)__popcll(__ballot(hole));
+      n_movers += (uint32_t)__popcll(__ballot(mover));
+    });
+    uint32_t ih, im;
+    im = over_waves(n_movers, sums[4], &total);
+    ih = over_waves(n_holes, sums[5], &total);   // as many holes as slots that move
+    moves = (int)total;
+    // rows that are not moved here need the lists in memory too
+    small = CACHED && moves <= kListed;
+    walk([&](int t, bool hole, bool mover) {
+      const uint64_t all_holes = __ballot(hole), all_movers = __ballot(mover);
+      const uint32_t to = ih + (uint32_t)__popcll(all_holes & lower), of = im + (uint32_t)__popcll(all_movers & lower);
+      if (hole) {
+        if (small) lists[to] = (uint16_t)t;
+        if (!MOVE) holes[to] = t;
+      }
+      if (mover) {
+        if (small) lists[kListed + of] = (uint16_t)t;
+        if (!MOVE) movers[of] = t;
+      }
+      ih += (uint32_t)__popcll(all_holes);
+      im += (uint32_t)__popcll(all_movers);
+    });
+    if (!MOVE && tid == 0) a.count[head] = moves;
+  }
   auto hole_at = [&](int i) { return small ? (int)lists[i] : holes[i]; };
   auto mover_at = [&](int i) { return small ? (int)lists[kListed + i] : movers[i]; };
   __syncthreads();   // the lists, every read of a weight or position for a key, and what the copies stored
@@ -506,9 +580,9 @@ struct EvictLaunch {
   EvictArgs a;
   hipStream_t s;
   bool here;
-  template <int THREADS, bool CACHED, int D, int GR, bool MOVE>
+  template <int THREADS, bool CACHED, int D, int GR, bool MOVE, bool FEW>
   int plan() const {
-    auto* kernel = kv4_plan_kernel<THREADS, CACHED, D, GR, MOVE>;
+    auto* kernel = kv4_plan_kernel<THREADS, CACHED, D, GR, MOVE, FEW>;
     const size_t lds = CACHED ? (size_t)a.max_len * sizeof(uint32_t) : 0;
     static std::atomic<uint64_t> seen{0};
     if (lds > 32768) {   // with the kernel's own, more than a launch may have unasked
@@ -521,9 +595,12 @@ struct EvictLaunch {
   }
   template <int D, int GR, bool MOVE>
   int plan_any() const {
+    if constexpr (MOVE)
+      if (a.max_len - a.budget <= kFew && a.max_len <= kCachedKeys)
+        return a.max_len <= 2048 ? plan<256, true, D, GR, true, true>() : plan<1024, true, D, GR, true, true>();
     // a wave's share of the steps against the barriers' cost
-    if (a.max_len <= 2048) return plan<256, true, D, GR, MOVE>();
-    return a.max_len <= kCachedKeys ? plan<1024, true, D, GR, MOVE>() : plan<1024, false, D, GR, MOVE>();
+    if (a.max_len <= 2048) return plan<256, true, D, GR, MOVE, false>();
+    return a.max_len <= kCachedKeys ? plan<1024, true, D, GR, MOVE, false>() : plan<1024, false, D, GR, MOVE, false>();
   }
   template <class T, int D, int GR>
   int operator()() const {

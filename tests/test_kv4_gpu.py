@@ -423,6 +423,22 @@ def test_eviction_goes_by_positions_where_slots_are_out_of_order(lib):
     _check_evict(lib, 2, 2, T, 64, 32, 120, 60, pos=pos, nxt=[5000, 0])      # none and all
 
 
+@pytest.mark.parametrize("T", [5, 70, 1000, 2049, 3000])
+def test_eviction_of_few_slots(lib, T):
+    """One to five slots more than the budget, with the lowest among the last slots, equal, recent, NaN or zero."""
+    for gone in (1, 2, 3, 4, 5):
+        budget = T - gone
+        if budget < 1:
+            continue
+        w = torch.rand(4, 2, T, generator=torch.Generator().manual_seed(T + gone))
+        w[1] = 0.5                                   # all equal: the last slots leave
+        w[2, :, budget:] = 0.0                       # the last slots leave
+        w[3, 0, ::2], w[3, 1, : T // 2] = float("nan"), 0.0
+        for recent in (0, 1, budget // 2, budget):
+            for alias in (True, False):
+                _check_evict(lib, 4, 2, T, 64, 64, budget, recent, weight=w, alias=alias, lens=[T, T, T - 1 if gone > 1 else T, T])
+
+
 def test_eviction_writes_lengths_over_what_it_reads(lib):
     """lens_out over lens or over the positions, with few and with many moves: every head goes by what was there before."""
     B, H, T = 2, 70, 300
