@@ -2,7 +2,7 @@
 // up, gate and down matrices of deployed core neurons; a token reads 0.28 of the bytes of 16-bit weights (groups of 64).
 //
 // Bound by those bytes where there are enough of them: a gated 13824 x 5120 product of one row, 80 MB, 15.1 us (5.3 TB/s, a large
-// copy's rate); 14746 x 9216 of eight rows, 77 MB, 18.0 us.  Small ones are bound by latency: 4096 x 6554 (14 MB) 7.2 us, 1024 x 256 4.2 us.
+// copy's rate); 14746 x 9216 of eight rows, 77 MB, 17.2 us.  Small ones are bound by latency: 4096 x 6554 (14 MB) 7.2 us, 1024 x 256 4.2 us.
 // From 32 rows on by what is read of x: 64 rows of the gated product 63 us.
 //
 // Layout.  Rows by 16 and columns by 128 make a block of 1 KB, which a wave loads with one instruction: lane 16 g + n holds row n, word j
