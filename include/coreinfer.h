@@ -586,7 +586,7 @@ int coreinfer_kv4_attend(const ci_kv4* cache, const void* q, int64_t S, int64_t 
  *     lens[b] - 1 get weight 0 and pos -1, others are left.  May be
  *     cache->weight and cache->pos.
  *   lens_out [B] or NULL: min(lens[b], budget); may be lens (apart from lens and next, calls
- *     of few moves take one launch instead of two).
+ *     of few moves and max_len <= 32768 take one launch instead of two).
  * The order of slots is no longer that of positions, which attention does not ask for.
  * ws: coreinfer_kv4_evict_workspace_size bytes, 16-byte aligned.
  * 1 <= budget, 0 <= recent <= budget, 1 <= max_len <= cap.

@@ -269,11 +269,13 @@ __device__ __forceinline__ void move_slot(const Kv4& c, size_t head, size_t to, 
 // Which slots of a head stay, which move where.  Keys: the last `recent` positions first, then by weight, NaN last; equal keys by the
 // lower slot.  The budget-th key is found eleven bits at a time from histograms in the LDS; the recent ones, all alike, and zeros, of which
 // there may be many, are counted by wave, or every lane would wait for all others at one bin.  CACHED: the keys of a head are kept in
-// the LDS.  MOVE: the rows are moved here as well (few of them, and nobody reads a length that this launch writes).  FEW: no more than
+// the LDS.  MOVE: the rows are moved here as well (few of them, and nobody reads a length that this launch writes), from lists in the LDS, whose
+// 16 bits a slot hold what CACHED allows.  FEW: no more than
 // kFew slots can leave, as in a cache that is cut at every step, so these are looked for one by one (one of 1025 slots of 320 heads: 6 us
 // instead of 13).
 template <int THREADS, bool CACHED, int D, int GR, bool MOVE, bool FEW>
 __global__ __launch_bounds__(THREADS) void kv4_plan_kernel(EvictArgs a) {
+  static_assert(CACHED || !MOVE, "without lists in the LDS the moves are another launch's, from those in memory");
   extern __shared__ uint32_t cache[];
   constexpr int kBins = 2048;
   __shared__ __attribute__((aligned(16))) uint32_t hist[3][kBins];   // of the three passes; the last uses half of its
@@ -341,7 +343,7 @@ __global__ __launch_bounds__(THREADS) void kv4_plan_kernel(EvictArgs a) {
   int moves;
   bool small;
   if constexpr (FEW) {
-    static_assert(CACHED && MOVE, "keys in the LDS, rows moved here");
+    static_assert(MOVE, "rows moved here");
     __shared__ uint32_t least[2][WAVES][2];   // by turns: one barrier a slot
     int gone[kFew];
 #pragma unroll
@@ -532,7 +534,7 @@ __global__ __launch_bounds__(256) void kv4_move_kernel(EvictArgs a) {
   move_slot<D, GR>(a.c, head, a.holes[head * a.max_moves + i], a.movers[head * a.max_moves + i], threadIdx.x & 15);
 }
 
-constexpr int kCachedKeys = 32768;
+constexpr int kCachedKeys = 32768;   // 128 KB of the LDS
 
 template <class T, class F>
 int by_shape(int D, int group, F&& f) {
@@ -594,13 +596,15 @@ struct EvictLaunch {
     return CI_OK;
   }
   template <int D, int GR, bool MOVE>
-  int plan_any() const {
+  int plan_any() const {   // MOVE: max_len <= kCachedKeys
     if constexpr (MOVE)
-      if (a.max_len - a.budget <= kFew && a.max_len <= kCachedKeys)
+      if (a.max_len - a.budget <= kFew)
         return a.max_len <= 2048 ? plan<256, true, D, GR, true, true>() : plan<1024, true, D, GR, true, true>();
     // a wave's share of the steps against the barriers' cost
     if (a.max_len <= 2048) return plan<256, true, D, GR, MOVE, false>();
-    return a.max_len <= kCachedKeys ? plan<1024, true, D, GR, MOVE, false>() : plan<1024, false, D, GR, MOVE, false>();
+    if constexpr (!MOVE)
+      if (a.max_len > kCachedKeys) return plan<1024, false, D, GR, false, false>();
+    return plan<1024, true, D, GR, MOVE, false>();
   }
   template <class T, int D, int GR>
   int operator()() const {
@@ -657,12 +661,13 @@ int launch_kv4_evict(const ci_kv4& c, const int32_t* lens, const int32_t* next, 
   a.count = reinterpret_cast<int32_t*>(ws);
   a.holes = a.count + words256(heads);
   a.movers = a.holes + words256(heads * a.max_moves);
-  // In one launch where a workgroup's own moves are few, unless it would write what others have yet to read.
+  // In one launch where a workgroup's own moves are few and the keys fit the LDS, unless it would write what others have yet to read.
   auto apart = [&](const int32_t* in) {
     const uintptr_t from = reinterpret_cast<uintptr_t>(in), to = reinterpret_cast<uintptr_t>(lens_out), bytes = c.B * sizeof(int32_t);
     return !lens_out || to + bytes <= from || from + bytes <= to;
   };
-  return by_shape<F32>(c.D, c.group, EvictLaunch{a, s, apart(lens) && apart(next) && a.max_moves <= kMovedHere});
+  const bool here = max_len <= kCachedKeys && a.max_moves <= kMovedHere && apart(lens) && apart(next);
+  return by_shape<F32>(c.D, c.group, EvictLaunch{a, s, here});
 }
 
 }  // namespace ci

@@ -1,6 +1,8 @@
 """The 4-bit cache on the GPU against the plain definitions: writes, reads and evictions exactly, attention within the rounding of
 its sums."""
 
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -462,3 +464,30 @@ def test_eviction_of_long_caches(lib, T):
     w = (torch.rand(1, 2, T, generator=torch.Generator().manual_seed(1)) * 500).floor() / 500    # many equal
     for budget in (2048, T - 1):
         _check_evict(lib, 1, 2, T, 64, 64, budget, 64, weight=w)
+
+
+@pytest.mark.parametrize("D,group", [(64, 64), (128, 32)])
+@pytest.mark.parametrize("T,budget", [(32768, 32767), (32769, 32768), (33000, 32999), (33000, 32990), (33000, 256), (33000, 100)])
+def test_eviction_of_few_slots_of_long_caches_into_other_lengths(lib, T, budget, D, group):
+    """Few moves, and lengths apart from what is read, on both sides of the 32768 slots whose keys fit the LDS."""
+    w = (torch.rand(1, 2, T, generator=torch.Generator().manual_seed(T + budget)) * 500).floor() / 500    # many equal
+    _check_evict(lib, 1, 2, T, D, group, budget, 64, weight=w, alias=False)
+
+
+def test_eviction_without_lengths(lib):
+    """lens_out NULL, which is apart from everything: the same slots stay as where the lengths are written."""
+    for T, budget in ((300, 299), (300, 50), (3000, 700), (33000, 32999), (33000, 200)):
+        got = []
+        for written in (True, False):
+            cache, _, _ = _filled(lib, 1, 2, T, 64, 32, F16, 4)
+            cache.weight[:, :, :T] = _rand((1, 2, T), F32, 5).abs()
+            n, out = _ints(T), _ints(0)
+            wo, po = torch.full_like(cache.weight, 9.0), torch.full_like(cache.pos, 9)
+            ws = torch.full((lib.kv4_evict_workspace_size(cache, T, budget),), 0xff, dtype=torch.uint8, device=DEV)
+            status = lib.raw.coreinfer_kv4_evict(ctypes.byref(cache.desc), n.data_ptr(), n.data_ptr(), T, budget, 9, wo.data_ptr(), po.data_ptr(),
+                                                 out.data_ptr() if written else None, ws.data_ptr(), ws.numel(),
+                                                 torch.cuda.current_stream().cuda_stream)
+            assert status == lib.CI_OK and out.item() == (budget if written else 0)
+            got.append((wo, po, *lib.kv4_read(cache, _ints(budget), 0, budget, F32)))
+        for a, b in zip(*got):
+            assert torch.equal(a, b)
