@@ -494,7 +494,8 @@ int coreinfer_w4_read(const void* packed, int64_t R, int64_t C, int group, void*
  * x [M, C] of x_dtype (row stride ldx >= C) and y [M, R] of y_dtype (row stride
  * ldy >= R) may be of different types, so that the hidden values between two
  * products stay in fp32; both are aligned to their elements.  16-bit x is multiplied
- * as it is, fp32 x in three bf16 pieces (24 bits); sums in fp32, in a fixed order.
+ * as it is, fp32 x in three bf16 pieces (24 bits); sums in fp32, in a fixed order,
+ * for 16-bit x of the codes plus 16 (1.4 of the 24 bits are the 16's).
  * A row of x with an infinity or a NaN gives NaN.  y must not overlap x.
  * ws: coreinfer_w4_matvec_workspace_size bytes, 16-byte aligned; NULL where
  * that is 0 (one row, and as many as fit 64 KB).

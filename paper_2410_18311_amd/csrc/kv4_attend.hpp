@@ -100,11 +100,11 @@ __device__ __forceinline__ uint4 value_operand(const uint4 (&v)[2], int j, const
   uint32_t e[4];
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
-    const uint32_t w = word_of(v[c / 2], (D / 64) * (c % 2) + j / 4) >> (4 * (j % 4));
-    if constexpr (OP == kOpBF16) {
-      e[c] = (w & magic.mask) | magic.magic;
+    const uint32_t w = word_of(v[c / 2], (D / 64) * (c % 2) + j / 4);
+    if constexpr (OP != kOpExact) {
+      e[c] = q4_pair<OP>(w, j % 4, magic);
     } else {
-      const uint32_t two = w & 0x000f000fu;
+      const uint32_t two = (w >> (4 * (j % 4))) & 0x000f000fu;
       e[c] = __builtin_amdgcn_perm(f2u((float)(two >> 16)), f2u((float)(two & 0xffffu)), 0x07060302u);
     }
   }

@@ -5,11 +5,11 @@
 //   step (sum n x) + low (sum x),
 // so the matrix cores multiply the codes themselves and the two fp16 numbers enter once per group, in fp32.
 //
-// A code becomes an operand without a conversion: the bits of a code in the mantissa of 128 (bf16) are 128 + n, in that of 64 (fp16)
-// 64 + n, and one instruction puts two of them there.  The constant comes out again with the sum of x, which the matrix cores form
-// beside (a product with ones): 0.9 vector instructions an element, where a conversion takes more than 2.  It costs log2(128 / 8) = 4
-// (fp16: 3) of the 24 bits of the sums, which 16-bit results do not show; operands for fp32 results carry the codes exactly and take twice the
-// instructions.
+// A code becomes an operand without a conversion: its bits at the top of the mantissa of 16 are 16 + n, and two instructions put two of them there.
+// The constant comes out again with the sum of x, which the matrix cores form beside (a product with ones): one vector instruction an element,
+// where a conversion takes more than 2.  At the bottom of the mantissa they would be 128 + n (fp16: 64 + n) and an eighth of the instructions less,
+// but the sums lose what their size loses: 24 on average instead of the codes' own 9, 1.4 of 24 bits, not 4.  Operands for fp32 rows carry the
+// codes exactly and take twice the instructions.
 #pragma once
 
 #include "common.hpp"
@@ -23,10 +23,11 @@ typedef _Float16 f16x8q __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2q __attribute__((ext_vector_type(2)));
 typedef float f32x2q __attribute__((ext_vector_type(2)));
 
-// What multiplies: bf16 with 128 + n, fp16 with 64 + n, bf16 with n.
+// What multiplies: bf16 with 16 + n, fp16 with 16 + n, bf16 with n.
 enum { kOpBF16, kOpF16, kOpExact };
-template <int OP> constexpr float kOffset = OP == kOpBF16 ? 128.0f : OP == kOpF16 ? 64.0f : 0.0f;
-template <int OP> constexpr uint32_t kMagic = OP == kOpBF16 ? 0x43004300u : 0x54005400u;
+template <int OP> constexpr float kOffset = OP == kOpExact ? 0.0f : 16.0f;
+template <int OP> constexpr uint32_t kMagic = OP == kOpF16 ? 0x4c004c00u : 0x41804180u;
+template <int OP> constexpr int kCodeBit = OP == kOpF16 ? 6 : 3;   // where a code stands in its half-word
 template <int OP> constexpr uint32_t kOnes = OP == kOpF16 ? 0x3c003c00u : 0x3f803f80u;
 
 // The other operand in as many pieces as hold it whole: fp32 values in three bf16 ones, 16-bit values as they are.
@@ -50,21 +51,24 @@ struct Q4Magic {
 };
 template <int OP>
 __device__ __forceinline__ Q4Magic q4_magic() {
-  Q4Magic m{OP == kOpF16 ? 0x00f000f0u : 0x000f000fu, kMagic<OP>};
+  Q4Magic m{0x000f000fu << kCodeBit<OP>, kMagic<OP>};
   asm("" : "+s"(m.mask), "+v"(m.magic));
   return m;
+}
+
+// The two codes at bits 4 i and 16 + 4 i of w.
+template <int OP>
+__device__ __forceinline__ uint32_t q4_pair(uint32_t w, int i, const Q4Magic& m) {
+  const int up = kCodeBit<OP> - 4 * i;
+  return ((up > 0 ? w << up : w >> -up) & m.mask) | m.magic;
 }
 
 // Eight codes as an operand's eight elements: element 2 i is the nibble i of w, element 2 i + 1 the nibble i + 4.
 template <int OP>
 __device__ __forceinline__ uint4 q4_operand(uint32_t w, const Q4Magic& m) {
-  if constexpr (OP == kOpBF16)
-    return make_uint4((w & m.mask) | m.magic, ((w >> 4) & m.mask) | m.magic, ((w >> 8) & m.mask) | m.magic,
-                      ((w >> 12) & m.mask) | m.magic);
-  else if constexpr (OP == kOpF16)
-    return make_uint4(((w << 4) & m.mask) | m.magic, (w & m.mask) | m.magic, ((w >> 4) & m.mask) | m.magic,
-                      ((w >> 8) & m.mask) | m.magic);
-  else {
+  if constexpr (OP != kOpExact) {
+    return make_uint4(q4_pair<OP>(w, 0, m), q4_pair<OP>(w, 1, m), q4_pair<OP>(w, 2, m), q4_pair<OP>(w, 3, m));
+  } else {
     // bytes 0 .. 3 of even: nibbles 0, 2, 4, 6; a code below 16 is exact in the upper half of its fp32 image
     const uint32_t even = w & 0x0f0f0f0fu, odd = (w >> 4) & 0x0f0f0f0fu;
     auto pair = [](uint32_t a, uint32_t b) {
