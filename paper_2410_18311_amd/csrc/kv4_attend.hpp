@@ -7,7 +7,8 @@
 // fp32: logit = step (q . codes) + low (sum q), and the probabilities are multiplied by the values' steps before they are split into
 // bf16 pieces (16 bits of them for 16-bit results, 24 for fp32; one piece would cost fp16 results as much as their own rounding).  The
 // running maximum is raised only when a logit passes it by 2^8, which a first look at the lane's own eight logits decides; the sums hold
-// that range in fp32.
+// that range in fp32.  The results' sums and what has to leave them again, the codes' offset times the probabilities, and their lowest values, are large
+// and nearly cancel, ever more so the more slots average out, so they are put together every few steps (kFold).
 //
 // Few rows: the waves of a workgroup take different steps and their sums are joined, and the slots of all sentences are shared out by length
 // over three workgroups a compute unit, joined by a second launch.  Bound by the cache's bytes: eight sentences of up to 65536 slots,
@@ -20,6 +21,10 @@
 
 namespace ci {
 namespace {
+
+// Steps of 32 slots after which a wave puts its sums together.  What stands between is 5 times (fp32: 2) what the slots' values come to at random
+// and rounded at every step: 1e-5 of the results (fp32 2e-6) however many slots there are.
+template <int OP> constexpr int kFold = OP == kOpExact ? 4 : 8;
 
 template <class T> struct AttendType;
 template <> struct AttendType<F32> { static constexpr int P = 3, OPV = kOpExact; };
@@ -391,6 +396,20 @@ __global__ __launch_bounds__(256, (kAttendWaves<T, D, GR>)) void gemm_q4_attend_
 #pragma unroll
   for (int j = 0; j < JV; ++j) o[j] = f32x4q{0.0f, 0.0f, 0.0f, 0.0f};
 
+  auto fold = [&] {   // the constants that entered with the codes, and the lowest values, over the lanes of a row
+#pragma unroll
+    for (int f = 0; f < NG; ++f) {
+      float c = low[f] + __shfl_xor(low[f], 16, kWave);
+      c += __shfl_xor(c, 32, kWave);
+      if constexpr (OPV != kOpExact) c = __builtin_fmaf(-kOffset<OPV>, one[f][0], c);
+#pragma unroll
+      for (int j = f * (GR / 16); j < (f + 1) * (GR / 16); ++j) o[j] += c;
+      low[f] = 0.0f;
+      one[f] = f32x4q{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+  };
+  int unfolded = 0;
+
   for (int step = step0; step < steps; step += stride) {
     const int t0 = step * 32, after = min(step + stride, steps - 1);
     const bool partial = t0 + 32 > low_limit;
@@ -482,19 +501,15 @@ __global__ __launch_bounds__(256, (kAttendWaves<T, D, GR>)) void gemm_q4_attend_
       }
     }
     if constexpr (JOINED) load_values(after);
+    if (++unfolded == kFold<OPV>) {
+      fold();
+      unfolded = 0;
+    }
   }
 
-  // sums over the lanes of a row, and the constants that entered with the codes
   l += __shfl_xor(l, 16, kWave);
   l += __shfl_xor(l, 32, kWave);
-#pragma unroll
-  for (int f = 0; f < NG; ++f) {
-    low[f] += __shfl_xor(low[f], 16, kWave);
-    low[f] += __shfl_xor(low[f], 32, kWave);
-    if constexpr (OPV != kOpExact) low[f] = __builtin_fmaf(-kOffset<OPV>, one[f][0], low[f]);
-  }
-#pragma unroll
-  for (int j = 0; j < JV; ++j) o[j] += low[j * 16 / GR];
+  fold();
   const size_t part = (size_t)blockIdx.x * a.row_tiles * 16;
   if constexpr (!JOINED) {
     if (row0 + n >= a.R) return;

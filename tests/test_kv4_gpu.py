@@ -350,6 +350,43 @@ def test_many_sentences_of_very_different_lengths(lib):
     _check_attend(lib, 3, 1, 2, 1500, 40, 64, 32, F16, lens=[1500, 20, 333])
 
 
+@pytest.mark.parametrize("qstd", [0.2, 1.5])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("H,S", [(32, 520), (390, 1)])
+def test_sums_over_a_long_context_that_is_not_split(lib, H, S, dtype, qstd):
+    """Results shrink as slots average out, and what the codes' offsets add up to does not: errors against the results' own size, at
+    calls of so many workgroups that one wave (prompts), or four (single tokens), sum a row's whole context.
+
+    16-bit results: rounding the exact ones is an error r, and the sums may add a quarter of that, independent of it: sqrt(1 + 1/16) r.
+    fp32: the codes' 7.5 on average and the lowest values below them cancel, which 4 steps of 32 slots hold until they are put
+    together; there they are up to 30 times what the slots' values come to at random, in four roundings of 2^-24 / 2: 3.6e-6, twice that
+    allowed, and 2^-20 for logits and probabilities."""
+    T, D, group = 16384, 64, 64
+    g = torch.Generator(device=DEV)
+    g.manual_seed(H + S)
+    rand = lambda *shape: torch.randn(*shape, generator=g, device=DEV).to(dtype)  # noqa: E731
+    cache = _dirty(lib.kv4_cache(1, H, T, D, group, weights=False, device=DEV))
+    k, v = rand(1, T, H, D), rand(1, T, H, D)
+    lib.kv4_append(cache, k, v, _ints(T))
+    q = (qstd * torch.randn(1, S, H, D, generator=g, device=DEV)).to(dtype)
+    out = lib.kv4_attend(q, cache, _ints(T))
+    got, want = [], []
+    for h in np.linspace(0, H - 1, 2 if S > 1 else 8).astype(int):
+        hk, hv = (orc.held_values(f64(t[0, :, h]), group) for t in (k, v))
+        for s in sorted({0, 1, S // 3, S // 2, S - 9, S - 1} & set(range(S))):
+            n = T - S + s + 1
+            z = D ** -0.5 * (hk[:n] @ f64(q[0, s, h]))
+            p = np.exp(z - z.max())
+            want.append(p @ hv[:n] / p.sum())
+            got.append(f64(out[0, s, h]))
+    got, want = np.array(got), np.array(want)
+    rms = lambda t: np.sqrt(np.mean(t ** 2))  # noqa: E731
+    rounding = rms(f64(torch.from_numpy(want).to(dtype)) - want)
+    allowed = (7.2e-6 + 2.0 ** -20) * rms(want) if dtype == F32 else np.sqrt(1 + 1 / 16) * rounding
+    print(f"H {H} S {S} {dtype} qstd {qstd}: error {rms(got - want) / rms(want):.2e}, allowed {allowed / rms(want):.2e}, rounding {rounding / rms(want):.2e}")
+    assert rms(got - want) <= allowed
+
+
 # ----------------------------------------------------------------------------------------------------- eviction
 
 def _check_evict(lib, B, H, T, D, group, budget, recent, lens=None, weight=None, pos=None, nxt=None, alias=True, max_len=None,
