@@ -38,24 +38,18 @@ static PyObject* ffn_decode(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   return PyLong_FromLong(status);
 }
 
-/* The 4-bit operators' calls: their C arguments in order, addresses and numbers alike as integers (or None), three element strides one
- * by one.  Everything fits long long; scale is a float. */
-static int values(const char* name, PyObject* const* a, Py_ssize_t n, Py_ssize_t want, long long* v) {
+/* The 4-bit operators' calls: their C arguments in order, three element strides one by one.  kinds, a letter an argument: p an address (an
+ * integer, or None for NULL), i an integer, f a float, which is left out of v. */
+static int values(const char* name, PyObject* const* a, Py_ssize_t n, const char* kinds, long long* v) {
   Py_ssize_t i;
-  if (n != want) {
-    PyErr_Format(PyExc_TypeError, "%s: %zd arguments", name, want);
+  if (n != (Py_ssize_t)strlen(kinds)) {
+    PyErr_Format(PyExc_TypeError, "%s: %zd arguments", name, (Py_ssize_t)strlen(kinds));
     return 0;
   }
   for (i = 0; i < n; ++i) {
-    if (a[i] == Py_None) {
-      v[i] = 0;
-    } else if (PyFloat_Check(a[i])) {
-      const double d = PyFloat_AS_DOUBLE(a[i]);
-      memcpy(&v[i], &d, sizeof d);
-    } else {
-      v[i] = PyLong_AsLongLong(a[i]);
-      if (v[i] == -1 && PyErr_Occurred()) return 0;
-    }
+    v[i] = 0;
+    if (kinds[i] == 'f' || (kinds[i] == 'p' && a[i] == Py_None)) continue;
+    if (!number(a[i], &v[i])) return 0;
   }
   return 1;
 }
@@ -67,7 +61,7 @@ static PyObject* w4_matvec(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   long long v[18];
   int status;
   (void)self;
-  if (!values("w4_matvec", a, n, 18, v)) return NULL;
+  if (!values("w4_matvec", a, n, "piiipppiiiiipiipip", v)) return NULL;
   Py_BEGIN_ALLOW_THREADS
   status = coreinfer_w4_matvec(P(0), v[1], v[2], I(3), P(4), P(5), P(6), I(7), I(8), v[9], v[10], I(11), P(12), v[13], I(14), P(15),
                                (size_t)v[16], P(17));
@@ -81,7 +75,7 @@ static PyObject* kv4_append(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   int64_t stride[3];
   int status;
   (void)self;
-  if (!values("kv4_append", a, n, 12, v)) return NULL;
+  if (!values("kv4_append", a, n, "pppiiiiipppp", v)) return NULL;
   stride[0] = v[4];
   stride[1] = v[5];
   stride[2] = v[6];
@@ -97,7 +91,7 @@ static PyObject* kv4_read(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   long long v[8];
   int status;
   (void)self;
-  if (!values("kv4_read", a, n, 8, v)) return NULL;
+  if (!values("kv4_read", a, n, "ppiippip", v)) return NULL;
   Py_BEGIN_ALLOW_THREADS
   status = coreinfer_kv4_read((const ci_kv4*)P(0), (const int32_t*)P(1), v[2], v[3], P(4), P(5), I(6), P(7));
   Py_END_ALLOW_THREADS
@@ -111,12 +105,9 @@ static PyObject* kv4_attend(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   double scale;
   int status;
   (void)self;
-  if (!values("kv4_attend", a, n, 17, v)) return NULL;
-  if (!PyFloat_Check(a[8])) {
-    PyErr_SetString(PyExc_TypeError, "kv4_attend: scale is a float");
-    return NULL;
-  }
-  memcpy(&scale, &v[8], sizeof scale);
+  if (!values("kv4_attend", a, n, "ppiiiiiifpippppip", v)) return NULL;
+  scale = PyFloat_AsDouble(a[8]);
+  if (scale == -1.0 && PyErr_Occurred()) return NULL;
   stride[0] = v[4];
   stride[1] = v[5];
   stride[2] = v[6];
@@ -132,7 +123,7 @@ static PyObject* kv4_evict(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   long long v[12];
   int status;
   (void)self;
-  if (!values("kv4_evict", a, n, 12, v)) return NULL;
+  if (!values("kv4_evict", a, n, "pppiiippppip", v)) return NULL;
   Py_BEGIN_ALLOW_THREADS
   status = coreinfer_kv4_evict((const ci_kv4*)P(0), (const int32_t*)P(1), (const int32_t*)P(2), v[3], v[4], v[5], (float*)P(6),
                                (int32_t*)P(7), (int32_t*)P(8), P(9), (size_t)v[10], P(11));

@@ -166,3 +166,20 @@ def test_python_binding_refuses_what_the_kernels_would_misread(lib):
         lib.w4_quantize(torch.zeros(16, 128), 64, packed=torch.zeros(8, dtype=torch.uint8))
     with pytest.raises(lib.CoreInferError):
         lib.kv4_cache(1, 2, 33, 64, 32, device="cpu")
+
+
+def test_the_per_token_calls_take_no_float_or_nothing_for_a_number(lib):
+    """The bits of a float, or 0 for None, are none of the sizes and addresses: refused before the library is called, with the C module
+    and through ctypes alike.  Every other argument is one that the library refuses by itself."""
+    calls = [   # p an address or None, i an integer, f a float
+        (lib._w4_matvec_call, "piiipppiiiiipiipip"), (lib._kv4_append_call, "pppiiiiipppp"), (lib._kv4_read_call, "ppiippip"),
+        (lib._kv4_attend_call, "ppiiiiiifpippppip"), (lib._kv4_evict_call, "pppiiippppip")]
+    for call, kinds in calls:
+        good = [{"p": None, "i": 0, "f": 1.0}[k] for k in kinds]
+        assert call(*good) == lib.CI_ERR_INVALID_ARG
+        for i, kind in enumerate(kinds):
+            for bad in {"p": (0.0, 1.5), "i": (0.0, 1.5, "1", None), "f": ("1", None)}[kind]:
+                with pytest.raises((TypeError, ctypes.ArgumentError)):
+                    call(*good[:i], bad, *good[i + 1:])
+        with pytest.raises(TypeError):
+            call(*good[:-1])
