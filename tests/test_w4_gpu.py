@@ -213,3 +213,21 @@ def test_fp32_results_of_16_bit_rows_keep_their_bits(lib, group, dtype, M):
     narrow, wide = (rms(f64(lib.w4_matvec(t, pw, out_dtype=F32)) - want) / rms(want) for t in (x, x.float()))
     print(f"group {group} {dtype} M {M}: error {narrow:.2e}, of the same rows in fp32 {wide:.2e}")
     assert wide <= 2.0 ** -20 and narrow <= 4 * wide
+
+
+@pytest.mark.parametrize("M,R,C,group,act,dtype", [
+    (8, 64, 6554, 64, "relu", F16), (8, 40, 6554, 128, "swiglu", BF16),       # an even number of core neurons
+    (16, 40, 4098, 128, "none", BF16), (9, 33, 4102, 32, "relu", F16), (16, 17, 2054, 64, "none", F16),
+    (2, 24, 20006, 64, "none", BF16), (1, 24, 33002, 128, "none", F16), (16, 14410, 2050, 64, "relu", BF16)])
+def test_rows_read_as_they_are_that_end_inside_a_piece(lib, M, R, C, group, act, dtype):
+    """16-bit rows past the LDS whose length is no multiple of the eight elements of a load: what follows a row, another one or the
+    end of them all, is no part of it, NaN or not; rows that are not even are laid out instead."""
+    _check(lib, M, R, C, group, act, dtype, seed=11)
+    _check(lib, M, R, C - 1, group, act, dtype, seed=12)
+    for gap in (2, 6, 8, 130):
+        base = torch.full((M, C + gap), float("nan"), dtype=dtype, device=DEV)
+        for first in (0, 2):
+            x = base[:, first:first + C]
+            x.copy_(_rand((M, C), dtype, 13))
+            _check(lib, M, R, C, group, act, dtype, seed=13, x=x)
+            base.fill_(float("nan"))
