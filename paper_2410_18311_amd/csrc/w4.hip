@@ -401,10 +401,9 @@ int launch_few(const RowsArgs& a, hipStream_t s) {
   while (waves < MOST && groups * waves < 2000 && waves * 2 <= a.nb) waves *= 2;
   if constexpr (DUAL) {
     return waves == 4 ? launch_rows<D, G, 2, 1, true, X, 256, ROWS>(a, waves, s) : launch_rows<D, G, 2, 1, true, X, MOST * 64, ROWS>(a, waves, s);
-  } else if (X == kXRows && RT == 2) {
-    return launch_rows<D, G, 4, 1, false, X, 512, ROWS>(a, 8, s);   // rows this long are more than eight blocks
   } else if (RT == 2) {
-    return launch_rows<D, G, 2, 1, false, X, 512, ROWS>(a, waves, s);   // never more than eight waves
+    if constexpr (X == kXRows) return launch_rows<D, G, 4, 1, false, X, 512, ROWS>(a, 8, s);   // rows this long are more than eight blocks
+    else return launch_rows<D, G, 2, 1, false, X, 512, ROWS>(a, waves, s);   // never more than eight waves
   } else {
     return waves == 4 ? launch_rows<D, G, 1, 1, false, X, 256, ROWS>(a, waves, s) : launch_rows<D, G, 1, 1, false, X, MOST * 64, ROWS>(a, waves, s);
   }

@@ -183,3 +183,18 @@ def test_the_per_token_calls_take_no_float_or_nothing_for_a_number(lib):
                     call(*good[:i], bad, *good[i + 1:])
         with pytest.raises(TypeError):
             call(*good[:-1])
+
+
+def test_no_kernel_is_built_that_no_call_launches(lib):
+    """Four tiles of weights a workgroup go with rows of x in memory and with nothing else; rows move in the launch that plans them only with the
+    keys in the LDS."""
+    import re
+    from paper_2410_18311_amd import build
+    with open(build.LIB_PATH, "rb") as f:
+        data = f.read()
+    rows = set(re.findall(rb"gemm_q4_rows_kernelINS_\d\w+?ELi\d+ELi(\d)ELi(\d)ELb(\d)ELi(\d)ELi(\d+)ELi(\d)EE", data))
+    assert {(t, x) for t, _, _, x, _, _ in rows} == {(b"1", b"0"), (b"2", b"0"), (b"4", b"0"), (b"1", b"1"), (b"2", b"1"), (b"2", b"2")}
+    assert not {dual for t, _, dual, x, _, _ in rows if (t, x) == (b"2", b"0")} & {b"0"}      # pairs there are pairs of up and gate
+    plans = set(re.findall(rb"kv4_plan_kernelILi(\d+)ELb(\d)ELi\d+ELi\d+ELb(\d)ELb(\d)EE", data))
+    assert plans == {(b"256", b"1", b"1", b"1"), (b"1024", b"1", b"1", b"1"), (b"256", b"1", b"1", b"0"), (b"1024", b"1", b"1", b"0"),
+                     (b"256", b"1", b"0", b"0"), (b"1024", b"1", b"0", b"0"), (b"1024", b"0", b"0", b"0")}
