@@ -497,8 +497,11 @@ int coreinfer_w4_read(const void* packed, int64_t R, int64_t C, int group, void*
  * as it is, fp32 x in three bf16 pieces (24 bits); sums in fp32, in a fixed order,
  * for 16-bit x of the codes plus 16 (1.4 of the 24 bits are the 16's).
  * A row of x with an infinity or a NaN gives NaN.  y must not overlap x.
- * ws: coreinfer_w4_matvec_workspace_size bytes, 16-byte aligned; NULL where
- * that is 0 (one row, and as many as fit 64 KB).
+ * ws: coreinfer_w4_matvec_workspace_size bytes, 16-byte aligned; NULL where that is
+ * 0: up to 16 rows of 64 KB together, at 2 bytes an element (fp32: 6) of rows filled up to
+ * 128s (one row: C <= 32768, fp32 10880).  The size is asked of longer 16-bit rows too, but
+ * up to 16 of them leave it alone where x, C and ldx are whole words, ldx <= 2^26 and
+ * (M - 1) ldx + C < 2^29.
  */
 int coreinfer_w4_matvec_workspace_size(int64_t M, int64_t C, int x_dtype, size_t* bytes);
 int coreinfer_w4_matvec(const void* x, int64_t M, int64_t ldx, int x_dtype, const void* w, const void* gate,

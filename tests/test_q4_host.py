@@ -55,6 +55,20 @@ def test_w4_matvec_refuses(lib):
         assert _matvec(lib, **kw) == lib.CI_ERR_WORKSPACE, kw
 
 
+def test_which_rows_need_a_workspace(lib):
+    """None while the operands of up to 16 rows, filled up to 128 columns, fit 64 KB; one row of hidden values may be too long for that."""
+    size = lambda M, C, dt: _size(lib.raw.coreinfer_w4_matvec_workspace_size, M, C, dt)  # noqa: E731
+    for dt, e in ((lib.CI_F16, 2), (lib.CI_BF16, 2), (lib.CI_F32, 6)):
+        for M in (1, 2, 3, 8, 16):
+            most = 65536 // (e * M) // 128 * 128
+            assert size(M, most, dt) == (0, 0)
+            assert size(M, most + 1, dt) == (0, 16 * (most + 128) * e)
+        assert size(17, 1, dt) == (0, 32 * 128 * e) and size(33, 129, dt) == (0, 64 * 256 * e)
+    assert size(1, 10880, lib.CI_F32) == size(1, 32768, lib.CI_F16) == (0, 0)
+    for kw in (dict(C=10881, xd=0), dict(C=32769, xd=1), dict(C=32769, xd=2)):
+        assert _matvec(lib, ldx=kw["C"], ws=None, wb=0, **kw) == lib.CI_ERR_WORKSPACE, kw
+
+
 def _cache(lib, **kw):
     f = dict(k=F, v=F, k_scale=F, v_scale=F, weight=F, pos=F, B=2, H=3, cap=64, D=128, group=64)
     f.update(kw)
