@@ -564,7 +564,7 @@ int coreinfer_kv4_read(const ci_kv4* cache, const int32_t* lens, int64_t first, 
  *   weight_out [B, H, cap] fp32 or NULL: cache->weight plus, for every slot t <
  *       lens[b], the p_t of all rows and heads that read it; other slots are left as
  *       they are.  May be cache->weight itself, which must not be NULL then.
- * scale > 0 and finite.  Softmax statistics and sums in fp32; keys and values enter
+ * scale > 0 and finite, also times log2(e).  Softmax statistics and sums in fp32; keys and values enter
  * as they are held, q as it is (fp32 q in three bf16 pieces), probabilities in
  * two bf16 pieces (fp32 q: three).  The order of the sums is fixed.
  * ws: coreinfer_kv4_attend_workspace_size bytes, 16-byte aligned (weights != 0: for

@@ -146,7 +146,7 @@ int coreinfer_kv4_attend(const ci_kv4* cache, const void* q, int64_t S, int64_t 
   rc = coreinfer_kv4_attend_workspace_size(cache->B, cache->H, cache->D, S, Hq, max_len, weight_out != nullptr, &need);
   if (rc != CI_OK) return rc;
   if (!q || !stride || !lens || !out || max_len > cache->cap || (weight_out && !cache->weight)) return CI_ERR_INVALID_ARG;
-  if (!(scale > 0.0f) || !isfinite(scale)) return CI_ERR_INVALID_ARG;
+  if (!(scale > 0.0f) || !isfinite(scale * 1.442695041f)) return CI_ERR_INVALID_ARG;   // the kernels multiply by scale log2(e)
   if (!strides_ok(stride) || !elem_aligned(q, dtype) || !aligned16(out) || !word_aligned(lens) || !word_aligned(lse) ||
       !word_aligned(weight_out))
     return CI_ERR_BAD_LAYOUT;

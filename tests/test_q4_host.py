@@ -212,3 +212,11 @@ def test_no_kernel_is_built_that_no_call_launches(lib):
     plans = set(re.findall(rb"kv4_plan_kernelILi(\d+)ELb(\d)ELi\d+ELi\d+ELb(\d)ELb(\d)EE", data))
     assert plans == {(b"256", b"1", b"1", b"1"), (b"1024", b"1", b"1", b"1"), (b"256", b"1", b"1", b"0"), (b"1024", b"1", b"1", b"0"),
                      (b"256", b"1", b"0", b"0"), (b"1024", b"1", b"0", b"0"), (b"1024", b"0", b"0", b"0")}
+
+
+def test_attention_refuses_a_scale_that_overflows_in_base_2(lib):
+    """Times log2(e), which is what multiplies the logits, it would be infinite, and a logit of 0 a NaN."""
+    call, c = _calls(lib)["attend"], _cache(lib)
+    for scale in (2.4e38, 3.4e38):
+        assert call(c, scale=scale) == lib.CI_ERR_INVALID_ARG
+    assert call(c, scale=2.3e38, ws=None) == lib.CI_ERR_WORKSPACE   # which is looked at after the scale
