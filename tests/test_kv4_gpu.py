@@ -387,6 +387,25 @@ def test_sums_over_a_long_context_that_is_not_split(lib, H, S, dtype, qstd):
     assert rms(got - want) <= allowed
 
 
+@pytest.mark.parametrize("D,group", [(128, 64), (128, 128), (64, 32)])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("S", [1, 40])
+def test_weights_of_16_bit_queries_keep_their_bits(lib, S, dtype, D, group):
+    """The fp32 weights that the slots get.  Logits of 16-bit queries multiply codes with an offset of 16, sums of about 24 instead of 9 where
+    the same queries in fp32 multiply the codes, and that is one part of a probability's error: at most 24 / 9 of it."""
+    T, H = 2048, 4
+    cache, k, v = _filled(lib, 1, H, T, D, group, dtype, 7)
+    q = _rand((1, S, H, D), dtype, 9)
+    _, _, want = orc.attend(f64(q), k, v, [T], D ** -0.5)
+    err = []
+    for x in (q, q.float()):
+        cache.weight.zero_()
+        lib.kv4_attend(x, cache, _ints(T), weight_out=cache.weight)
+        err.append(np.sqrt(np.mean(((f64(cache.weight) - want) / want) ** 2)))
+    print(f"S {S} {dtype} {D} {group}: error {err[0]:.2e}, of the same queries in fp32 {err[1]:.2e}")
+    assert err[1] <= 2.0 ** -20 and err[0] <= 24 / 9 * err[1]
+
+
 # ----------------------------------------------------------------------------------------------------- eviction
 
 def _check_evict(lib, B, H, T, D, group, budget, recent, lens=None, weight=None, pos=None, nxt=None, alias=True, max_len=None,
