@@ -1,6 +1,7 @@
 // Writing keys and values to a cache in 4 bits, reading them back, and evicting the slots that got the least weight (kv4.hpp).
-// Reading is bound by its bytes (8 x 40 heads x 1024 slots, 220 MB: 46 us, 4.8 TB/s); writing by the packing's instructions from a few
-// hundred tokens on (1023 tokens of 32 heads 12.4 us), and by latency below (one token of 8 x 72 heads 4.0 us); eviction by the chain of barriers
+// Reading is bound by its bytes (8 x 40 heads x 1024 slots, 220 MB: 46 us, 4.8 TB/s); writing from a few hundred tokens on by the packing's
+// instructions, about half of it, and by the rows' latency (1023 tokens of 32 heads 12.3 us, 6.4 of them instructions; four waves a SIMD, which
+// wait in half of their cycles), and by latency alone below (one token of 8 x 72 heads 4.0 us); eviction by the chain of barriers
 // in which a head's slots are chosen (one of 1025 slots 6 us with its move, 6144 of 8192 21 us and 18 for the moves).
 #include <algorithm>
 #include <type_traits>

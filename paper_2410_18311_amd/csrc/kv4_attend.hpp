@@ -12,9 +12,10 @@
 //
 // Few rows: the waves of a workgroup take different steps and their sums are joined, and the slots of all sentences are shared out by length
 // over three workgroups a compute unit, joined by a second launch.  Bound by the cache's bytes: eight sentences of up to 65536 slots,
-// 259 MB, 56 us and 7 of the join (4.6 TB/s); where there are few of them by two launches' latency: 4096 slots of 40 heads 12 and 5 us.
-// Many rows: the waves take different tiles and share a step's operands.  Bound by vector instructions, 27 a logit and row: 512 rows over 2048 slots of 32
-// heads 58 us, and 28 for the slots' weights, for which the logits are computed again.
+// 259 MB, 57 us and 7 of the join (4.5 TB/s); where there are few of them by two launches' latency: 4096 slots of 40 heads 13 and 5 us.
+// Many rows: the waves take different tiles and share a step's operands.  512 rows over 2048 slots of 32 heads 58 us, of which vector
+// instructions, 28 a logit and row, are 27, operands from the LDS (16 KB a wave and step) up to 22 and matrix products 11: side by side only in part, and
+// the waves, three a SIMD, wait in 29 % of their cycles.  27 us for the slots' weights, for which the logits are computed again.
 #pragma once
 
 #include "kv4.hpp"

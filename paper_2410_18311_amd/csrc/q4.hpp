@@ -124,8 +124,9 @@ __device__ __forceinline__ uint32_t q4_code(float x, uint32_t scale) {
   const float n = rintf((x - half_hi(scale)) / step);
   return (uint32_t)fminf(fmaxf(n, 0.0f), 15.0f);
 }
-// The codes of eight elements of a group.  A product with the reciprocal is within 2^-20 of the quotient for what counts (up to 16), so only
-// where it lies that close to the middle between two codes do the divisions decide; a fifth of the instructions otherwise.
+// The codes of eight elements of a group.  A product with the reciprocal differs from the quotient by the reciprocal's 2^-23, the product's 2^-24
+// and the quotient's own 2^-24, 2^-22 of it together: at most 2^-18 = 3.8e-6 for what counts (up to 16).  Only where it lies within twice that of the
+// middle between two codes do the divisions decide; a fifth of the instructions otherwise.
 __device__ __forceinline__ void q4_codes(const float (&x)[8], uint32_t scale, uint32_t (&n)[8]) {
   const float step = half_lo(scale), low = half_hi(scale), inv = __builtin_amdgcn_rcpf(step);
   bool close = false;

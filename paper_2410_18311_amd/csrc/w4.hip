@@ -1,9 +1,10 @@
 // Products of one to 64 rows with 4-bit weights (q4.hpp): y = act(W x + b), or SiLU(G x) * (U x).  The projections of a decode step and the
 // up, gate and down matrices of deployed core neurons; a token reads 0.28 of the bytes of 16-bit weights (groups of 64).
 //
-// Bound by those bytes where there are enough of them: a gated 13824 x 5120 product of one row, 80 MB, 15.1 us (5.3 TB/s, a large
-// copy's rate); 14746 x 9216 of eight rows, 77 MB, 17.2 us.  Small ones are bound by latency: 4096 x 6554 (14 MB) 7.2 us, 1024 x 256 4.2 us.
-// From 32 rows on by what is read of x: 64 rows of the gated product 63 us.
+// Bound by those bytes where there are enough of them: a gated 13824 x 5120 product of one row, 80 MB, 15.2 us with two sets of weights by turns
+// (5.2 TB/s, a large copy's rate; the memory-side cache has a part), 16.1 with three; 14746 x 9216 of eight rows, 77 MB, 17.4 us.  Small ones
+// are bound by latency: 4096 x 6554 (14 MB) 7.2 us, 1024 x 256 4.2 us.  Above 16 rows by what is read of x from the L2, all of it in every
+// workgroup: 64 rows of the gated product 64 us.
 //
 // Layout.  Rows by 16 and columns by 128 make a block of 1 KB, which a wave loads with one instruction: lane 16 g + n holds row n, word j
 // the columns 32 j + 8 g .. + 7, so that the word is the matrix cores' operand (16 rows, 32 columns) once its codes are unpacked and
