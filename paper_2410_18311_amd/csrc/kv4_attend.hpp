@@ -663,9 +663,9 @@ __global__ __launch_bounds__(256) void gemm_q4_weights_kernel(Kv4Attend a) {
   __shared__ uint4 tile_of_q[2][JK][V][64];
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int heads = a.c.B * a.c.H, bh = blockIdx.x % heads, b = bh / a.c.H, h = bh % a.c.H;   // heads fastest: a head's rows stay in one L2
+  const int bh = blockIdx.x, b = bh / a.c.H, h = bh % a.c.H;   // heads fastest: a head's rows stay in one L2
   const int len = min(max(a.lens[b], 0), a.max_len);
-  const int t_block = (int)(blockIdx.x / heads) * 128, t0 = t_block + wave * 32;
+  const int t_block = (int)(blockIdx.z * gridDim.y + blockIdx.y) * 128, t0 = t_block + wave * 32;
   if (t_block >= len) return;   // the whole workgroup; t0 + 32 may pass len, but not a multiple of 32 that holds it, so not the capacity
   const bool idle = t0 >= len;
   const Q4Magic mk = q4_magic<OP>();
@@ -748,8 +748,11 @@ int launch_attend(const Kv4Attend& a, hipStream_t s) {
     CI_HIP_CHECK_LAUNCH();
   }
   if (a.weights == 2) {
-    hipLaunchKernelGGL((gemm_q4_weights_kernel<T, D, GR>), dim3((uint32_t)(a.c.B * a.c.H) * ((a.max_len + 127) / 128)), dim3(256), 0,
-                       s, a);
+    // up to 2^16 heads and 2^17 workgroups along the slots: together more threads than one dimension of a launch may have, of which the rest
+    // would be left out without an error
+    const uint32_t along = (uint32_t)(a.max_len + 127) / 128, most = 32768;
+    hipLaunchKernelGGL((gemm_q4_weights_kernel<T, D, GR>), dim3(a.c.B * a.c.H, along < most ? along : most, (along + most - 1) / most), dim3(256),
+                       0, s, a);
     CI_HIP_CHECK_LAUNCH();
   }
   return CI_OK;

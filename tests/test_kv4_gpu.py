@@ -406,6 +406,24 @@ def test_weights_of_16_bit_queries_keep_their_bits(lib, S, dtype, D, group):
     assert err[1] <= 2.0 ** -20 and err[0] <= 24 / 9 * err[1]
 
 
+def test_weights_of_many_rows_of_more_than_2_to_the_31_slots(lib):
+    """A workgroup has 128 slots of a head: more threads than 32 bits count.  All slots are alike, so each row gives every one that it sees
+    the same weight."""
+    H, cap, D, group, S = 129, 16777216, 64, 64, 20
+    if torch.cuda.mem_get_info()[0] < 190 << 30:
+        pytest.skip("180 GB of device memory are not free")
+    cache = lib.kv4_cache(1, H, cap, D, group, device=DEV)
+    for t in (cache.k, cache.v, cache.k_scale, cache.v_scale):
+        t.zero_()
+    lib.kv4_attend(_rand((1, S, H, D), F16, 3), cache, _ints(cap), weight_out=cache.weight)
+    rows = torch.full((cap,), float(S), device=DEV)
+    rows[cap - S:] = torch.arange(S, 0, -1, device=DEV)
+    off = max((cache.weight[0, h] * cap - rows).abs().max().item() for h in range(H))
+    del cache
+    torch.cuda.empty_cache()
+    assert off <= S * 2.0 ** -16      # log-sums of 24: 2^-20 of each of S weights, and rows that see up to 20 slots fewer
+
+
 # ----------------------------------------------------------------------------------------------------- eviction
 
 def _check_evict(lib, B, H, T, D, group, budget, recent, lens=None, weight=None, pos=None, nxt=None, alias=True, max_len=None,
