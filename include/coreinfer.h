@@ -600,6 +600,130 @@ int coreinfer_kv4_evict(const ci_kv4* cache, const int32_t* lens, const int32_t*
                         int64_t recent, float* weight_out, int32_t* pos_out, int32_t* lens_out, void* ws,
                         size_t ws_bytes, void* stream);
 
+/*
+ * ---------------------------------------------------------------------------
+ * Serving from a cache in pages, in the layer's own type, for packed batches.
+ *
+ * The new tokens of B sentences are T rows one behind the other: those of sentence b
+ * are the rows first[b] .. first[b + 1] - 1 (first [B + 1] int32 on the device,
+ * ascending from 0), so that a prompt's chunk and other sentences' single tokens
+ * go together; a sentence may have none.  lens [B] int32 on the device: a sentence's
+ * slots in use, its new tokens included, which are its last ones: row i of n is in slot
+ * lens[b] - n + i.  Rows from first[B] on belong to no sentence: what they would
+ * write stays as it is.  Entries of first outside 0 .. T are taken as its ends.
+ * Strides are in elements, of a row (token) and of a head; a head's channels are
+ * contiguous.  T = 0 is CI_OK and does nothing (no pointer is looked at).
+ * ---------------------------------------------------------------------------
+ */
+#define CI_MAX_PACKED_ROWS 1048576 /* T                     */
+#define CI_MAX_ROPE_CHANNELS 512   /* D of coreinfer_rope   */
+
+/*
+ * Rotary positions.  Of a head's D channels the first `rot` are turned, in pairs
+ * i = 0 .. rot / 2 - 1 of the channels
+ *     CI_ROPE_HALF          i and i + rot / 2,
+ *     CI_ROPE_INTERLEAVED   2 i and 2 i + 1,
+ * a pair (a, c) at position p becomes scale (a cos - c sin, c cos + a sin) of the angle
+ * 2 pi turns[i] p / 2^64.  In whole 2^-64ths of a turn an angle is exact at every
+ * position, however far.  The other channels stay as they are.
+ */
+typedef enum { CI_ROPE_HALF = 0, CI_ROPE_INTERLEAVED = 1 } ci_rope_style;
+typedef struct {
+  const uint64_t* turns; /* [rot / 2] device, 8-byte aligned; NULL where rot is 0 */
+  float scale;           /* of the turned channels, finite                        */
+  int32_t rot;           /* even, 0 .. D; 0 turns nothing                         */
+  int32_t style;
+} ci_rope;
+
+/*
+ * turns [rot / 2] (HOST array) of the frequencies f_i = base^(-2 i / rot) radians a
+ * position (Su et al. 2021), or of those scaled for a context `factor` times as long:
+ *     CI_ROPE_LINEAR  f_i / factor (positions are squeezed)
+ *     CI_ROPE_BASE    base factor^(rot / (rot - 2)) in the place of base (the slowest pair is squeezed, the
+ *                     fastest stays)
+ *     CI_ROPE_PARTS   f_i (g + (1 - g) / factor), g = (original f_i / (2 pi) - slow) /
+ *                     (fast - slow) within 0 .. 1: pairs that turn more than `fast` times in the
+ *                     `original` context stay, those below `slow` are squeezed (Peng et al.
+ *                     2023, who also scale by 0.1 ln(factor) + 1: ci_rope's scale)
+ * Host-only.  rot even, 2 .. 512; base > 0; factor > 0 (not looked at for CI_ROPE_PLAIN);
+ * original > 0 and fast > slow for CI_ROPE_PARTS only; everything finite.
+ */
+typedef enum { CI_ROPE_PLAIN = 0, CI_ROPE_LINEAR = 1, CI_ROPE_BASE = 2, CI_ROPE_PARTS = 3 } ci_rope_scaling;
+int coreinfer_rope_turns(int64_t rot, double base, int scaling, double factor, double original, double fast, double slow,
+                         uint64_t* turns);
+
+/*
+ * y = x [T, H, D] normed by head and turned by its positions, in one pass:
+ *   norm [D] of `dtype` or NULL: n = x / sqrt(mean over the head of x^2 + eps) norm, eps >= 0;
+ *   then rope (NULL: nothing is turned) at positions pos [T] int32 (may be negative;
+ *   NULL where nothing is turned).
+ * backward != 0: the angles' signs are turned, which is the gradient (the transpose) of
+ * the rotation and, up to scale^2, its inverse; with a norm CI_ERR_INVALID_ARG.
+ * Everything in fp32, rounded once.  y (any strides) may be x itself with x's strides, and must not
+ * overlap it otherwise.  x and y are aligned to their elements; it is fastest
+ * where they and norm are aligned to 16 bytes, strides included, and D and rot are multiples of 32 bytes.
+ * 1 <= H <= 65535, 1 <= D <= CI_MAX_ROPE_CHANNELS.
+ */
+int coreinfer_rope(const void* x, const int64_t* stride, int64_t T, int64_t H, int64_t D, int dtype, const void* norm,
+                   float eps, const ci_rope* rope, const int32_t* pos, int backward, void* y, const int64_t* y_stride,
+                   void* stream);
+
+/*
+ * A layer's keys and values in pages of `page` slots (16, 32, 64, 128 or 256), H heads of
+ * D = 64 or 128 channels (other D or page: CI_ERR_UNSUPPORTED).  table [B, most]: slot t of
+ * sentence b is slot t % page of page table[b][t / page]; the caller gives pages
+ * out, and may give a page to several sentences that begin alike.  An entry outside 0 .. pages - 1
+ * is no page: nothing is written there and no row sees its slots.  The buffers need no
+ * initialisation: no result depends on what lies behind a sentence's last slot.
+ * most * page <= CI_MAX_CACHE_SLOTS, B * H <= 65535.
+ */
+typedef struct {
+  void* k;              /* [pages, H, page, D] of dtype, 16-byte aligned */
+  void* v;              /* the same                                      */
+  const int32_t* table; /* [B, most] device                              */
+  int64_t pages, most, B;
+  int32_t H, page, D, dtype;
+} ci_kvp;
+
+/*
+ * Writes the packed tokens' keys and values, k and v [T, H, D] of the cache's type (strides
+ * shared by both, e.g. slices of one fused projection), to their slots; slots that have no page, or outside
+ * 0 .. most * page - 1, are not written.  On the way the keys are normed by head
+ * (k_norm [D], NULL: not) and turned by their positions (rope, NULL: not), as
+ * coreinfer_rope does; pos [T] or NULL: a token's position is its slot.  q [T, Hq, D] (or NULL, with
+ * Hq = 0) goes the same way, with q_norm, to q_out [T, Hq, D] contiguous, 16-byte aligned, not
+ * overlapping q.  Values are copied.  No two tokens may go to the same slot.
+ */
+int coreinfer_kvp_append(const ci_kvp* cache, const void* k, const void* v, const int64_t* stride, int64_t T,
+                         const int32_t* first, const int32_t* lens, const int32_t* pos, const ci_rope* rope,
+                         const void* k_norm, float eps, const void* q, int64_t Hq, const int64_t* q_stride,
+                         const void* q_norm, void* q_out, void* stream);
+
+/*
+ * Attention of packed rows q [T, Hq, D] of the cache's type (Hq a multiple of H, query head
+ * i reads head i / (Hq / H)) over their sentences' slots:
+ *     out[r, i] = sum_t p_t v_t,   p = softmax over t of scale (q . k_t).
+ * The row in slot p sees the slots t <= p; with window > 0 of those only t > p - window
+ * and t < sinks.  A row that sees none gives zeros.  What it does not see, infinities and NaN
+ * included, does not touch it.
+ *   max_rows  the most rows of a sentence, max_len the most slots (<= most * page): they choose
+ *             and size the launches.  lens beyond 0 .. max_len are taken as its ends; rows
+ *             of a sentence from max_rows on are left as they are.
+ *   out [T, Hq, D] contiguous, 16-byte aligned, not overlapping q.
+ *   lse [T, Hq] fp32 or NULL: log of the sum of exp(scale q . k_t) (-infinity where nothing is seen).
+ * scale > 0 and finite, also times log2(e).  Softmax statistics and sums in fp32, in a fixed order.
+ * Probabilities enter the product with 16-bit values in two pieces of that type where few
+ * rows share a head, and rounded to it in prompts.
+ * ws: coreinfer_kvp_attend_workspace_size bytes, 16-byte aligned; NULL where that is 0.  Calls
+ * that share a workspace must not overlap in time.
+ * window, sinks >= 0.  Hq / H <= 4096, T * (Hq / H) <= 2^28.
+ */
+int coreinfer_kvp_attend_workspace_size(const ci_kvp* cache, int64_t T, int64_t Hq, int64_t max_rows, int64_t max_len,
+                                        int64_t window, int64_t sinks, size_t* bytes);
+int coreinfer_kvp_attend(const ci_kvp* cache, const void* q, int64_t Hq, const int64_t* stride, int64_t T,
+                         const int32_t* first, const int32_t* lens, int64_t max_rows, int64_t max_len, int64_t window,
+                         int64_t sinks, float scale, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -20,7 +20,7 @@ LIB_PATH = os.path.join(PKG_DIR, "libcoreinfer.so")
 # a Python module for this interpreter, linked against the library beside it
 BINDING_PATH = os.path.join(PKG_DIR, "_binding" + sysconfig.get_config_var("EXT_SUFFIX"))
 
-SOURCES = ["api.hip", "api4.hip", "kv4_attend_f32.hip", "kv4_attend_f16.hip", "kv4_attend_bf16.hip", "kv4_attend.hip", "kv4.hip", "w4.hip", "ffn_decode.hip", "ffn_decode_small.hip", "ffn_decode_fused.hip", "ffn_union.hip", "select.hip", "compact.hip", "centroid.hip", "gemv.hip", "gemm_mfma.hip", "gemm_f32.hip", "gemm_wide.hip", "gemm_mid.hip", "gemm_slim_f16.hip", "gemm_slim_bf16.hip", "stream_probe.hip"]
+SOURCES = ["kvp_attend_f32.hip", "kvp_attend_f16.hip", "kvp_attend_bf16.hip", "api.hip", "api4.hip", "api_pages.hip", "kvp_attend.hip", "rope.hip", "kv4_attend_f32.hip", "kv4_attend_f16.hip", "kv4_attend_bf16.hip", "kv4_attend.hip", "kv4.hip", "w4.hip", "ffn_decode.hip", "ffn_decode_small.hip", "ffn_decode_fused.hip", "ffn_union.hip", "select.hip", "compact.hip", "centroid.hip", "gemv.hip", "gemm_mfma.hip", "gemm_f32.hip", "gemm_wide.hip", "gemm_mid.hip", "gemm_slim_f16.hip", "gemm_slim_bf16.hip", "stream_probe.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

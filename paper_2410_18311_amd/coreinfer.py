@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import itertools
+import math
 import os
 from typing import Optional
 
@@ -53,6 +54,15 @@ class ci_ffn_weights(ctypes.Structure):
 class ci_kv4(ctypes.Structure):
     _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("weight", _vp), ("pos", _vp),
                 ("B", _i64), ("H", _i64), ("cap", _i64), ("D", ctypes.c_int32), ("group", ctypes.c_int32)]
+
+
+class ci_rope(ctypes.Structure):
+    _fields_ = [("turns", _vp), ("scale", ctypes.c_float), ("rot", ctypes.c_int32), ("style", ctypes.c_int32)]
+
+
+class ci_kvp(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("table", _vp), ("pages", _i64), ("most", _i64), ("B", _i64), ("H", ctypes.c_int32),
+                ("page", ctypes.c_int32), ("D", ctypes.c_int32), ("dtype", ctypes.c_int32)]
 
 
 _SIGNATURES = {
@@ -108,6 +118,14 @@ _SIGNATURES = {
                                     _vp, _vp, _vp, _vp, _sz, _vp]),
     "coreinfer_kv4_evict_workspace_size": (_int, [_i64, _i64, _i64, _i64, ctypes.POINTER(_sz)]),
     "coreinfer_kv4_evict": (_int, [ctypes.POINTER(ci_kv4), _vp, _vp, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "coreinfer_rope_turns": (_int, [_i64, _dbl, _int, _dbl, _dbl, _dbl, _dbl, _vp]),
+    "coreinfer_rope": (_int, [_vp, ctypes.POINTER(_i64), _i64, _i64, _i64, _int, _vp, ctypes.c_float, ctypes.POINTER(ci_rope), _vp, _int,
+                              _vp, ctypes.POINTER(_i64), _vp]),
+    "coreinfer_kvp_append": (_int, [ctypes.POINTER(ci_kvp), _vp, _vp, ctypes.POINTER(_i64), _i64, _vp, _vp, _vp,
+                                    ctypes.POINTER(ci_rope), _vp, ctypes.c_float, _vp, _i64, ctypes.POINTER(_i64), _vp, _vp, _vp]),
+    "coreinfer_kvp_attend_workspace_size": (_int, [ctypes.POINTER(ci_kvp), _i64, _i64, _i64, _i64, _i64, _i64, ctypes.POINTER(_sz)]),
+    "coreinfer_kvp_attend": (_int, [ctypes.POINTER(ci_kvp), _vp, _i64, ctypes.POINTER(_i64), _i64, _vp, _vp, _i64, _i64, _i64, _i64,
+                                    ctypes.c_float, _vp, _vp, _vp, _sz, _vp]),
 }
 for _name, (_res, _args) in _SIGNATURES.items():
     _f = getattr(_lib, _name)
@@ -121,6 +139,7 @@ if os.path.exists(BINDING_PATH):
     _decode_call = _binding.ffn_decode
     _w4_matvec_call, _kv4_append_call, _kv4_read_call = _binding.w4_matvec, _binding.kv4_append, _binding.kv4_read
     _kv4_attend_call, _kv4_evict_call = _binding.kv4_attend, _binding.kv4_evict
+    _rope_call, _kvp_append_call, _kvp_attend_call = _binding.rope, _binding.kvp_append, _binding.kvp_attend
 else:
     _binding = None
     _prototype = lambda name, *args: ctypes.CFUNCTYPE(_int, *args)((name, _lib))  # noqa: E731
@@ -135,6 +154,19 @@ else:
 
     def _kv4_attend_call(cache, q, S, Hq, s0, s1, s2, *rest):
         return _kv4_attend_c(cache, q, S, Hq, (_i64 * 3)(s0, s1, s2), *rest)
+
+    _rope_c, _kvp_append_c, _kvp_attend_c = (
+        _prototype(name, *(_vp if issubclass(t, ctypes._Pointer) and t is not ctypes.POINTER(_i64) else t for t in _SIGNATURES[name][1]))
+        for name in ("coreinfer_rope", "coreinfer_kvp_append", "coreinfer_kvp_attend"))
+
+    def _rope_call(x, s0, s1, T, H, D, dtype, norm, eps, angles, pos, backward, y, y0, y1, stream):
+        return _rope_c(x, (_i64 * 2)(s0, s1), T, H, D, dtype, norm, eps, angles, pos, backward, y, (_i64 * 2)(y0, y1), stream)
+
+    def _kvp_append_call(cache, k, v, s0, s1, T, first, lens, pos, angles, k_norm, eps, q, Hq, q0, q1, *rest):
+        return _kvp_append_c(cache, k, v, (_i64 * 2)(s0, s1), T, first, lens, pos, angles, k_norm, eps, q, Hq, (_i64 * 2)(q0, q1), *rest)
+
+    def _kvp_attend_call(cache, q, Hq, s0, s1, *rest):
+        return _kvp_attend_c(cache, q, Hq, (_i64 * 2)(s0, s1), *rest)
     _decode_call = ctypes.CFUNCTYPE(_int, _vp, _i64, _vp, _int, _int, _vp, _vp, _sz, _vp)(("coreinfer_ffn_decode", _lib))
 
 raw = _lib  # the bare C entry points, for tests of the error paths
@@ -856,3 +888,153 @@ def kv4_evict(cache: Kv4Cache, lens: torch.Tensor, next_pos: torch.Tensor, budge
                              _ptr(pos_out), lens_out.data_ptr(), ws.data_ptr(), ws.numel(), _stream(lens))
     if status != CI_OK:
         raise CoreInferError(status, "coreinfer_kv4_evict")
+
+
+CI_ROPE_HALF, CI_ROPE_INTERLEAVED = 0, 1
+ROPE_STYLE = {"half": CI_ROPE_HALF, "interleaved": CI_ROPE_INTERLEAVED}
+ROPE_SCALING = {"none": 0, "linear": 1, "base": 2, "parts": 3}
+
+
+class RopeAngles:
+    """Frequencies of rotary positions on the device (rope_angles)."""
+
+    def __init__(self, turns: torch.Tensor, scale: float, rot: int, style: str):
+        self.turns, self.scale, self.rot, self.style = turns, scale, rot, style
+        self.desc = ci_rope(_ptr(turns), scale, rot, ROPE_STYLE[style])
+        self.ptr = ctypes.addressof(self.desc)
+
+
+def rope_turns(rot: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, original: float = 0.0,
+               fast: float = 32.0, slow: float = 1.0) -> torch.Tensor:
+    """coreinfer_rope_turns: what each pair turns by a position, in 2^-64ths of a turn, [rot / 2] int64 (the bits of
+    uint64) on the host."""
+    turns = torch.empty(max(int(rot), 0) // 2, dtype=torch.int64)
+    _check(_lib.coreinfer_rope_turns(int(rot), float(base), ROPE_SCALING[scaling], float(factor), float(original), float(fast), float(slow),
+                                     _ptr(turns)), "coreinfer_rope_turns")
+    return turns
+
+
+def rope_angles(rot: int, base: float = 10000.0, style: str = "half", scaling: str = "none", factor: float = 1.0,
+                original: float = 0.0, fast: float = 32.0, slow: float = 1.0, scale: Optional[float] = None,
+                device="cuda") -> RopeAngles:
+    """Angles of the first `rot` channels of each head: pairs of channels rot / 2 apart ("half") or of neighbours
+    ("interleaved"); scaling "none", "linear", "base" or "parts" for a context `factor` times as long as `original`.  scale:
+    of the turned channels; by default 1, and 0.1 ln(factor) + 1 for "parts"."""
+    turns = rope_turns(rot, base, scaling, factor, original, fast, slow).to(device)
+    if scale is None:
+        scale = 0.1 * math.log(factor) + 1.0 if scaling == "parts" else 1.0
+    return RopeAngles(turns, float(scale), int(rot), style)
+
+
+def _check_norm(norm: Optional[torch.Tensor], D: int, dtype: torch.dtype):
+    assert norm is None or (norm.shape == (D,) and norm.dtype == dtype and norm.is_contiguous())
+
+
+def rope(x: torch.Tensor, pos: Optional[torch.Tensor], angles: Optional[RopeAngles], norm: Optional[torch.Tensor] = None,
+         eps: float = 1e-6, backward: bool = False, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """coreinfer_rope: x [T, H, D] (any strides, channels contiguous), normed by head with `norm` [D] and turned by the
+    positions pos [T] int32.  backward: the gradient of the rotation.  out: any strides; may be x."""
+    T, H, D = shape = x.shape
+    dtype = x.dtype
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=x.device)
+    s, o = x.stride(), out.stride()
+    assert s[2] == 1 and out.shape == shape and out.dtype == dtype and o[2] == 1
+    assert pos is None or (pos.dtype == torch.int32 and pos.shape == (T,) and pos.is_contiguous())
+    _check_norm(norm, D, dtype)
+    status = _rope_call(x.data_ptr(), s[0], s[1], T, H, D, DTYPE_CODE[dtype], _ptr(norm), float(eps),
+                        None if angles is None else angles.ptr, _ptr(pos), int(bool(backward)), out.data_ptr(), o[0], o[1], _stream(x))
+    if status != CI_OK:
+        raise CoreInferError(status, "coreinfer_rope")
+    return out
+
+
+class KvpCache:
+    """A layer's keys and values in pages (kvp_cache): k, v [pages, H, page, D], table [B, most]."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor):
+        assert k.dim() == 4 and v.shape == k.shape and v.dtype == k.dtype and k.is_contiguous() and v.is_contiguous()
+        assert table.dim() == 2 and table.dtype == torch.int32 and table.is_contiguous()
+        self.k, self.v, self.table, self.dtype = k, v, table, k.dtype
+        self.pages, self.H, self.page, self.D = k.shape
+        self.B, self.most = table.shape
+        self.desc = ci_kvp(_ptr(k), _ptr(v), _ptr(table), self.pages, self.most, self.B, self.H, self.page, self.D, DTYPE_CODE[k.dtype])
+        self.ptr = ctypes.addressof(self.desc)
+
+
+def kvp_cache(pages: int, H: int, page: int, D: int, dtype: torch.dtype, table: torch.Tensor) -> KvpCache:
+    """Buffers for `pages` pages of `page` slots (16, 32, 64, 128 or 256) of H heads of D channels, on the table's device.  table
+    [B, most] int32: the page of each sentence's slots page * i .. + page - 1 (-1: none yet); it is the caller's, who gives
+    pages out by writing to it."""
+    k, v = (torch.empty((pages, H, page, D), dtype=dtype, device=table.device) for _ in range(2))
+    return KvpCache(k, v, table)
+
+
+def _check_packed(cache: KvpCache, first: torch.Tensor, lens: torch.Tensor):
+    assert first.dtype == torch.int32 and first.shape == (cache.B + 1,) and first.is_contiguous()
+    assert lens.dtype == torch.int32 and lens.shape == (cache.B,) and lens.is_contiguous()
+
+
+def kvp_append(cache: KvpCache, k: torch.Tensor, v: torch.Tensor, first: torch.Tensor, lens: torch.Tensor,
+               angles: Optional[RopeAngles] = None, pos: Optional[torch.Tensor] = None, k_norm: Optional[torch.Tensor] = None,
+               eps: float = 1e-6, q: Optional[torch.Tensor] = None, q_norm: Optional[torch.Tensor] = None,
+               q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """coreinfer_kvp_append: the packed tokens' k, v [T, H, D] (the same strides, channels contiguous) to their slots, keys normed
+    and turned on the way; q [T, Hq, D] goes the same way to q_out, which is returned."""
+    T, H, D = shape = k.shape
+    dtype, s = k.dtype, k.stride()
+    assert v.shape == shape and v.dtype == dtype and v.stride() == s and s[2] == 1
+    assert (H, D, dtype) == (cache.H, cache.D, cache.dtype)
+    _check_packed(cache, first, lens)
+    assert pos is None or (pos.dtype == torch.int32 and pos.shape == (T,) and pos.is_contiguous())
+    _check_norm(k_norm, D, dtype)
+    _check_norm(q_norm, D, dtype)
+    Hq, qs = 0, (0, 0, 1)
+    if q is not None:
+        Hq, qs = q.shape[1], q.stride()
+        assert q.shape == (T, Hq, D) and q.dtype == dtype and qs[2] == 1
+        if q_out is None:
+            q_out = torch.empty((T, Hq, D), dtype=dtype, device=q.device)
+        assert q_out.shape == q.shape and q_out.dtype == dtype and q_out.is_contiguous()
+    else:
+        assert q_out is None and q_norm is None
+    status = _kvp_append_call(cache.ptr, k.data_ptr(), v.data_ptr(), s[0], s[1], T, first.data_ptr(), lens.data_ptr(), _ptr(pos),
+                              None if angles is None else angles.ptr, _ptr(k_norm), float(eps), _ptr(q), Hq, qs[0], qs[1], _ptr(q_norm),
+                              _ptr(q_out), _stream(k))
+    if status != CI_OK:
+        raise CoreInferError(status, "coreinfer_kvp_append")
+    return q_out
+
+
+def kvp_attend_workspace_size(cache: KvpCache, T: int, Hq: int, max_rows: int, max_len: int, window: int = 0, sinks: int = 0) -> int:
+    b = _sz(0)
+    _check(_lib.coreinfer_kvp_attend_workspace_size(ctypes.byref(cache.desc), T, Hq, max_rows, max_len, window, sinks, ctypes.byref(b)),
+           "coreinfer_kvp_attend_workspace_size")
+    return b.value
+
+
+def kvp_attend(q: torch.Tensor, cache: KvpCache, first: torch.Tensor, lens: torch.Tensor, max_rows: Optional[int] = None,
+               max_len: Optional[int] = None, window: int = 0, sinks: int = 0, scale: Optional[float] = None,
+               out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """coreinfer_kvp_attend: the packed rows q [T, Hq, D] over their sentences' pages, all that came before them or, with a
+    window, the last `window` slots and the first `sinks`.  max_rows, max_len: the most rows and slots of a sentence (all
+    rows and the table's slots by default; the launches are chosen and sized by them).  scale: 1 / sqrt(D) by default."""
+    T, Hq, D = shape = q.shape
+    dtype, s = q.dtype, q.stride()
+    assert (D, dtype) == (cache.D, cache.dtype) and s[2] == 1
+    _check_packed(cache, first, lens)
+    max_rows = max(T, 1) if max_rows is None else max_rows
+    max_len = cache.most * cache.page if max_len is None else max_len
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=q.device)
+    assert out.shape == shape and out.dtype == dtype and out.is_contiguous()
+    assert lse is None or (lse.shape == (T, Hq) and lse.dtype == torch.float32 and lse.is_contiguous())
+    if ws is None:
+        need = kvp_attend_workspace_size(cache, T, Hq, max_rows, max_len, window, sinks)
+        ws = _workspace(need, q) if need else None
+    status = _kvp_attend_call(cache.ptr, q.data_ptr(), Hq, s[0], s[1], T, first.data_ptr(), lens.data_ptr(), max_rows, max_len, window,
+                              sinks, D ** -0.5 if scale is None else float(scale), out.data_ptr(), _ptr(lse), _ptr(ws),
+                              0 if ws is None else ws.numel(), _stream(q))
+    if status != CI_OK:
+        raise CoreInferError(status, "coreinfer_kvp_attend")
+    return out

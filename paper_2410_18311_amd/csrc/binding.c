@@ -131,8 +131,70 @@ static PyObject* kv4_evict(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   return PyLong_FromLong(status);
 }
 
+static int real(PyObject* o, float* out) {
+  const double x = PyFloat_AsDouble(o);
+  *out = (float)x;
+  return x != -1.0 || !PyErr_Occurred();
+}
+
+/* x, strides t, h, T, H, D, dtype, norm, eps (a float), rope, pos, backward, y, strides t, h, stream */
+static PyObject* rope(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  long long v[16];
+  int64_t stride[2], y_stride[2];
+  float eps;
+  int status;
+  (void)self;
+  if (!values("rope", a, n, "piiiiiipfppipiip", v) || !real(a[8], &eps)) return NULL;
+  stride[0] = v[1];
+  stride[1] = v[2];
+  y_stride[0] = v[13];
+  y_stride[1] = v[14];
+  Py_BEGIN_ALLOW_THREADS
+  status = coreinfer_rope(P(0), stride, v[3], v[4], v[5], I(6), P(7), eps, (const ci_rope*)P(9), (const int32_t*)P(10), I(11), P(12),
+                          y_stride, P(15));
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+/* cache, k, v, strides t, h, T, first, lens, pos, rope, k_norm, eps (a float), q, Hq, strides t, h, q_norm, q_out, stream */
+static PyObject* kvp_append(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  long long v[19];
+  int64_t stride[2], q_stride[2];
+  float eps;
+  int status;
+  (void)self;
+  if (!values("kvp_append", a, n, "pppiiipppppfpiiippp", v) || !real(a[11], &eps)) return NULL;
+  stride[0] = v[3];
+  stride[1] = v[4];
+  q_stride[0] = v[14];
+  q_stride[1] = v[15];
+  Py_BEGIN_ALLOW_THREADS
+  status = coreinfer_kvp_append((const ci_kvp*)P(0), P(1), P(2), stride, v[5], (const int32_t*)P(6), (const int32_t*)P(7),
+                                (const int32_t*)P(8), (const ci_rope*)P(9), P(10), eps, P(12), v[13], q_stride, P(16), P(17), P(18));
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+/* cache, q, Hq, strides t, h, T, first, lens, max_rows, max_len, window, sinks, scale (a float), out, lse, ws, ws_bytes, stream */
+static PyObject* kvp_attend(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  long long v[18];
+  int64_t stride[2];
+  float scale;
+  int status;
+  (void)self;
+  if (!values("kvp_attend", a, n, "ppiiiippiiiifpppip", v) || !real(a[12], &scale)) return NULL;
+  stride[0] = v[3];
+  stride[1] = v[4];
+  Py_BEGIN_ALLOW_THREADS
+  status = coreinfer_kvp_attend((const ci_kvp*)P(0), P(1), v[2], stride, v[5], (const int32_t*)P(6), (const int32_t*)P(7), v[8], v[9],
+                                v[10], v[11], scale, P(13), (float*)P(14), P(15), (size_t)v[16], P(17));
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
 #define CALL(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, NULL}
-static PyMethodDef methods[] = {CALL(ffn_decode), CALL(w4_matvec), CALL(kv4_append), CALL(kv4_read), CALL(kv4_attend), CALL(kv4_evict),
+static PyMethodDef methods[] = {CALL(ffn_decode), CALL(w4_matvec), CALL(kv4_append), CALL(kv4_read), CALL(kv4_attend), CALL(kv4_evict), CALL(rope),
+                                CALL(kvp_append), CALL(kvp_attend),
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", NULL, -1, methods, NULL, NULL, NULL, NULL};
 

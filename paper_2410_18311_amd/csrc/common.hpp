@@ -291,4 +291,15 @@ size_t kv4_evict_ws_bytes(int64_t heads, int64_t max_len, int64_t budget);
 int launch_kv4_evict(const ci_kv4& c, const int32_t* lens, const int32_t* next, int64_t max_len, int64_t budget, int64_t recent,
                      float* weight_out, int32_t* pos_out, int32_t* lens_out, void* ws, hipStream_t s);
 
+// Rotary positions and a cache in pages (rope.hip, kvp_attend.hip).
+int launch_rope(const void* x, const int64_t (&stride)[2], int64_t T, int64_t H, int64_t D, int dtype, const void* norm, float eps,
+                const ci_rope* rope, const int32_t* pos, bool backward, void* y, const int64_t (&y_stride)[2], hipStream_t s);
+int launch_kvp_append(const ci_kvp& c, const void* k, const void* v, const int64_t (&stride)[2], int64_t T, const int32_t* first,
+                      const int32_t* lens, const int32_t* pos, const ci_rope* rope, const void* k_norm, float eps, const void* q,
+                      int64_t Hq, const int64_t (&q_stride)[2], const void* q_norm, void* q_out, hipStream_t s);
+size_t kvp_attend_ws_bytes(const ci_kvp& c, int64_t T, int64_t G, int64_t max_rows, int64_t max_len, int64_t window, int64_t sinks);
+int launch_kvp_attend(const ci_kvp& c, const void* q, int64_t G, const int64_t (&stride)[2], int64_t T, const int32_t* first,
+                      const int32_t* lens, int64_t max_rows, int64_t max_len, int64_t window, int64_t sinks, float scale, void* out,
+                      float* lse, void* ws, hipStream_t s);
+
 }  // namespace ci

@@ -1,0 +1,93 @@
+// Attention over a cache in pages: how a call is split over the chip (the kernels are in kvp_rows.hpp).
+#include <algorithm>
+
+#include "kvp_attend.hpp"
+
+namespace ci {
+namespace {
+
+constexpr int kCus = 256;   // of an MI355X; a workspace query knows no device
+constexpr double kLog2e = 1.4426950408889634;
+
+struct AttendPlan {
+  int few, row_tiles, blocks, wanted, least;
+  size_t place, m, l, o, bytes;   // places in the workspace
+};
+
+// Most steps of `step` slots that the rows of a sentence see something of.
+int64_t most_steps(int64_t step, int64_t rows, int64_t max_len, int64_t window, int64_t sinks) {
+  const int64_t all = (max_len + step - 1) / step;
+  return window == 0 ? all : std::min(all, (window + rows) / step + 2 + (sinks + step - 1) / step);
+}
+
+AttendPlan attend_plan(const ci_kvp& c, int64_t T, int64_t G, int64_t max_rows, int64_t max_len, int64_t window, int64_t sinks) {
+  AttendPlan p = {};
+  const int64_t heads = c.B * c.H, R = max_rows * G;
+  p.few = 1 << 30;
+  const int64_t tiles = (std::min<int64_t>(R, p.few) + 15) / 16, steps = most_steps(32, max_rows, max_len, window, sinks);
+  // Three workgroups a compute unit, what the registers leave room for; no piece below two steps a wave.
+  const int64_t wanted = 3 * kCus;
+  p.least = 8;
+  p.wanted = heads * tiles * 2 > wanted || steps <= p.least ? 0 : (int)(wanted / tiles);
+  p.blocks = (int)heads + p.wanted;
+  p.row_tiles = (int)std::min<int64_t>(tiles, 65535);   // beyond, a workgroup takes several
+  if (p.wanted == 0) return p;
+  auto take = [&](size_t words) {
+    const size_t at = p.bytes;
+    p.bytes += (words * sizeof(float) + 255) / 256 * 256;
+    return at;
+  };
+  const size_t rows = (size_t)p.blocks * p.row_tiles * 16;
+  p.place = take(2 * (size_t)c.B);
+  p.m = take(rows);
+  p.l = take(rows);
+  p.o = take(rows * c.D);
+  return p;
+}
+
+}  // namespace
+
+size_t kvp_attend_ws_bytes(const ci_kvp& c, int64_t T, int64_t G, int64_t max_rows, int64_t max_len, int64_t window, int64_t sinks) {
+  return attend_plan(c, T, G, max_rows, max_len, window, sinks).bytes;
+}
+
+int launch_kvp_attend(const ci_kvp& c, const void* q, int64_t G, const int64_t (&stride)[2], int64_t T, const int32_t* first,
+                      const int32_t* lens, int64_t max_rows, int64_t max_len, int64_t window, int64_t sinks, float scale, void* out,
+                      float* lse, void* ws, hipStream_t s) {
+  const AttendPlan p = attend_plan(c, T, G, max_rows, max_len, window, sinks);
+  KvpAttend a = {};
+  a.c = make_kvp(c);
+  a.q = q;
+  a.q_t = stride[0];
+  a.q_h = stride[1];
+  a.out = out;
+  a.lse = lse;
+  a.first = first;
+  a.lens = lens;
+  a.T = (int)T;
+  a.G = (int)G;
+  a.max_rows = (int)max_rows;
+  a.max_len = (int)max_len;
+  a.window = window >= max_len ? 0 : (int)window;   // everything is inside it
+  a.sinks = (int)std::min(sinks, max_len);
+  a.scale = (float)(scale * kLog2e);
+  const int e = elem_bytes(c.dtype);
+  a.q_vectors = aligned16(q) && stride[0] * e % 16 == 0 && stride[1] * e % 16 == 0;
+  char* base = reinterpret_cast<char*>(ws);
+  a.place = reinterpret_cast<int2*>(base + p.place);
+  a.m = reinterpret_cast<float*>(base + p.m);
+  a.l = reinterpret_cast<float*>(base + p.l);
+  a.o = reinterpret_cast<float*>(base + p.o);
+  a.few = p.few;
+  a.row_tiles = p.row_tiles;
+  a.blocks = p.blocks;
+  a.wanted = p.wanted;
+  a.least = p.least;
+  switch (c.dtype) {
+    case CI_F32: return launch_kvp_attend_type<F32>(a, c.D, s);
+    case CI_F16: return launch_kvp_attend_type<F16>(a, c.D, s);
+    default: return launch_kvp_attend_type<BF16>(a, c.D, s);
+  }
+}
+
+}  // namespace ci

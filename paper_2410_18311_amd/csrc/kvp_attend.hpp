@@ -1,0 +1,187 @@
+// Attention of packed rows over a cache in pages (ci_kvp in coreinfer.h): out = softmax(scale q k^T) v over the slots t <= p, with a window
+// those of t > p - window or t < sinks, in one pass with a running maximum and sum.
+//
+// Logits come out of the matrix cores with slots down and rows across, so that a lane holds one row's: its maximum and sum need two exchanges,
+// its sums of values one factor, and its probabilities enter the product with the values as they lie.
+#pragma once
+
+#include <math.h>
+
+#include "kvp.hpp"
+
+namespace ci {
+
+constexpr int kMaxPieces = 64;   // of a sentence's slots: the lanes of the join keep a factor of each
+
+struct KvpAttend {
+  Kvp c;
+  const void* q;
+  int64_t q_t, q_h;   // strides in elements
+  void* out;
+  float* lse;
+  const int32_t *first, *lens;
+  int T, G, max_rows, max_len, window, sinks;   // window 0: none
+  float scale;                                  // of the logits, with log2(e)
+  int q_vectors;
+  // Few rows: `row_tiles` tiles of 16 rows a head (what more rows a sentence has, others do); the slots of all sentences in `wanted` pieces
+  // and one more a head, none below `least` steps; wanted 0: one piece a head.
+  int few, row_tiles, blocks, wanted, least;
+  int2* place;        // [B]: a sentence's first piece and how many a head has
+  float *m, *l, *o;   // [blocks, row_tiles 16] twice and [.., D]
+};
+
+template <class E> int launch_kvp_attend_type(const KvpAttend& a, int D, hipStream_t s);
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+template <class E>
+__device__ __forceinline__ f32x4 mfma16(const uint4& a, const uint4& b, const f32x4& c) {
+  if constexpr (E::BYTES == 4) return c;
+  else if constexpr (__is_same(E, F16))
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma16_f32(float a, float b, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
+}
+
+// Two numbers rounded to E, and what that leaves of them.
+template <class E>
+__device__ __forceinline__ uint32_t pair_of(float x, float y) {
+  const typename E::T t[2] = {from_float<E>(x), from_float<E>(y)};
+  uint32_t u;
+  __builtin_memcpy(&u, t, sizeof(u));
+  return u;
+}
+template <class E>
+__device__ __forceinline__ void two_pieces(float x, float y, uint32_t* high, uint32_t* low) {
+  typename E::T t[2] = {from_float<E>(x), from_float<E>(y)};
+  __builtin_memcpy(high, t, sizeof(*high));
+  *low = pair_of<E>(x - to_float<E>(t[0]), y - to_float<E>(t[1]));
+}
+
+__device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }   // false for NaN
+
+// A sentence's rows: they begin at packed row `first`, `rows` of them are this call's, the first in slot `slot` (negative: ahead of the
+// first slot, where it sees nothing).
+struct Sentence {
+  int first, rows, len, slot;
+};
+__device__ __forceinline__ Sentence sentence(const KvpAttend& a, int b) {
+  const int from = clamp_row(a.first[b], a.T), n = max(clamp_row(a.first[b + 1], a.T) - from, 0);
+  const int len = min(max(a.lens[b], 0), a.max_len);
+  return Sentence{from, min(n, a.max_rows), len, len - n};
+}
+
+// Steps of STEP slots that rows in slots p0 .. p1 see something of: `sinks` of them from the first slot on, then those from `window` on.
+template <int STEP>
+struct Steps {
+  int sinks, window, total;
+  __device__ Steps(const KvpAttend& a, int p0, int p1, int len) {
+    const int high = min(len, p1 + 1), low = a.window ? max(0, p0 - a.window + 1) : 0;
+    window = low / STEP;
+    sinks = min((min(a.sinks, low) + STEP - 1) / STEP, window);
+    total = high <= 0 ? 0 : sinks + max(0, (high + STEP - 1) / STEP - window);
+  }
+  __device__ int slot(int step) const { return (step < sinks ? step : window + step - sinks) * STEP; }
+};
+
+__device__ __forceinline__ bool sees(const KvpAttend& a, int p, int t) {
+  return t <= p && (a.window == 0 || t > p - a.window || t < a.sinks);
+}
+
+// A sentence's pages.  Slots from the last one in use on read that one, which is as finite as the rest.
+struct Pages {
+  const int32_t* table;
+  int last;
+  __device__ Pages(const KvpAttend& a, int b, int len) : table(a.c.table + (int64_t)b * a.c.most), last(max(len - 1, 0)) {}
+  // Page of a slot; -1: none.
+  __device__ int of(const KvpAttend& a, int slot) const {
+    const int n = table[min(slot, last) >> a.c.shift];
+    return n >= 0 && n < a.c.pages ? n : -1;
+  }
+};
+// Elements from the pages' start to the first slot of a head in a page; page -1: of page 0, whatever lies there.
+template <int D>
+__device__ __forceinline__ int64_t page_start(const KvpAttend& a, int page, int h) {
+  return (((int64_t)max(page, 0) * a.c.H + h) << a.c.shift) * D;
+}
+
+template <class E>
+__device__ __forceinline__ void store_row4(const KvpAttend& a, int D, int64_t at, int d, const float (&v)[4]) {
+  typename E::T* dst = reinterpret_cast<typename E::T*>(a.out) + at * D + d;
+  if constexpr (E::VEC == 4)
+    *reinterpret_cast<float4*>(dst) = make_float4(v[0], v[1], v[2], v[3]);
+  else
+    *reinterpret_cast<uint2*>(dst) = make_uint2(pair_of<E>(v[0], v[1]), pair_of<E>(v[2], v[3]));
+}
+__device__ __forceinline__ void store_lse(const KvpAttend& a, int64_t at, float m, float l) {
+  if (a.lse) a.lse[at] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+}
+// Packed row and head of row r of head h of the cache, as a row of out.
+__device__ __forceinline__ int64_t out_row(const KvpAttend& a, const Sentence& s, int h, int r) {
+  const int i = r / a.G;
+  return ((int64_t)s.first + i) * a.c.H * a.G + h * a.G + (r - i * a.G);
+}
+
+// One row over steps begin .. end - 1 by a whole workgroup, slot by slot, without the slots that it does not see: what the matrix cores cannot leave
+// out when a value that a row does not see is infinite or NaN, because they multiply it by 0.  o: of the D threads that have a channel each.
+// lds: 260 floats.
+template <class E, int D, int STEP>
+__device__ __forceinline__ void careful_row(const KvpAttend& a, const Sentence& s, const Pages& pages, int h, int r, const Steps<STEP>& steps,
+                                            int begin, int end, float* lds, float* m_out, float* l_out, float* o_out) {
+  using T = typename E::T;
+  const int tid = threadIdx.x, i = r / a.G, p = s.slot + i;
+  const T* q = reinterpret_cast<const T*>(a.q) + (int64_t)(s.first + i) * a.q_t + (int64_t)(h * a.G + r - i * a.G) * a.q_h;
+  float m = -INFINITY, l = 0.0f, o = 0.0f;
+  const int64_t slots = (int64_t)(end - begin) * STEP;
+  for (int64_t from = 0; from < slots; from += 256) {
+    const int64_t mine = from + tid;
+    float z = -INFINITY;
+    if (mine < slots) {
+      const int t = steps.slot(begin + (int)(mine / STEP)) + (int)(mine % STEP), page = t < s.len ? pages.of(a, t) : -1;
+      if (page >= 0 && t < s.len && sees(a, p, t)) {
+        const T* k = reinterpret_cast<const T*>(a.c.k) + page_start<D>(a, page, h) + (t & ((1 << a.c.shift) - 1)) * D;
+        float sum = 0.0f;
+        for (int d = 0; d < D; ++d) sum = __builtin_fmaf(to_float<E>(k[d]), to_float<E>(q[d]), sum);
+        z = sum * a.scale;
+      }
+    }
+    float top = z != z ? INFINITY : z;   // a NaN makes everything NaN
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, kWave));
+    if ((tid & 63) == 0) lds[256 + (tid >> 6)] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(lds[256], lds[257]), fmaxf(lds[258], lds[259]));
+    const float next = fmaxf(m, top), ref = next == -INFINITY ? 0.0f : next;
+    // seen, but too small for fp32: not nothing, as it is multiplied by what may be infinite
+    lds[tid] = z == -INFINITY ? 0.0f : z != z ? z : fmaxf(__builtin_amdgcn_exp2f(z - ref), 1e-37f);
+    __syncthreads();
+    const float was = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - ref);
+    m = next;
+    l *= was;
+    o *= was;
+    for (int e = 0; e < 256 && from + e < slots; ++e) {
+      const float w = lds[e];
+      if (w == 0.0f) continue;
+      l += w;
+      if (tid < D) {
+        const int t = steps.slot(begin + (int)((from + e) / STEP)) + (int)((from + e) % STEP);
+        const T* v = reinterpret_cast<const T*>(a.c.v) + page_start<D>(a, pages.of(a, t), h) + (t & ((1 << a.c.shift) - 1)) * D;
+        o += w * to_float<E>(v[tid]);
+      }
+    }
+    __syncthreads();
+  }
+  *m_out = m;
+  *l_out = l;
+  *o_out = o;
+}
+
+}  // namespace
+}  // namespace ci

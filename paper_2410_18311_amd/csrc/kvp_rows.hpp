@@ -1,0 +1,386 @@
+// Attention of few rows of a head over a cache in pages (kvp_attend.hpp), one token a sentence above all: bound by the cache's bytes.
+//
+// The slots of all sentences are shared out by length over three workgroups a compute unit, whose waves take every fourth step of 32 slots.  A wave
+// reads keys and values as they lie, 16 bytes a lane, without the LDS: a lane's eight channels of eight slots are turned into eight
+// operands of one channel by one permutation a word.  A second launch joins the pieces.
+#pragma once
+
+#include "kvp_attend.hpp"
+
+namespace ci {
+namespace {
+
+// How the slots are shared out: pieces of `chunk` steps, so that a long sentence among short ones has as many workgroups as its
+// length asks for.  Everything follows from first and lens, in every wave for itself.
+struct PieceShares {
+  int chunk;
+  // Steps of a sentence that has few rows; -1: another's work, or none.
+  __device__ static int steps_of(const KvpAttend& a, int b) {
+    const Sentence s = sentence(a, b);
+    if (s.rows == 0 || (int64_t)s.rows * a.G > a.few) return -1;
+    return Steps<32>(a, max(s.slot, 0), s.slot + s.rows - 1, s.len).total;
+  }
+  // At least one piece: it writes the zeros of rows that see nothing.
+  __device__ int count(int steps) const { return steps < 0 ? 0 : max(1, (steps + chunk - 1) / chunk); }
+
+  __device__ explicit PieceShares(const KvpAttend& a) {
+    if (a.wanted == 0) {
+      chunk = 1 << 30;
+      return;
+    }
+    int64_t total = 0;
+    int longest = 0;
+    for (int b = threadIdx.x & 63; b < a.c.B; b += 64) {
+      const int n = max(steps_of(a, b), 0);
+      total += n;
+      longest = max(longest, n);
+    }
+    if (a.c.B > 1) {
+#pragma unroll
+      for (int off = 1; off < 64; off <<= 1) {
+        total += __shfl_xor(total, off, kWave);
+        longest = max(longest, __shfl_xor(longest, off, kWave));
+      }
+    }
+    // all pieces together are at most wanted + B H: a sentence's last one need not be full
+    const int64_t even = (total * a.c.H + a.wanted - 1) / a.wanted, least = max(a.least, (longest + kMaxPieces - 1) / kMaxPieces);
+    chunk = __builtin_amdgcn_readfirstlane((int)((max(even, least) + 3) / 4 * 4));
+  }
+  // The sentence of piece `at` and the pieces before that sentence's; b = B where there is no such piece.
+  __device__ void find(const KvpAttend& a, int at, int* b, int* before) const {
+    const int lane = threadIdx.x & 63;
+    int base = 0;
+    for (int b0 = 0; b0 < a.c.B; b0 += 64) {
+      const int mine = b0 + lane < a.c.B ? count(steps_of(a, b0 + lane)) * a.c.H : 0;
+      int upto = mine;
+      if (a.c.B > 1) {
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+          const int n = __shfl_up(upto, off, kWave);
+          if (lane >= off) upto += n;
+        }
+      }
+      const uint64_t past = __ballot(base + upto > at);
+      if (past) {
+        const int hit = __builtin_ctzll(past);
+        *b = b0 + hit;
+        *before = base + __shfl(upto - mine, hit, kWave);
+        return;
+      }
+      base += __shfl(upto, 63, kWave);
+    }
+    *b = a.c.B;
+    *before = base;
+  }
+};
+
+// What a lane holds of 32 slots: of keys the row n of both halves, a quarter (g) of each 64 bytes; of values the channels CH n .. of the slots
+// 4 g .. + 3 of both halves.
+template <class E, int D>
+struct Step32 {
+  static constexpr int K = D * E::BYTES / 64, CH = D / 16, V = CH * E::BYTES / 4;   // vectors of keys; channels and words of values
+  uint4 k[2][K];
+  uint32_t v[8][V];
+  int page[2];   // of the halves
+};
+
+template <int WORDS>
+__device__ __forceinline__ void ld_words(const void* p, uint32_t (&to)[WORDS]) {
+  if constexpr (WORDS == 2) {
+    const uint2 u = *reinterpret_cast<const uint2*>(p);
+    to[0] = u.x, to[1] = u.y;
+  } else {
+#pragma unroll
+    for (int i = 0; i < WORDS; i += 4) {
+      const uint4 u = ld16(reinterpret_cast<const uint32_t*>(p) + i);
+      to[i] = u.x, to[i + 1] = u.y, to[i + 2] = u.z, to[i + 3] = u.w;
+    }
+  }
+}
+
+// A row of q as the operand that goes with the keys' vectors.
+template <class E, int D>
+__device__ __forceinline__ void load_query(const KvpAttend& a, const Sentence& s, int h, int r, uint4 (&q)[Step32<E, D>::K]) {
+  const int g = (threadIdx.x & 63) >> 4, i = r / a.G;
+  const typename E::T* src = reinterpret_cast<const typename E::T*>(a.q) + (int64_t)(s.first + i) * a.q_t +
+                             (int64_t)(h * a.G + r - i * a.G) * a.q_h + g * E::VEC;
+#pragma unroll
+  for (int j = 0; j < Step32<E, D>::K; ++j) {
+    if (a.q_vectors) {
+      q[j] = ld16(src + 4 * j * E::VEC);
+    } else {
+      typename E::T x[E::VEC];
+#pragma unroll
+      for (int e = 0; e < E::VEC; ++e) x[e] = src[4 * j * E::VEC + e];
+      __builtin_memcpy(&q[j], x, sizeof(x));
+    }
+  }
+}
+
+template <class E, int D>
+__global__ __launch_bounds__(256, E::BYTES == 4 ? 2 : 3) void gemm_kvp_rows_kernel(KvpAttend a) {
+  using S32 = Step32<E, D>;
+  constexpr int K = S32::K, CH = S32::CH, VW = S32::V;
+  __shared__ float ml[2][4][16];
+  __shared__ __attribute__((aligned(16))) float sums[4][16][D + 4];
+  __shared__ unsigned broken;   // rows, a bit each
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const PieceShares shares(a);
+  int b, before;
+  shares.find(a, blockIdx.x, &b, &before);
+  b = __builtin_amdgcn_readfirstlane(b);
+  before = __builtin_amdgcn_readfirstlane(before);
+  if (b >= a.c.B) return;
+  const int h = ((int)blockIdx.x - before) % a.c.H, piece = ((int)blockIdx.x - before) / a.c.H;
+  const Sentence s = sentence(a, b);
+  const int R = s.rows * a.G;
+  const Steps<32> steps(a, max(s.slot, 0), s.slot + s.rows - 1, s.len);
+  const int pieces = shares.count(steps.total);
+  if (a.wanted && (int)blockIdx.x == before && blockIdx.y == 0 && threadIdx.x == 0) a.place[b] = make_int2(before, pieces);   // for the join
+  const int begin = min(steps.total, piece * shares.chunk), end = min(steps.total, begin + min(shares.chunk, steps.total));
+  const Pages pages(a, b, s.len);
+  const int inside = (1 << a.c.shift) - 1;
+  for (int tile = blockIdx.y; tile * 16 < R; tile += gridDim.y) {
+    const int row0 = tile * 16;
+    const int row = min(row0 + n, R - 1);   // rows past the last repeat it
+    const int p = s.slot + row / a.G;
+    const int p_low = s.slot + row0 / a.G, p_high = s.slot + min(row0 + 15, R - 1) / a.G;   // of the tile's rows
+
+    if (threadIdx.x == 0) broken = 0;
+    uint4 q[K];
+    load_query<E, D>(a, s, h, row, q);
+
+    S32 x;
+    auto find_pages = [&](int step) {
+      const int t = steps.slot(min(step, end - 1));
+  #pragma unroll
+      for (int i = 0; i < 2; ++i) x.page[i] = pages.of(a, t + 16 * i);
+    };
+    auto load_keys = [&](int step, const int (&page)[2]) {
+      const int t = steps.slot(step);
+  #pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int slot = min(t + 16 * i + n, pages.last) & inside;
+        const typename E::T* src = reinterpret_cast<const typename E::T*>(a.c.k) + page_start<D>(a, page[i], h) + slot * D + g * E::VEC;
+  #pragma unroll
+        for (int j = 0; j < K; ++j) x.k[i][j] = ld16(src + 4 * j * E::VEC);
+      }
+    };
+    auto load_values = [&](int step, const int (&page)[2]) {
+      const int t = steps.slot(step);
+  #pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const typename E::T* src = reinterpret_cast<const typename E::T*>(a.c.v) + page_start<D>(a, page[i], h) + n * CH;
+  #pragma unroll
+        for (int r = 0; r < 4; ++r) ld_words<VW>(src + (min(t + 16 * i + 4 * g + r, pages.last) & inside) * D, x.v[4 * i + r]);
+      }
+    };
+
+    float m = -INFINITY, l = 0.0f;   // l: of the lane's own slots
+    f32x4 acc[CH];
+  #pragma unroll
+    for (int c = 0; c < CH; ++c) acc[c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+    int step = begin + wave;
+    if (step < end) {
+      find_pages(step);
+      int page[2] = {x.page[0], x.page[1]};
+      load_keys(step, page);
+      load_values(step, page);
+      find_pages(step + 4);
+      for (; step < end; step += 4) {
+        const int t = steps.slot(step);
+        const int next[2] = {x.page[0], x.page[1]};
+        const bool more = step + 4 < end;
+        f32x4 z[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+  #pragma unroll
+        for (int j = 0; j < K; ++j)
+  #pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            if constexpr (E::BYTES == 2) {
+              z[i] = mfma16<E>(x.k[i][j], q[j], z[i]);
+            } else {
+              float kf[4], qf[4];
+              unpack<F32>(x.k[i][j], kf);
+              unpack<F32>(q[j], qf);
+  #pragma unroll
+              for (int c = 0; c < 4; ++c) z[i] = mfma16_f32(kf[c], qf[c], z[i]);
+            }
+          }
+        if (more) load_keys(step + 4, next);
+        const bool masked = page[0] < 0 || page[1] < 0 || t + 31 > p_low || (a.window && t <= p_high - a.window && t + 31 >= a.sinks);
+  #pragma unroll
+        for (int i = 0; i < 2; ++i)
+  #pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            z[i][r] *= a.scale;
+            if (masked && (page[i] < 0 || !sees(a, p, t + 16 * i + 4 * g + r))) z[i][r] = -INFINITY;
+          }
+        float top = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])), fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])));
+        // The maximum is raised only when a logit passes it by 2^8; the sums hold that range in fp32.
+        if (__any(top > m + 8.0f)) {
+          top = fmaxf(top, __shfl_xor(top, 16, kWave));
+          top = fmaxf(top, __shfl_xor(top, 32, kWave));
+          const float raised = fmaxf(m, top), was = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - raised);
+          m = raised;
+          l *= was;
+  #pragma unroll
+          for (int c = 0; c < CH; ++c) acc[c] *= was;
+        }
+        const float ref = m == -INFINITY ? 0.0f : m;
+  #pragma unroll
+        for (int i = 0; i < 2; ++i)
+  #pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            z[i][r] = __builtin_amdgcn_exp2f(z[i][r] - ref);
+            l += z[i][r];
+          }
+        if constexpr (E::BYTES == 2) {
+          uint4 high, low;
+          two_pieces<E>(z[0][0], z[0][1], &high.x, &low.x);
+          two_pieces<E>(z[0][2], z[0][3], &high.y, &low.y);
+          two_pieces<E>(z[1][0], z[1][1], &high.z, &low.z);
+          two_pieces<E>(z[1][2], z[1][3], &high.w, &low.w);
+  #pragma unroll
+          for (int c = 0; c < CH; ++c) {
+            const uint32_t half = c % 2 ? 0x07060302u : 0x05040100u;
+            const uint4 e = make_uint4(__builtin_amdgcn_perm(x.v[1][c / 2], x.v[0][c / 2], half), __builtin_amdgcn_perm(x.v[3][c / 2], x.v[2][c / 2], half),
+                                       __builtin_amdgcn_perm(x.v[5][c / 2], x.v[4][c / 2], half), __builtin_amdgcn_perm(x.v[7][c / 2], x.v[6][c / 2], half));
+            acc[c] = mfma16<E>(e, high, acc[c]);
+            acc[c] = mfma16<E>(e, low, acc[c]);
+          }
+        } else {
+  #pragma unroll
+          for (int c = 0; c < CH; ++c)
+  #pragma unroll
+            for (int i = 0; i < 8; ++i) acc[c] = mfma16_f32(u2f(x.v[i][c]), z[i / 4][i % 4], acc[c]);
+        }
+        if (more) {
+          load_values(step + 4, next);
+          page[0] = next[0];
+          page[1] = next[1];
+          find_pages(step + 8);
+        }
+      }
+    }
+
+    // the four waves' sums against their common maximum; a lane's slots are a quarter of its row's
+    l += __shfl_xor(l, 16, kWave);
+    l += __shfl_xor(l, 32, kWave);
+    if (g == 0) {
+      ml[0][wave][n] = m;
+      ml[1][wave][n] = l;
+    }
+    __syncthreads();
+    float top = ml[0][0][n];
+  #pragma unroll
+    for (int w = 1; w < 4; ++w) top = fmaxf(top, ml[0][w][n]);
+    const float own = m == -INFINITY ? (l != 0.0f ? NAN : 0.0f) : __builtin_amdgcn_exp2f(m - top);
+    if (row0 + n < R) {
+  #pragma unroll
+      for (int r = 0; r < 4; ++r)
+  #pragma unroll
+        for (int c = 0; c < CH; c += 4)
+          *reinterpret_cast<float4*>(&sums[wave][n][CH * (4 * g + r) + c]) =
+              make_float4(acc[c][r] * own, acc[c + 1][r] * own, acc[c + 2][r] * own, acc[c + 3][r] * own);
+    }
+    __syncthreads();
+
+    const int live = min(16, R - row0);
+    const size_t part = a.wanted ? ((size_t)blockIdx.x * a.row_tiles + tile) * 16 : 0;
+    for (int e = threadIdx.x; e < live * (D / 4); e += 256) {
+      const int r = e / (D / 4), d = e % (D / 4) * 4;
+      float t = -INFINITY, total = 0.0f, v[4];
+  #pragma unroll
+      for (int w = 0; w < 4; ++w) t = fmaxf(t, ml[0][w][r]);
+  #pragma unroll
+      for (int w = 0; w < 4; ++w)
+        total += ml[0][w][r] == -INFINITY ? ml[1][w][r] : ml[1][w][r] * __builtin_amdgcn_exp2f(ml[0][w][r] - t);
+  #pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = (sums[0][r][d + i] + sums[1][r][d + i]) + (sums[2][r][d + i] + sums[3][r][d + i]);
+      if (!(finite(v[0]) && finite(v[1]) && finite(v[2]) && finite(v[3]))) atomicOr(&broken, 1u << r);
+      if (a.wanted) {
+        *reinterpret_cast<float4*>(a.o + (part + r) * D + d) = make_float4(v[0], v[1], v[2], v[3]);
+        if (d == 0) {
+          a.m[part + r] = t;
+          a.l[part + r] = total;
+        }
+      } else {
+        const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
+  #pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] *= inverse;
+        const int64_t at = out_row(a, s, h, row0 + r);
+        store_row4<E>(a, D, at, d, v);
+        if (d == 0) store_lse(a, at, t, total);
+      }
+    }
+    __syncthreads();
+    // an infinity or a NaN among the values, seen or not
+    for (unsigned left = broken; left; left &= left - 1) {
+      const int r = __builtin_ctz(left);
+      float mr, lr, o;
+      careful_row<E, D, 32>(a, s, pages, h, row0 + r, steps, begin, end, &sums[0][0][0], &mr, &lr, &o);
+      if (a.wanted) {
+        if (threadIdx.x < D) a.o[(part + r) * D + threadIdx.x] = o;
+        if (threadIdx.x == 0) {
+          a.m[part + r] = mr;
+          a.l[part + r] = lr;
+        }
+      } else {
+        const int64_t at = out_row(a, s, h, row0 + r);
+        if (threadIdx.x < D) reinterpret_cast<typename E::T*>(a.out)[at * D + threadIdx.x] = from_float<E>(lr == 0.0f ? 0.0f : o / lr);
+        if (threadIdx.x == 0) store_lse(a, at, mr, lr);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// The pieces of a row put together, a wave a row.
+template <class E, int D>
+__global__ __launch_bounds__(256) void kvp_join_kernel(KvpAttend a) {
+  const int Hq = a.c.H * a.G, lane = threadIdx.x & 63;
+  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);   // row of out
+  if (at >= (int64_t)a.T * Hq) return;
+  const int t = (int)(at / Hq), head = (int)(at - (int64_t)t * Hq), h = head / a.G;
+  const int b = sentence_of(a.first, a.c.B, t);
+  const Sentence s = sentence(a, b);
+  if (t < s.first || t - s.first >= s.rows || (int64_t)s.rows * a.G > a.few) return;
+  const int2 place = a.place[b];
+  const int r = (t - s.first) * a.G + head - h * a.G;
+  const size_t from = ((size_t)(place.x + h) * a.row_tiles + r / 16) * 16 + r % 16, next = (size_t)a.c.H * a.row_tiles * 16;
+  const float m = lane < place.y ? a.m[from + lane * next] : -INFINITY, l = lane < place.y ? a.l[from + lane * next] : 0.0f;
+  float top = m;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) top = fmaxf(top, __shfl_xor(top, off, kWave));
+  // a piece without a maximum saw nothing, or nothing but NaN
+  const float factor = m == -INFINITY ? (l != 0.0f ? NAN : 0.0f) : __builtin_amdgcn_exp2f(m - top);
+  const float total = wave_sum(m == -INFINITY ? l : l * factor);
+  float sum[D / 64] = {};
+  for (int i = 0; i < place.y; ++i) {
+    const float f = __shfl(factor, i, kWave);
+    const float* o = a.o + (from + i * next) * D + lane * (D / 64);
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) sum[c] += f == 0.0f ? 0.0f : f * o[c];
+  }
+  const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
+  typename E::T* dst = reinterpret_cast<typename E::T*>(a.out) + at * D + lane * (D / 64);
+#pragma unroll
+  for (int c = 0; c < D / 64; ++c) dst[c] = from_float<E>(sum[c] * inverse);
+  if (lane == 0) store_lse(a, at, top, total);
+}
+
+template <class E, int D>
+int launch_rows(const KvpAttend& a, hipStream_t s) {
+  hipLaunchKernelGGL((gemm_kvp_rows_kernel<E, D>), dim3((unsigned)a.blocks, (unsigned)a.row_tiles), dim3(256), 0, s, a);
+  CI_HIP_CHECK_LAUNCH();
+  if (a.wanted) {
+    hipLaunchKernelGGL((kvp_join_kernel<E, D>), dim3((unsigned)(((int64_t)a.T * a.c.H * a.G + 3) / 4)), dim3(256), 0, s, a);
+    CI_HIP_CHECK_LAUNCH();
+  }
+  return CI_OK;
+}
+
+}  // namespace
+}  // namespace ci

@@ -22,7 +22,7 @@ OBJDUMP = os.path.join(os.path.dirname(os.path.dirname(os.environ.get("HIPCC", "
                        "llvm-objdump")
 WAIT_STATES = 5
 TO_PRODUCT, FROM_PRODUCT = 2, 18
-BY_COMPILER = ("gemm_slim_kernel", "gemm_f32_", "gemm_q4_")   # kernels whose products are builtins: the compiler keeps the hardware's own, shorter, states
+BY_COMPILER = ("gemm_slim_kernel", "gemm_f32_", "gemm_q4_", "gemm_kvp_")   # kernels whose products are builtins: the compiler keeps the hardware's own, shorter, states
 MAGIC = b"__CLANG_OFFLOAD_BUNDLE__"
 
 
