@@ -716,7 +716,7 @@ int coreinfer_kvp_append(const ci_kvp* cache, const void* k, const void* v, cons
  * rows share a head, and rounded to it in prompts.
  * ws: coreinfer_kvp_attend_workspace_size bytes, 16-byte aligned; NULL where that is 0.  Calls
  * that share a workspace must not overlap in time.
- * window, sinks >= 0.  Hq / H <= 4096, T * (Hq / H) <= 2^28.
+ * window, sinks >= 0.  Hq / H <= 4096, T * Hq <= 2^30.
  */
 int coreinfer_kvp_attend_workspace_size(const ci_kvp* cache, int64_t T, int64_t Hq, int64_t max_rows, int64_t max_len,
                                         int64_t window, int64_t sinks, size_t* bytes);

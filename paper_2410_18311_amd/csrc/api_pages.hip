@@ -113,7 +113,7 @@ int coreinfer_kvp_attend_workspace_size(const ci_kvp* cache, int64_t T, int64_t 
   const int rc = cache_status(cache);
   if (rc != CI_OK) return rc;
   if (!bytes || T < 0 || T > CI_MAX_PACKED_ROWS || Hq < cache->H || Hq % cache->H != 0 || Hq / cache->H > 4096 ||
-      T * (Hq / cache->H) > (1 << 28) || max_rows < 1 || max_rows > CI_MAX_PACKED_ROWS || max_len < 1 ||
+      T * Hq > ((int64_t)1 << 30) || max_rows < 1 || max_rows > CI_MAX_PACKED_ROWS || max_len < 1 ||
       max_len > cache->most * cache->page || window < 0 || sinks < 0 || window > INT64_MAX / 2 || sinks > INT64_MAX / 2)
     return CI_ERR_INVALID_ARG;
   *bytes = T == 0 ? 0 : kvp_attend_ws_bytes(*cache, T, Hq / cache->H, std::min(max_rows, T), max_len, window, sinks);

@@ -1,4 +1,4 @@
-// Attention over a cache in pages: how a call is split over the chip (the kernels are in kvp_rows.hpp).
+// Attention over a cache in pages: how a call is split over the chip (the kernels are in kvp_rows.hpp and kvp_tiles.hpp).
 #include <algorithm>
 
 #include "kvp_attend.hpp"
@@ -10,38 +10,61 @@ constexpr int kCus = 256;   // of an MI355X; a workspace query knows no device
 constexpr double kLog2e = 1.4426950408889634;
 
 struct AttendPlan {
+  bool rows, in_tiles;   // which kernels run
   int few, row_tiles, blocks, wanted, least;
-  size_t place, m, l, o, bytes;   // places in the workspace
+  int tiles, pieces;
+  size_t place, m, l, o, tile_m, tile_l, tile_o, bytes;   // places in the workspace
 };
+
+constexpr int kTileRows = 128;
 
 // Most steps of `step` slots that the rows of a sentence see something of.
 int64_t most_steps(int64_t step, int64_t rows, int64_t max_len, int64_t window, int64_t sinks) {
   const int64_t all = (max_len + step - 1) / step;
-  return window == 0 ? all : std::min(all, (window + rows) / step + 2 + (sinks + step - 1) / step);
+  return window == 0 || window >= max_len ? all : std::min(all, (window + rows) / step + 2 + (std::min(sinks, max_len) + step - 1) / step);
 }
 
 AttendPlan attend_plan(const ci_kvp& c, int64_t T, int64_t G, int64_t max_rows, int64_t max_len, int64_t window, int64_t sinks) {
   AttendPlan p = {};
   const int64_t heads = c.B * c.H, R = max_rows * G;
-  p.few = 1 << 30;
-  const int64_t tiles = (std::min<int64_t>(R, p.few) + 15) / 16, steps = most_steps(32, max_rows, max_len, window, sinks);
-  // Three workgroups a compute unit, what the registers leave room for; no piece below two steps a wave.
-  const int64_t wanted = 3 * kCus;
-  p.least = 8;
-  p.wanted = heads * tiles * 2 > wanted || steps <= p.least ? 0 : (int)(wanted / tiles);
-  p.blocks = (int)heads + p.wanted;
-  p.row_tiles = (int)std::min<int64_t>(tiles, 65535);   // beyond, a workgroup takes several
-  if (p.wanted == 0) return p;
+  // Prompts of 16-bit types go in tiles.  Where all sentences may be prompts the tiles take short ones too; beside single
+  // tokens they leave those of up to 16 rows.
+  p.in_tiles = c.dtype != CI_F32 && R > 64;
+  p.rows = !p.in_tiles || T < c.B * max_rows;
+  p.few = !p.in_tiles ? 1 << 30 : p.rows ? 16 : 0;
   auto take = [&](size_t words) {
     const size_t at = p.bytes;
     p.bytes += (words * sizeof(float) + 255) / 256 * 256;
     return at;
   };
-  const size_t rows = (size_t)p.blocks * p.row_tiles * 16;
-  p.place = take(2 * (size_t)c.B);
-  p.m = take(rows);
-  p.l = take(rows);
-  p.o = take(rows * c.D);
+  if (p.rows) {
+    const int64_t tiles = (std::min<int64_t>(R, p.few) + 15) / 16, steps = most_steps(32, max_rows, max_len, window, sinks);
+    // Three workgroups a compute unit, what the registers leave room for; no piece below two steps a wave.
+    const int64_t wanted = 3 * kCus;
+    p.least = 8;
+    p.wanted = heads * tiles * 2 > wanted || steps <= p.least ? 0 : (int)(wanted / tiles);
+    p.blocks = (int)heads + p.wanted;
+    p.row_tiles = (int)std::min<int64_t>(tiles, 65535);   // beyond, a workgroup takes several
+    if (p.wanted) {
+      const size_t rows = (size_t)p.blocks * p.row_tiles * 16;
+      p.place = take(2 * (size_t)c.B);
+      p.m = take(rows);
+      p.l = take(rows);
+      p.o = take(rows * c.D);
+    }
+  }
+  if (p.in_tiles) {
+    p.tiles = (int)(T * G / kTileRows + c.B);   // see tile_start
+    const int64_t full = std::max<int64_t>(1, T * G / kTileRows) * c.H, steps = most_steps(64, max_rows, max_len, window, sinks);
+    // Two workgroups a compute unit are what fits; no piece below eight steps.
+    p.pieces = (int)std::max<int64_t>(1, std::min<int64_t>({2 * kCus / full, steps / 8, kMaxPieces}));
+    if (p.pieces > 1) {
+      const size_t rows = (size_t)p.tiles * c.H * p.pieces * kTileRows;
+      p.tile_m = take(rows);
+      p.tile_l = take(rows);
+      p.tile_o = take(rows * c.D);
+    }
+  }
   return p;
 }
 
@@ -83,10 +106,16 @@ int launch_kvp_attend(const ci_kvp& c, const void* q, int64_t G, const int64_t (
   a.blocks = p.blocks;
   a.wanted = p.wanted;
   a.least = p.least;
+  a.tiles = p.tiles;
+  a.tile_rows = kTileRows;
+  a.pieces = p.pieces;
+  a.tile_m = reinterpret_cast<float*>(base + p.tile_m);
+  a.tile_l = reinterpret_cast<float*>(base + p.tile_l);
+  a.tile_o = reinterpret_cast<float*>(base + p.tile_o);
   switch (c.dtype) {
-    case CI_F32: return launch_kvp_attend_type<F32>(a, c.D, s);
-    case CI_F16: return launch_kvp_attend_type<F16>(a, c.D, s);
-    default: return launch_kvp_attend_type<BF16>(a, c.D, s);
+    case CI_F32: return launch_kvp_attend_type<F32>(a, c.D, p.rows, p.in_tiles, s);
+    case CI_F16: return launch_kvp_attend_type<F16>(a, c.D, p.rows, p.in_tiles, s);
+    default: return launch_kvp_attend_type<BF16>(a, c.D, p.rows, p.in_tiles, s);
   }
 }
 

@@ -28,9 +28,13 @@ struct KvpAttend {
   int few, row_tiles, blocks, wanted, least;
   int2* place;        // [B]: a sentence's first piece and how many a head has
   float *m, *l, *o;   // [blocks, row_tiles 16] twice and [.., D]
+  // Prompts: `tiles` tiles of tile_rows rows at most, the steps of each in `pieces`.
+  int tiles, tile_rows, pieces;
+  float *tile_m, *tile_l, *tile_o;   // [tiles H, pieces, tile_rows] twice and [.., D]
 };
 
-template <class E> int launch_kvp_attend_type(const KvpAttend& a, int D, hipStream_t s);
+// rows, tiles: which of the kernels
+template <class E> int launch_kvp_attend_type(const KvpAttend& a, int D, bool rows, bool tiles, hipStream_t s);
 
 namespace {
 
@@ -39,14 +43,14 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 template <class E>
-__device__ __forceinline__ f32x4 mfma16(const uint4& a, const uint4& b, const f32x4& c) {
+__device__ __forceinline__ f32x4 product16(const uint4& a, const uint4& b, const f32x4& c) {
   if constexpr (E::BYTES == 4) return c;
   else if constexpr (__is_same(E, F16))
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
   else
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
-__device__ __forceinline__ f32x4 mfma16_f32(float a, float b, const f32x4& c) {
+__device__ __forceinline__ f32x4 product16_f32(float a, float b, const f32x4& c) {
   return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
 
@@ -97,9 +101,10 @@ __device__ __forceinline__ bool sees(const KvpAttend& a, int p, int t) {
 
 // A sentence's pages.  Slots from the last one in use on read that one, which is as finite as the rest.
 struct Pages {
-  const int32_t* table;
+  const __attribute__((address_space(4))) int32_t* table;   // constant: a uniform slot's entry comes by a scalar load
   int last;
-  __device__ Pages(const KvpAttend& a, int b, int len) : table(a.c.table + (int64_t)b * a.c.most), last(max(len - 1, 0)) {}
+  __device__ Pages(const KvpAttend& a, int b, int len)
+      : table((const __attribute__((address_space(4))) int32_t*)(uintptr_t)(a.c.table + (int64_t)b * a.c.most)), last(max(len - 1, 0)) {}
   // Page of a slot; -1: none.
   __device__ int of(const KvpAttend& a, int slot) const {
     const int n = table[min(slot, last) >> a.c.shift];
@@ -123,6 +128,9 @@ __device__ __forceinline__ void store_row4(const KvpAttend& a, int D, int64_t at
 __device__ __forceinline__ void store_lse(const KvpAttend& a, int64_t at, float m, float l) {
   if (a.lse) a.lse[at] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
 }
+// Workgroups of four waves for that many rows, each a wave's; beyond, a wave takes several.
+inline unsigned join_blocks(int64_t rows) { return (unsigned)((rows + 3) / 4 < 65536 ? (rows + 3) / 4 : 65536); }
+
 // Packed row and head of row r of head h of the cache, as a row of out.
 __device__ __forceinline__ int64_t out_row(const KvpAttend& a, const Sentence& s, int h, int r) {
   const int i = r / a.G;

@@ -2,7 +2,7 @@
 #include "kvp_rows.hpp"
 
 namespace ci {
-template <> int launch_kvp_attend_type<F32>(const KvpAttend& a, int D, hipStream_t s) {
+template <> int launch_kvp_attend_type<F32>(const KvpAttend& a, int D, bool, bool, hipStream_t s) {
   return D == 64 ? launch_rows<F32, 64>(a, s) : launch_rows<F32, 128>(a, s);
 }
 }  // namespace ci

@@ -199,13 +199,13 @@ __global__ __launch_bounds__(256, E::BYTES == 4 ? 2 : 3) void gemm_kvp_rows_kern
   #pragma unroll
           for (int i = 0; i < 2; ++i) {
             if constexpr (E::BYTES == 2) {
-              z[i] = mfma16<E>(x.k[i][j], q[j], z[i]);
+              z[i] = product16<E>(x.k[i][j], q[j], z[i]);
             } else {
               float kf[4], qf[4];
               unpack<F32>(x.k[i][j], kf);
               unpack<F32>(q[j], qf);
   #pragma unroll
-              for (int c = 0; c < 4; ++c) z[i] = mfma16_f32(kf[c], qf[c], z[i]);
+              for (int c = 0; c < 4; ++c) z[i] = product16_f32(kf[c], qf[c], z[i]);
             }
           }
         if (more) load_keys(step + 4, next);
@@ -247,14 +247,14 @@ __global__ __launch_bounds__(256, E::BYTES == 4 ? 2 : 3) void gemm_kvp_rows_kern
             const uint32_t half = c % 2 ? 0x07060302u : 0x05040100u;
             const uint4 e = make_uint4(__builtin_amdgcn_perm(x.v[1][c / 2], x.v[0][c / 2], half), __builtin_amdgcn_perm(x.v[3][c / 2], x.v[2][c / 2], half),
                                        __builtin_amdgcn_perm(x.v[5][c / 2], x.v[4][c / 2], half), __builtin_amdgcn_perm(x.v[7][c / 2], x.v[6][c / 2], half));
-            acc[c] = mfma16<E>(e, high, acc[c]);
-            acc[c] = mfma16<E>(e, low, acc[c]);
+            acc[c] = product16<E>(e, high, acc[c]);
+            acc[c] = product16<E>(e, low, acc[c]);
           }
         } else {
   #pragma unroll
           for (int c = 0; c < CH; ++c)
   #pragma unroll
-            for (int i = 0; i < 8; ++i) acc[c] = mfma16_f32(u2f(x.v[i][c]), z[i / 4][i % 4], acc[c]);
+            for (int i = 0; i < 8; ++i) acc[c] = product16_f32(u2f(x.v[i][c]), z[i / 4][i % 4], acc[c]);
         }
         if (more) {
           load_values(step + 4, next);
@@ -341,34 +341,34 @@ __global__ __launch_bounds__(256, E::BYTES == 4 ? 2 : 3) void gemm_kvp_rows_kern
 template <class E, int D>
 __global__ __launch_bounds__(256) void kvp_join_kernel(KvpAttend a) {
   const int Hq = a.c.H * a.G, lane = threadIdx.x & 63;
-  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);   // row of out
-  if (at >= (int64_t)a.T * Hq) return;
-  const int t = (int)(at / Hq), head = (int)(at - (int64_t)t * Hq), h = head / a.G;
-  const int b = sentence_of(a.first, a.c.B, t);
-  const Sentence s = sentence(a, b);
-  if (t < s.first || t - s.first >= s.rows || (int64_t)s.rows * a.G > a.few) return;
-  const int2 place = a.place[b];
-  const int r = (t - s.first) * a.G + head - h * a.G;
-  const size_t from = ((size_t)(place.x + h) * a.row_tiles + r / 16) * 16 + r % 16, next = (size_t)a.c.H * a.row_tiles * 16;
-  const float m = lane < place.y ? a.m[from + lane * next] : -INFINITY, l = lane < place.y ? a.l[from + lane * next] : 0.0f;
-  float top = m;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) top = fmaxf(top, __shfl_xor(top, off, kWave));
-  // a piece without a maximum saw nothing, or nothing but NaN
-  const float factor = m == -INFINITY ? (l != 0.0f ? NAN : 0.0f) : __builtin_amdgcn_exp2f(m - top);
-  const float total = wave_sum(m == -INFINITY ? l : l * factor);
-  float sum[D / 64] = {};
-  for (int i = 0; i < place.y; ++i) {
-    const float f = __shfl(factor, i, kWave);
-    const float* o = a.o + (from + i * next) * D + lane * (D / 64);
-#pragma unroll
-    for (int c = 0; c < D / 64; ++c) sum[c] += f == 0.0f ? 0.0f : f * o[c];
+  for (int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); at < (int64_t)a.T * Hq; at += (int64_t)gridDim.x * 4) {   // row of out
+    const int t = (int)(at / Hq), head = (int)(at - (int64_t)t * Hq), h = head / a.G;
+    const int b = sentence_of(a.first, a.c.B, t);
+    const Sentence s = sentence(a, b);
+    if (t < s.first || t - s.first >= s.rows || (int64_t)s.rows * a.G > a.few) continue;
+    const int2 place = a.place[b];
+    const int r = (t - s.first) * a.G + head - h * a.G;
+    const size_t from = ((size_t)(place.x + h) * a.row_tiles + r / 16) * 16 + r % 16, next = (size_t)a.c.H * a.row_tiles * 16;
+    const float m = lane < place.y ? a.m[from + lane * next] : -INFINITY, l = lane < place.y ? a.l[from + lane * next] : 0.0f;
+    float top = m;
+  #pragma unroll
+    for (int off = 1; off < 64; off <<= 1) top = fmaxf(top, __shfl_xor(top, off, kWave));
+    // a piece without a maximum saw nothing, or nothing but NaN
+    const float factor = m == -INFINITY ? (l != 0.0f ? NAN : 0.0f) : __builtin_amdgcn_exp2f(m - top);
+    const float total = wave_sum(m == -INFINITY ? l : l * factor);
+    float sum[D / 64] = {};
+    for (int i = 0; i < place.y; ++i) {
+      const float f = __shfl(factor, i, kWave);
+      const float* o = a.o + (from + i * next) * D + lane * (D / 64);
+  #pragma unroll
+      for (int c = 0; c < D / 64; ++c) sum[c] += f == 0.0f ? 0.0f : f * o[c];
+    }
+    const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
+    typename E::T* dst = reinterpret_cast<typename E::T*>(a.out) + at * D + lane * (D / 64);
+  #pragma unroll
+    for (int c = 0; c < D / 64; ++c) dst[c] = from_float<E>(sum[c] * inverse);
+    if (lane == 0) store_lse(a, at, top, total);
   }
-  const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
-  typename E::T* dst = reinterpret_cast<typename E::T*>(a.out) + at * D + lane * (D / 64);
-#pragma unroll
-  for (int c = 0; c < D / 64; ++c) dst[c] = from_float<E>(sum[c] * inverse);
-  if (lane == 0) store_lse(a, at, top, total);
 }
 
 template <class E, int D>
@@ -376,7 +376,7 @@ int launch_rows(const KvpAttend& a, hipStream_t s) {
   hipLaunchKernelGGL((gemm_kvp_rows_kernel<E, D>), dim3((unsigned)a.blocks, (unsigned)a.row_tiles), dim3(256), 0, s, a);
   CI_HIP_CHECK_LAUNCH();
   if (a.wanted) {
-    hipLaunchKernelGGL((kvp_join_kernel<E, D>), dim3((unsigned)(((int64_t)a.T * a.c.H * a.G + 3) / 4)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((kvp_join_kernel<E, D>), dim3(join_blocks((int64_t)a.T * a.c.H * a.G)), dim3(256), 0, s, a);
     CI_HIP_CHECK_LAUNCH();
   }
   return CI_OK;

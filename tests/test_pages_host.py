@@ -134,7 +134,7 @@ def test_append_refuses(lib):
 def test_attend_refuses(lib):
     for kw in (dict(q=None), dict(st=None), dict(first=None), dict(lens=None), dict(out=None), dict(Hq=4), dict(Hq=0), dict(Hq=3 * 4097),
                dict(T=1 << 21), dict(rows=0), dict(max_len=0), dict(max_len=65), dict(window=-1), dict(sinks=-1), dict(scale=0.0),
-               dict(scale=-1.0), dict(scale=math.nan), dict(scale=3e38), dict(T=1 << 20, Hq=3 * 512)):
+               dict(scale=-1.0), dict(scale=math.nan), dict(scale=3e38), dict(T=1 << 20, Hq=1026)):
         assert _attend(lib, **kw) == lib.CI_ERR_INVALID_ARG, kw
     for kw in (dict(q=F + 1), dict(out=F + 8), dict(first=F + 2), dict(lens=F + 1), dict(lse=F + 2), dict(st=_strides(-8, 8))):
         assert _attend(lib, **kw) == lib.CI_ERR_BAD_LAYOUT, kw
