@@ -8,12 +8,13 @@ namespace ci {
 struct Kvp {
   void *k, *v;
   const int32_t* table;
-  int64_t pages, most;
+  int64_t most;
+  uint32_t pages;
   int B, H, shift;   // page = 1 << shift slots
 };
 
 inline Kvp make_kvp(const ci_kvp& c) {
-  return Kvp{c.k, c.v, c.table, c.pages, c.most, (int)c.B, c.H, __builtin_ctz((unsigned)c.page)};
+  return Kvp{c.k, c.v, c.table, c.most, (uint32_t)c.pages, (int)c.B, c.H, __builtin_ctz((unsigned)c.page)};
 }
 
 // The sentence of a packed row: the last one that does not begin behind it.  The lanes of a wave look at 64 beginnings at once, so that up to
@@ -29,6 +30,26 @@ __device__ __forceinline__ int sentence_of(const int32_t* __restrict__ first, in
     n = min(step, n - last * step);
   }
   return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// Sums (of integers) or maxima (of those from 0 on) over the lanes up to each, by moves between lanes instead of through the LDS.
+__device__ __forceinline__ int scan_add(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);   // one, two, four, eight lanes on within 16
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);   // the last of 16 to the next 16, of 32 to the next 32
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+  return v;
+}
+__device__ __forceinline__ int scan_max(int v) {
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false));
+  return v;
 }
 
 // The packed rows of a sentence, as the calls' limits take them.

@@ -13,10 +13,10 @@ struct AttendPlan {
   bool rows, in_tiles;   // which kernels run
   int few, row_tiles, blocks, wanted, least;
   int tiles, pieces;
-  size_t place, m, l, o, tile_m, tile_l, tile_o, bytes;   // places in the workspace
+  size_t place, m, l, o, tile_m, tile_l, tile_exact, tile_o, bytes;   // places in the workspace
 };
 
-constexpr int kTileRows = 128;
+constexpr int kTileRows = 256;
 
 // Most steps of `step` slots that the rows of a sentence see something of.
 int64_t most_steps(int64_t step, int64_t rows, int64_t max_len, int64_t window, int64_t sinks) {
@@ -56,12 +56,13 @@ AttendPlan attend_plan(const ci_kvp& c, int64_t T, int64_t G, int64_t max_rows, 
   if (p.in_tiles) {
     p.tiles = (int)(T * G / kTileRows + c.B);   // see tile_start
     const int64_t full = std::max<int64_t>(1, T * G / kTileRows) * c.H, steps = most_steps(64, max_rows, max_len, window, sinks);
-    // Two workgroups a compute unit are what fits; no piece below eight steps.
-    p.pieces = (int)std::max<int64_t>(1, std::min<int64_t>({2 * kCus / full, steps / 8, kMaxPieces}));
+    // No piece below eight steps.
+    p.pieces = (int)std::max<int64_t>(1, std::min<int64_t>({kCus / full, steps / 8, kMaxPieces}));
     if (p.pieces > 1) {
       const size_t rows = (size_t)p.tiles * c.H * p.pieces * kTileRows;
       p.tile_m = take(rows);
       p.tile_l = take(rows);
+      p.tile_exact = take(rows);
       p.tile_o = take(rows * c.D);
     }
   }
@@ -106,11 +107,13 @@ int launch_kvp_attend(const ci_kvp& c, const void* q, int64_t G, const int64_t (
   a.blocks = p.blocks;
   a.wanted = p.wanted;
   a.least = p.least;
+  a.join_rows = (int)std::max<int64_t>(1, std::min<int64_t>(max_rows, p.few / G));
   a.tiles = p.tiles;
   a.tile_rows = kTileRows;
   a.pieces = p.pieces;
   a.tile_m = reinterpret_cast<float*>(base + p.tile_m);
   a.tile_l = reinterpret_cast<float*>(base + p.tile_l);
+  a.tile_exact = reinterpret_cast<float*>(base + p.tile_exact);
   a.tile_o = reinterpret_cast<float*>(base + p.tile_o);
   switch (c.dtype) {
     case CI_F32: return launch_kvp_attend_type<F32>(a, c.D, p.rows, p.in_tiles, s);

@@ -25,12 +25,12 @@ struct KvpAttend {
   int q_vectors;
   // Few rows: `row_tiles` tiles of 16 rows a head (what more rows a sentence has, others do); the slots of all sentences in `wanted` pieces
   // and one more a head, none below `least` steps; wanted 0: one piece a head.
-  int few, row_tiles, blocks, wanted, least;
+  int few, row_tiles, blocks, wanted, least, join_rows;   // join_rows: packed rows of such a sentence at most
   int2* place;        // [B]: a sentence's first piece and how many a head has
   float *m, *l, *o;   // [blocks, row_tiles 16] twice and [.., D]
   // Prompts: `tiles` tiles of tile_rows rows at most, the steps of each in `pieces`.
   int tiles, tile_rows, pieces;
-  float *tile_m, *tile_l, *tile_o;   // [tiles H, pieces, tile_rows] twice and [.., D]
+  float *tile_m, *tile_l, *tile_exact, *tile_o;   // [tiles H, pieces, tile_rows] three times (the third for lse) and [.., D]
 };
 
 // rows, tiles: which of the kernels
@@ -54,19 +54,27 @@ __device__ __forceinline__ f32x4 product16_f32(float a, float b, const f32x4& c)
   return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
 
-// Two numbers rounded to E, and what that leaves of them.
+// Two numbers rounded to E (one instruction), and what that leaves of them.
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 template <class E>
 __device__ __forceinline__ uint32_t pair_of(float x, float y) {
-  const typename E::T t[2] = {from_float<E>(x), from_float<E>(y)};
-  uint32_t u;
-  __builtin_memcpy(&u, t, sizeof(u));
-  return u;
+  const f32x2 v = {x, y};
+  if constexpr (__is_same(E, F16))
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, half2_t));
+  else
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+}
+template <class E>
+__device__ __forceinline__ f32x2 both_of(uint32_t u) {
+  if constexpr (__is_same(E, F16)) return __builtin_convertvector(__builtin_bit_cast(half2_t, u), f32x2);
+  else return f32x2{u2f(u << 16), u2f(u & 0xffff0000u)};
 }
 template <class E>
 __device__ __forceinline__ void two_pieces(float x, float y, uint32_t* high, uint32_t* low) {
-  typename E::T t[2] = {from_float<E>(x), from_float<E>(y)};
-  __builtin_memcpy(high, t, sizeof(*high));
-  *low = pair_of<E>(x - to_float<E>(t[0]), y - to_float<E>(t[1]));
+  *high = pair_of<E>(x, y);
+  const f32x2 t = both_of<E>(*high);
+  *low = pair_of<E>(x - t[0], y - t[1]);
 }
 
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }   // false for NaN
@@ -82,6 +90,12 @@ __device__ __forceinline__ Sentence sentence(const KvpAttend& a, int b) {
   return Sentence{from, min(n, a.max_rows), len, len - n};
 }
 
+// The same in scalar registers, for a sentence that all lanes share.
+__device__ __forceinline__ Sentence uniform(const Sentence& s) {
+  return Sentence{__builtin_amdgcn_readfirstlane(s.first), __builtin_amdgcn_readfirstlane(s.rows), __builtin_amdgcn_readfirstlane(s.len),
+                  __builtin_amdgcn_readfirstlane(s.slot)};
+}
+
 // Steps of STEP slots that rows in slots p0 .. p1 see something of: `sinks` of them from the first slot on, then those from `window` on.
 template <int STEP>
 struct Steps {
@@ -95,8 +109,9 @@ struct Steps {
   __device__ int slot(int step) const { return (step < sinks ? step : window + step - sinks) * STEP; }
 };
 
+// Without a branch for each of a lane's logits.
 __device__ __forceinline__ bool sees(const KvpAttend& a, int p, int t) {
-  return t <= p && (a.window == 0 || t > p - a.window || t < a.sinks);
+  return (t <= p) & ((a.window == 0) | (t > p - a.window) | (t < a.sinks));
 }
 
 // A sentence's pages.  Slots from the last one in use on read that one, which is as finite as the rest.
@@ -108,7 +123,7 @@ struct Pages {
   // Page of a slot; -1: none.
   __device__ int of(const KvpAttend& a, int slot) const {
     const int n = table[min(slot, last) >> a.c.shift];
-    return n >= 0 && n < a.c.pages ? n : -1;
+    return (uint32_t)n < a.c.pages ? n : -1;   // pages below 2^31
   }
 };
 // Elements from the pages' start to the first slot of a head in a page; page -1: of page 0, whatever lies there.
@@ -128,8 +143,8 @@ __device__ __forceinline__ void store_row4(const KvpAttend& a, int D, int64_t at
 __device__ __forceinline__ void store_lse(const KvpAttend& a, int64_t at, float m, float l) {
   if (a.lse) a.lse[at] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
 }
-// Workgroups of four waves for that many rows, each a wave's; beyond, a wave takes several.
-inline unsigned join_blocks(int64_t rows) { return (unsigned)((rows + 3) / 4 < 65536 ? (rows + 3) / 4 : 65536); }
+// Workgroups for that many pieces of work; beyond, one takes several.
+inline unsigned join_blocks(int64_t n) { return (unsigned)(n < 262144 ? n : 262144); }
 
 // Packed row and head of row r of head h of the cache, as a row of out.
 __device__ __forceinline__ int64_t out_row(const KvpAttend& a, const Sentence& s, int h, int r) {
@@ -139,22 +154,22 @@ __device__ __forceinline__ int64_t out_row(const KvpAttend& a, const Sentence& s
 
 // One row over steps begin .. end - 1 by a whole workgroup, slot by slot, without the slots that it does not see: what the matrix cores cannot leave
 // out when a value that a row does not see is infinite or NaN, because they multiply it by 0.  o: of the D threads that have a channel each.
-// lds: 260 floats.
-template <class E, int D, int STEP>
+// lds: THREADS + 16 floats.
+template <class E, int D, int STEP, int THREADS>
 __device__ __forceinline__ void careful_row(const KvpAttend& a, const Sentence& s, const Pages& pages, int h, int r, const Steps<STEP>& steps,
                                             int begin, int end, float* lds, float* m_out, float* l_out, float* o_out) {
   using T = typename E::T;
-  const int tid = threadIdx.x, i = r / a.G, p = s.slot + i;
+  const int tid = threadIdx.x, i = r / a.G, p = s.slot + i, inside = (1 << a.c.shift) - 1;
   const T* q = reinterpret_cast<const T*>(a.q) + (int64_t)(s.first + i) * a.q_t + (int64_t)(h * a.G + r - i * a.G) * a.q_h;
   float m = -INFINITY, l = 0.0f, o = 0.0f;
-  const int64_t slots = (int64_t)(end - begin) * STEP;
-  for (int64_t from = 0; from < slots; from += 256) {
-    const int64_t mine = from + tid;
+  const int slots = (end - begin) * STEP;   // below 2^25
+  auto slot_of = [&](int n) { return steps.slot(begin + n / STEP) + n % STEP; };
+  for (int from = 0; from < slots; from += THREADS) {
     float z = -INFINITY;
-    if (mine < slots) {
-      const int t = steps.slot(begin + (int)(mine / STEP)) + (int)(mine % STEP), page = t < s.len ? pages.of(a, t) : -1;
-      if (page >= 0 && t < s.len && sees(a, p, t)) {
-        const T* k = reinterpret_cast<const T*>(a.c.k) + page_start<D>(a, page, h) + (t & ((1 << a.c.shift) - 1)) * D;
+    if (from + tid < slots) {
+      const int t = slot_of(from + tid), page = t < s.len ? pages.of(a, t) : -1;
+      if (page >= 0 && sees(a, p, t)) {
+        const T* k = reinterpret_cast<const T*>(a.c.k) + page_start<D>(a, page, h) + (t & inside) * D;
         float sum = 0.0f;
         for (int d = 0; d < D; ++d) sum = __builtin_fmaf(to_float<E>(k[d]), to_float<E>(q[d]), sum);
         z = sum * a.scale;
@@ -163,9 +178,9 @@ __device__ __forceinline__ void careful_row(const KvpAttend& a, const Sentence& 
     float top = z != z ? INFINITY : z;   // a NaN makes everything NaN
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, kWave));
-    if ((tid & 63) == 0) lds[256 + (tid >> 6)] = top;
+    if ((tid & 63) == 0) lds[THREADS + (tid >> 6)] = top;
     __syncthreads();
-    top = fmaxf(fmaxf(lds[256], lds[257]), fmaxf(lds[258], lds[259]));
+    for (int w = 0; w < THREADS / 64; ++w) top = fmaxf(top, lds[THREADS + w]);
     const float next = fmaxf(m, top), ref = next == -INFINITY ? 0.0f : next;
     // seen, but too small for fp32: not nothing, as it is multiplied by what may be infinite
     lds[tid] = z == -INFINITY ? 0.0f : z != z ? z : fmaxf(__builtin_amdgcn_exp2f(z - ref), 1e-37f);
@@ -174,13 +189,13 @@ __device__ __forceinline__ void careful_row(const KvpAttend& a, const Sentence& 
     m = next;
     l *= was;
     o *= was;
-    for (int e = 0; e < 256 && from + e < slots; ++e) {
+    for (int e = 0; e < THREADS && from + e < slots; ++e) {
       const float w = lds[e];
       if (w == 0.0f) continue;
       l += w;
       if (tid < D) {
-        const int t = steps.slot(begin + (int)((from + e) / STEP)) + (int)((from + e) % STEP);
-        const T* v = reinterpret_cast<const T*>(a.c.v) + page_start<D>(a, pages.of(a, t), h) + (t & ((1 << a.c.shift) - 1)) * D;
+        const int t = slot_of(from + e);
+        const T* v = reinterpret_cast<const T*>(a.c.v) + page_start<D>(a, pages.of(a, t), h) + (t & inside) * D;
         o += w * to_float<E>(v[tid]);
       }
     }

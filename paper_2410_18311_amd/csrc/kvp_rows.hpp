@@ -11,66 +11,65 @@ namespace ci {
 namespace {
 
 // How the slots are shared out: pieces of `chunk` steps, so that a long sentence among short ones has as many workgroups as its
-// length asks for.  Everything follows from first and lens, in every wave for itself.
-struct PieceShares {
+// length asks for.  Everything follows from first and lens, in every wave for itself, a sentence a lane.
+struct Piece {
+  Sentence s;
+  int b, before, pieces, steps;   // the sentence, the pieces before its own, how many a head has, the steps of all; b = B: no such piece
   int chunk;
-  // Steps of a sentence that has few rows; -1: another's work, or none.
-  __device__ static int steps_of(const KvpAttend& a, int b) {
-    const Sentence s = sentence(a, b);
-    if (s.rows == 0 || (int64_t)s.rows * a.G > a.few) return -1;
-    return Steps<32>(a, max(s.slot, 0), s.slot + s.rows - 1, s.len).total;
-  }
-  // At least one piece: it writes the zeros of rows that see nothing.
-  __device__ int count(int steps) const { return steps < 0 ? 0 : max(1, (steps + chunk - 1) / chunk); }
-
-  __device__ explicit PieceShares(const KvpAttend& a) {
-    if (a.wanted == 0) {
-      chunk = 1 << 30;
-      return;
-    }
-    int64_t total = 0;
-    int longest = 0;
-    for (int b = threadIdx.x & 63; b < a.c.B; b += 64) {
-      const int n = max(steps_of(a, b), 0);
-      total += n;
-      longest = max(longest, n);
-    }
-    if (a.c.B > 1) {
-#pragma unroll
-      for (int off = 1; off < 64; off <<= 1) {
-        total += __shfl_xor(total, off, kWave);
-        longest = max(longest, __shfl_xor(longest, off, kWave));
-      }
-    }
-    // all pieces together are at most wanted + B H: a sentence's last one need not be full
-    const int64_t even = (total * a.c.H + a.wanted - 1) / a.wanted, least = max(a.least, (longest + kMaxPieces - 1) / kMaxPieces);
-    chunk = __builtin_amdgcn_readfirstlane((int)((max(even, least) + 3) / 4 * 4));
-  }
-  // The sentence of piece `at` and the pieces before that sentence's; b = B where there is no such piece.
-  __device__ void find(const KvpAttend& a, int at, int* b, int* before) const {
+  __device__ Piece(const KvpAttend& a, int at) {
     const int lane = threadIdx.x & 63;
-    int base = 0;
-    for (int b0 = 0; b0 < a.c.B; b0 += 64) {
-      const int mine = b0 + lane < a.c.B ? count(steps_of(a, b0 + lane)) * a.c.H : 0;
-      int upto = mine;
-      if (a.c.B > 1) {
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-          const int n = __shfl_up(upto, off, kWave);
-          if (lane >= off) upto += n;
+    Sentence own{0, 0, 0, 0};
+    int mine = -1;   // steps of the lane's sentence; -1: another's work, or none
+    auto look = [&](int b0) {
+      mine = -1;
+      if (b0 + lane >= a.c.B) return;
+      own = sentence(a, b0 + lane);
+      if (own.rows > 0 && (int64_t)own.rows * a.G <= a.few)
+        mine = Steps<32>(a, max(own.slot, 0), own.slot + own.rows - 1, own.len).total;
+    };
+    look(0);
+    chunk = 1 << 30;
+    if (a.wanted) {
+      int64_t total = 0;
+      int longest = 0;
+      for (int b0 = 0;;) {
+        const int v = max(mine, 0);
+        if (a.c.B == 1) {
+          total = longest = __builtin_amdgcn_readfirstlane(v);
+        } else {
+          total += __builtin_amdgcn_readlane(scan_add(v), 63);
+          longest = max(longest, __builtin_amdgcn_readlane(scan_max(v), 63));
         }
+        b0 += 64;
+        if (b0 >= a.c.B) break;
+        look(b0);
       }
-      const uint64_t past = __ballot(base + upto > at);
+      if (a.c.B > 64) look(0);
+      // all pieces together are at most wanted + B H: a sentence's last one need not be full
+      const int64_t even = (total * a.c.H + a.wanted - 1) / a.wanted, least = max(a.least, (longest + kMaxPieces - 1) / kMaxPieces);
+      chunk = (int)((max(even, least) + 3) / 4 * 4);
+    }
+    int base = 0;
+    for (int b0 = 0;;) {
+      // at least one piece: it writes the zeros of rows that see nothing
+      const int count = mine < 0 ? 0 : max(1, (mine + chunk - 1) / chunk), upto = a.c.B == 1 ? count : scan_add(count);
+      const uint64_t past = __ballot(base + upto * a.c.H > at);
       if (past) {
         const int hit = __builtin_ctzll(past);
-        *b = b0 + hit;
-        *before = base + __shfl(upto - mine, hit, kWave);
+        b = b0 + hit;
+        pieces = __builtin_amdgcn_readlane(count, hit);
+        before = base + (__builtin_amdgcn_readlane(upto, hit) - pieces) * a.c.H;
+        steps = __builtin_amdgcn_readlane(mine, hit);
+        s = Sentence{__builtin_amdgcn_readlane(own.first, hit), __builtin_amdgcn_readlane(own.rows, hit),
+                     __builtin_amdgcn_readlane(own.len, hit), __builtin_amdgcn_readlane(own.slot, hit)};
         return;
       }
-      base += __shfl(upto, 63, kWave);
+      base += __builtin_amdgcn_readlane(upto, 63) * a.c.H;
+      b0 += 64;
+      if (b0 >= a.c.B) break;
+      look(b0);
     }
-    *b = a.c.B;
-    *before = base;
+    b = a.c.B;
   }
 };
 
@@ -126,19 +125,16 @@ __global__ __launch_bounds__(256, E::BYTES == 4 ? 2 : 3) void gemm_kvp_rows_kern
   __shared__ unsigned broken;   // rows, a bit each
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const PieceShares shares(a);
-  int b, before;
-  shares.find(a, blockIdx.x, &b, &before);
-  b = __builtin_amdgcn_readfirstlane(b);
-  before = __builtin_amdgcn_readfirstlane(before);
+  const Piece found(a, blockIdx.x);
+  const int b = found.b;
   if (b >= a.c.B) return;
-  const int h = ((int)blockIdx.x - before) % a.c.H, piece = ((int)blockIdx.x - before) / a.c.H;
-  const Sentence s = sentence(a, b);
+  const int piece = ((int)blockIdx.x - found.before) / a.c.H, h = (int)blockIdx.x - found.before - piece * a.c.H;
+  const Sentence s = found.s;
   const int R = s.rows * a.G;
   const Steps<32> steps(a, max(s.slot, 0), s.slot + s.rows - 1, s.len);
-  const int pieces = shares.count(steps.total);
-  if (a.wanted && (int)blockIdx.x == before && blockIdx.y == 0 && threadIdx.x == 0) a.place[b] = make_int2(before, pieces);   // for the join
-  const int begin = min(steps.total, piece * shares.chunk), end = min(steps.total, begin + min(shares.chunk, steps.total));
+  if (a.wanted && (int)blockIdx.x == found.before && blockIdx.y == 0 && threadIdx.x == 0)
+    a.place[b] = make_int2(found.before, found.pieces);   // for the join
+  const int begin = min(steps.total, piece * found.chunk), end = min(steps.total, begin + min(found.chunk, steps.total));
   const Pages pages(a, b, s.len);
   const int inside = (1 << a.c.shift) - 1;
   for (int tile = blockIdx.y; tile * 16 < R; tile += gridDim.y) {
@@ -215,7 +211,7 @@ __global__ __launch_bounds__(256, E::BYTES == 4 ? 2 : 3) void gemm_kvp_rows_kern
   #pragma unroll
           for (int r = 0; r < 4; ++r) {
             z[i][r] *= a.scale;
-            if (masked && (page[i] < 0 || !sees(a, p, t + 16 * i + 4 * g + r))) z[i][r] = -INFINITY;
+            if (masked) z[i][r] = ((page[i] >= 0) & sees(a, p, t + 16 * i + 4 * g + r)) ? z[i][r] : -INFINITY;
           }
         float top = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])), fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])));
         // The maximum is raised only when a logit passes it by 2^8; the sums hold that range in fp32.
@@ -320,7 +316,7 @@ __global__ __launch_bounds__(256, E::BYTES == 4 ? 2 : 3) void gemm_kvp_rows_kern
     for (unsigned left = broken; left; left &= left - 1) {
       const int r = __builtin_ctz(left);
       float mr, lr, o;
-      careful_row<E, D, 32>(a, s, pages, h, row0 + r, steps, begin, end, &sums[0][0][0], &mr, &lr, &o);
+      careful_row<E, D, 32, 256>(a, s, pages, h, row0 + r, steps, begin, end, &sums[0][0][0], &mr, &lr, &o);
       if (a.wanted) {
         if (threadIdx.x < D) a.o[(part + r) * D + threadIdx.x] = o;
         if (threadIdx.x == 0) {
@@ -337,37 +333,50 @@ __global__ __launch_bounds__(256, E::BYTES == 4 ? 2 : 3) void gemm_kvp_rows_kern
   }
 }
 
-// The pieces of a row put together, a wave a row.
+// The pieces of a row put together, a workgroup a row: a wave takes every fourth, all of which it requests at once.
 template <class E, int D>
 __global__ __launch_bounds__(256) void kvp_join_kernel(KvpAttend a) {
-  const int Hq = a.c.H * a.G, lane = threadIdx.x & 63;
-  for (int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); at < (int64_t)a.T * Hq; at += (int64_t)gridDim.x * 4) {   // row of out
-    const int t = (int)(at / Hq), head = (int)(at - (int64_t)t * Hq), h = head / a.G;
-    const int b = sentence_of(a.first, a.c.B, t);
+  constexpr int N = kMaxPieces / 4, C = D / 64;
+  __shared__ float sums[4][D];
+  const int Hq = a.c.H * a.G, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  for (int64_t each = blockIdx.x; each < (int64_t)a.c.B * a.join_rows * Hq; each += gridDim.x) {
+    const int b = (int)(each / (a.join_rows * Hq)), in = (int)(each - (int64_t)b * a.join_rows * Hq);
+    const int i = in / Hq, head = in - i * Hq, h = head / a.G;
     const Sentence s = sentence(a, b);
-    if (t < s.first || t - s.first >= s.rows || (int64_t)s.rows * a.G > a.few) continue;
-    const int2 place = a.place[b];
-    const int r = (t - s.first) * a.G + head - h * a.G;
+    const int2 place = a.place[b];   // written for sentences that have few rows only
+    if (i >= s.rows || (int64_t)s.rows * a.G > a.few) continue;
+    const int r = i * a.G + head - h * a.G;
+    const int64_t at = (int64_t)(s.first + i) * Hq + head;   // row of out
     const size_t from = ((size_t)(place.x + h) * a.row_tiles + r / 16) * 16 + r % 16, next = (size_t)a.c.H * a.row_tiles * 16;
     const float m = lane < place.y ? a.m[from + lane * next] : -INFINITY, l = lane < place.y ? a.l[from + lane * next] : 0.0f;
+    float o[N][C];
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+      if (wave + 4 * n < place.y) __builtin_memcpy(o[n], a.o + (from + (wave + 4 * n) * next) * D + lane * C, sizeof(o[n]));
     float top = m;
-  #pragma unroll
+#pragma unroll
     for (int off = 1; off < 64; off <<= 1) top = fmaxf(top, __shfl_xor(top, off, kWave));
     // a piece without a maximum saw nothing, or nothing but NaN
     const float factor = m == -INFINITY ? (l != 0.0f ? NAN : 0.0f) : __builtin_amdgcn_exp2f(m - top);
     const float total = wave_sum(m == -INFINITY ? l : l * factor);
-    float sum[D / 64] = {};
-    for (int i = 0; i < place.y; ++i) {
-      const float f = __shfl(factor, i, kWave);
-      const float* o = a.o + (from + i * next) * D + lane * (D / 64);
-  #pragma unroll
-      for (int c = 0; c < D / 64; ++c) sum[c] += f == 0.0f ? 0.0f : f * o[c];
+    float sum[C] = {};
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      if (wave + 4 * n >= place.y) continue;
+      const float f = __shfl(factor, wave + 4 * n, kWave);
+#pragma unroll
+      for (int c = 0; c < C; ++c) sum[c] += f == 0.0f ? 0.0f : f * o[n][c];
     }
-    const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
-    typename E::T* dst = reinterpret_cast<typename E::T*>(a.out) + at * D + lane * (D / 64);
-  #pragma unroll
-    for (int c = 0; c < D / 64; ++c) dst[c] = from_float<E>(sum[c] * inverse);
-    if (lane == 0) store_lse(a, at, top, total);
+#pragma unroll
+    for (int c = 0; c < C; ++c) sums[wave][lane * C + c] = sum[c];
+    __syncthreads();
+    if (threadIdx.x < D) {
+      const int d = threadIdx.x;
+      const float v = (sums[0][d] + sums[1][d]) + (sums[2][d] + sums[3][d]);
+      reinterpret_cast<typename E::T*>(a.out)[at * D + d] = from_float<E>(total == 0.0f ? 0.0f : v * (1.0f / total));
+      if (d == 0) store_lse(a, at, top, total);
+    }
+    __syncthreads();
   }
 }
 
@@ -376,7 +385,7 @@ int launch_rows(const KvpAttend& a, hipStream_t s) {
   hipLaunchKernelGGL((gemm_kvp_rows_kernel<E, D>), dim3((unsigned)a.blocks, (unsigned)a.row_tiles), dim3(256), 0, s, a);
   CI_HIP_CHECK_LAUNCH();
   if (a.wanted) {
-    hipLaunchKernelGGL((kvp_join_kernel<E, D>), dim3(join_blocks((int64_t)a.T * a.c.H * a.G)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((kvp_join_kernel<E, D>), dim3(join_blocks((int64_t)a.c.B * a.join_rows * a.c.H * a.G)), dim3(256), 0, s, a);
     CI_HIP_CHECK_LAUNCH();
   }
   return CI_OK;

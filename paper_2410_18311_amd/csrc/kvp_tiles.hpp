@@ -21,6 +21,7 @@ __device__ __forceinline__ f32x16 mfma32(const uint4& a, const uint4& b, const f
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
+constexpr int kSchedProduct = 0x8, kSchedLds = 0x100;   // kinds of instructions for the compiler's scheduler: matrix products, reads of the LDS
 constexpr int kTileStep = 64;   // slots of a step
 
 // Rows of D channels in the LDS, 16-byte chunk c of row r in the place c ^ swizzle(r), so that what 16 lanes read at once lies in
@@ -29,6 +30,20 @@ template <int D>
 __device__ __forceinline__ int key_swizzle(int r) { return D == 128 ? r & 15 : r >> 1 & 7; }
 template <int D>
 __device__ __forceinline__ int value_swizzle(int r) { return (D == 128 ? r & 3 : r >> 1 & 1) << 2; }
+
+// load_to_lds that is no access of memory to the compiler: it writes a buffer that nobody reads before the next meeting of the waves.
+__device__ __forceinline__ void load_ahead(uint32_t lds, uint32_t off, i32x4 rsrc) {
+  uint32_t m0;
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds" : "={m0}"(m0) : "s"(lds), "v"(off), "s"(rsrc));
+}
+// Two numbers added to a sum.
+template <class E>
+__device__ __forceinline__ float add_pair(uint32_t u, float sum) {
+  if constexpr (__is_same(E, F16))
+    return __builtin_amdgcn_fdot2(__builtin_bit_cast(half2_t, u), half2_t{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
+  else
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, u), bf16x2{(__bf16)1.0f, (__bf16)1.0f}, sum, false);
+}
 
 // Where the tiles of a sentence begin among all: each has at least as many as its rows fill, whatever `rows` of a tile.
 __device__ __forceinline__ int64_t tile_start(const KvpAttend& a, int b, int rows) {
@@ -47,21 +62,22 @@ __device__ __forceinline__ int sentence_of_tile(const KvpAttend& a, int tile, in
   return __builtin_amdgcn_readfirstlane(lo);
 }
 
-template <class E, int D, int WAVES>
+template <class E, int D, int WAVES, bool LSE>
 __global__ __launch_bounds__(64 * WAVES, 2) void gemm_kvp_tiles_kernel(KvpAttend a) {
   constexpr int BM = 32 * WAVES, ROW = 2 * D, HALF = kTileStep * ROW, KK = D / 16, CB = D / 32;
   constexpr int LOADS = HALF / 1024 / WAVES, ROWS = 1024 / ROW;   // loads of a wave and tensor, rows of a load
-  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];   // [2][keys, values][64 rows]
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];   // three steps' keys and three steps' values, 64 rows each
   __shared__ unsigned broken[WAVES];
+  __shared__ int missing[WAVES];   // whether a wave has met slots without a page
   const int lane = threadIdx.x & 63, n = lane & 31, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = blockIdx.x % a.c.H, tile = a.tiles - 1 - (int)(blockIdx.x / a.c.H);   // the last tiles of a prompt see most
   const int b = sentence_of_tile(a, tile, BM);
-  const Sentence s = sentence(a, b);
+  const Sentence s = uniform(sentence(a, b));
   const int R = s.rows * a.G;
   const int64_t local = tile - tile_start(a, b, BM);
   if (R <= a.few || local < 0 || local * BM >= R) return;
-  const int row0 = (int)local * BM, mine0 = row0 + 32 * wave;   // of the tile, of the wave
+  const int row0 = __builtin_amdgcn_readfirstlane((int)local) * BM, mine0 = row0 + 32 * wave;   // of the tile, of the wave
   const bool live = mine0 < R;
   const int row = min(mine0 + n, R - 1), p = s.slot + row / a.G;
   const int p_low = s.slot + min(mine0, R - 1) / a.G, p_high = s.slot + min(mine0 + 31, R - 1) / a.G;
@@ -88,106 +104,217 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_kvp_tiles_kernel(KvpAttend
     }
   }
 
-  // A wave fetches LOADS * ROWS neighbouring rows of a step, which are of one page.
-  const int fetch_row = lane / (ROW / 16), fetch_chunk = lane % (ROW / 16);
-  auto fetch = [&](int step, int buffer) {
-    const int t = steps.slot(step) + wave * LOADS * ROWS;
-    const int page = pages.of(a, t);
-    const int64_t at = page_start<D>(a, page, h) * 2;
-    const i32x4 k = rsrc_at(reinterpret_cast<const char*>(a.c.k) + at), v = rsrc_at(reinterpret_cast<const char*>(a.c.v) + at);
+  // A wave fetches LOADS * ROWS neighbouring rows of a step's keys and values, which are of one page; what lies behind the last slot in use comes as
+  // zeros.  off: the lane's 16 bytes of a load.
+  const int fetch_row = lane / (ROW / 16), fetch_chunk = lane % (ROW / 16), fetch_from = wave * LOADS * ROWS;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) unsigned char*)smem + fetch_from * ROW;
+  int key_off[LOADS], value_off[LOADS];
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const int r = wave * LOADS * ROWS + i * ROWS + fetch_row;
-      const int from = (min(t + i * ROWS + fetch_row, pages.last) & inside) * ROW;
-      unsigned char* to = smem + buffer * 2 * HALF + (wave * LOADS + i) * 1024;
-      load_to_lds(to, from + 16 * (fetch_chunk ^ key_swizzle<D>(r)), k);
-      load_to_lds(to + HALF, from + 16 * (fetch_chunk ^ value_swizzle<D>(r)), v);
-    }
+  for (int i = 0; i < LOADS; ++i) {
+    const int r = i * ROWS + fetch_row;
+    key_off[i] = r * ROW + 16 * (fetch_chunk ^ key_swizzle<D>(fetch_from + r));
+    value_off[i] = r * ROW + 16 * (fetch_chunk ^ value_swizzle<D>(fetch_from + r));
+  }
+  auto rows_at = [&](int step, int page, const void* tensor) {
+    const int t = steps.slot(step) + fetch_from;
+    const int64_t at = page_start<D>(a, page, h) * 2 + (t & inside) * ROW;
+    i32x4 r = rsrc_at(reinterpret_cast<const char*>(tensor) + at);
+    int rows = max(s.len - t, 0);
+    asm("" : "+s"(rows));   // else the two become one vector instruction
+    r[2] = min(rows, kTileStep) * ROW;
+    return r;
   };
+  auto fetch = [&](int step, int page, const void* tensor, int place, bool keys) {
+    const i32x4 rsrc = rows_at(step, page, tensor);
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) load_ahead(lds0 + place * HALF + i * 1024, keys ? key_off[i] : value_off[i], rsrc);
+  };
+  auto page_of = [&](int step) { return pages.of(a, steps.slot(min(step, end - 1)) + fetch_from); };
+  int pages_ahead[2] = {0, 0};   // of the step whose values are fetched next, of the one behind it, whose keys are
+  if (begin < end) {
+    const int page0 = page_of(begin), page1 = page_of(begin + 1);
+    pages_ahead[0] = page_of(begin + 2);
+    pages_ahead[1] = page_of(begin + 3);
+    fetch(begin, page0, a.c.k, 0, true);
+    fetch(begin, page0, a.c.v, 3, false);
+    fetch(min(begin + 1, end - 1), page1, a.c.k, 1, true);
+    fetch(min(begin + 1, end - 1), page1, a.c.v, 4, false);
+    fetch(min(begin + 2, end - 1), pages_ahead[0], a.c.k, 2, true);
+    if (lane == 0) missing[wave] = (page0 | page1 | pages_ahead[0] | pages_ahead[1]) < 0;
+  }
+  // here, not at their first use in the loop, where the wait would be for the loads of the next step as well
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(q[kk].x), "+v"(q[kk].y), "+v"(q[kk].z), "+v"(q[kk].w));
 
-  float m = -INFINITY, l = 0.0f;   // m: scaled; l: of the lane's own slots
-  f32x16 acc[CB];
+  float m = -INFINITY, l = 0.0f, exact = 0.0f;   // m: scaled; sums of the lane's own slots, of the weights as they are multiplied and before
+  f32x16 acc[CB], z[2];
+  uint4 w[4];   // probabilities of 16 slots each, as operands
 #pragma unroll
   for (int c = 0; c < CB; ++c) acc[c] = f32x16{};
 
-  // the lane's places in a buffer: keys of row n, by 16 channels; values of slots 4 g + .. by 32 channels
+  // the lane's places in a step's rows: keys of row n, 16 bytes of the first 16 channels; values of slots 4 g + .., 8 bytes of the first 32 channels.
+  // Those of the channels 16 kk or 32 c on differ in bits of their own.
+  const int key_at = n * ROW + 16 * (g ^ key_swizzle<D>(n));
   const int value_row = 4 * g + (lane & 15) / 4;
-  const int value_at = value_row * ROW + 32 * (lane >> 4 & 1) + 8 * (lane & 3);
-  if (begin < end) fetch(begin, 0);
-  for (int step = begin; step < end; ++step) {
-    const int buffer = (step - begin) & 1;
-    // this step's slots have come for all waves, and all have done with the other buffer
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    if (step + 1 < end) fetch(step + 1, buffer ^ 1);
+  const int value_at = value_row * ROW + 32 * (lane >> 4 & 1) + 8 * (lane & 3) + 16 * value_swizzle<D>(value_row);
+  // 32 slots' keys or 32 channels' values as operands; at: the lane's place in the step's buffer
+  auto key_operand = [&](int at, int kk, int i) { return *reinterpret_cast<const uint4*>(smem + (at ^ (32 * kk)) + i * 32 * ROW); };
+  auto value_operand = [&](int at, int kb, int c) {
+    const unsigned char* from = smem + (at ^ (64 * c)) + 16 * kb * ROW;
+    const s16x4 first = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)from);
+    const s16x4 second = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(from + 8 * ROW));
+    const uint2 x = __builtin_bit_cast(uint2, first), y = __builtin_bit_cast(uint2, second);
+    return make_uint4(x.x, x.y, y.x, y.y);
+  };
+  // the products of 64 slots' keys with the rows, slots down
+  auto logits = [&](int buffer) {
+    z[0] = z[1] = f32x16{};
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) z[i] = mfma32<E>(key_operand(key_at + buffer * HALF, kk, i), q[kk], z[i]);
+  };
+  // The logits as weights of the products with the values.  any: some slot has no page.
+  auto weights = [&](int step, bool any) {
     const int t = steps.slot(step);
-    if (!live || t > p_high) continue;
-    const unsigned char* keys = smem + buffer * 2 * HALF;
-    const unsigned char* values = keys + HALF;
-    f32x16 z[2] = {f32x16{}, f32x16{}};
+    if (any || step >= end || t + kTileStep - 1 > p_low || (a.window && t <= p_high - a.window && t + kTileStep - 1 >= a.sinks)) {
+      // of the lane's first slot: how far it is behind the row, its window and the sinks' end, against constants
+      const int behind = step < end ? p - t - 4 * g : -1, outside = a.window ? behind - a.window : -1, sinks = a.sinks - t - 4 * g;
+      int page[4] = {0, 0, 0, 0};
+      if (any) {
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-      const int at = n * ROW + 16 * ((2 * kk + g) ^ key_swizzle<D>(n));
-#pragma unroll
-      for (int i = 0; i < 2; ++i) z[i] = mfma32<E>(*reinterpret_cast<const uint4*>(keys + at + i * 32 * ROW), q[kk], z[i]);
-    }
-    bool masked = t + kTileStep - 1 > p_low || (a.window && t <= p_high - a.window && t + kTileStep - 1 >= a.sinks);
-    int page[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      page[i] = pages.of(a, t + 16 * i);
-      masked = masked || page[i] < 0;
-    }
-    if (masked) {
+        for (int i = 0; i < 4; ++i) page[i] = pages.of(a, t + 16 * i);
+      }
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (page[2 * i + e / 8] < 0 || !sees(a, p, t + 32 * i + 8 * (e / 4) + 4 * g + e % 4)) z[i][e] = -INFINITY;
+        for (int e = 0; e < 16; ++e) {
+          const int c = 32 * i + 8 * (e / 4) + e % 4;
+          z[i][e] = ((page[2 * i + e / 8] >= 0) & (c <= behind) & ((c > outside) | (c < sinks))) ? z[i][e] : -INFINITY;
+        }
     }
-    float top = z[0][0];
+    float tops[4];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 4; ++j) {
+      tops[j] = z[j / 2][8 * (j % 2)];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) top = fmaxf(top, z[i][e]);
-    top *= a.scale;
+      for (int e = 1; e < 8; ++e) tops[j] = fmaxf(tops[j], z[j / 2][8 * (j % 2) + e]);
+    }
+    float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * a.scale;
     // The maximum is raised only when a logit passes it by 2^8; the sums hold that range in fp32, and so do probabilities of 16 bits.
     if (__any(top > m + 8.0f)) {
       top = fmaxf(top, __shfl_xor(top, 32, kWave));
       const float raised = fmaxf(m, top), was = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - raised);
       m = raised;
       l *= was;
+      exact *= was;
 #pragma unroll
       for (int c = 0; c < CB; ++c)
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[c][e] *= was;
     }
     const float ref = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        z[i][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i][e], a.scale, -ref));
-        l += z[i][e];
-      }
+    float add[4] = {};
 #pragma unroll
     for (int kb = 0; kb < 4; ++kb) {
       const int i = kb / 2, e = 8 * (kb % 2);
-      const uint4 w = make_uint4(pair_of<E>(z[i][e], z[i][e + 1]), pair_of<E>(z[i][e + 2], z[i][e + 3]), pair_of<E>(z[i][e + 4], z[i][e + 5]),
-                                 pair_of<E>(z[i][e + 6], z[i][e + 7]));
+      float x[8];
 #pragma unroll
-      for (int c = 0; c < CB; ++c) {
-        const int at = value_at + ((64 * c) ^ (16 * value_swizzle<D>(value_row))) + 16 * kb * ROW;
-        const s16x4 first = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(values + at));
-        const s16x4 second = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(values + at + 8 * ROW));
-        const uint2 x = __builtin_bit_cast(uint2, first), y = __builtin_bit_cast(uint2, second);
-        acc[c] = mfma32<E>(make_uint4(x.x, x.y, y.x, y.y), w, acc[c]);
+      for (int j = 0; j < 8; ++j) {
+        x[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i][e + j], a.scale, -ref));
+        if constexpr (LSE) exact += x[j];
       }
+      // what is added up is what enters the products, so that a row's weights have the sum 1 however they are rounded
+      w[kb] = make_uint4(pair_of<E>(x[0], x[1]), pair_of<E>(x[2], x[3]), pair_of<E>(x[4], x[5]), pair_of<E>(x[6], x[7]));
+      add[0] = add_pair<E>(w[kb].x, add[0]);
+      add[1] = add_pair<E>(w[kb].y, add[1]);
+      add[2] = add_pair<E>(w[kb].z, add[2]);
+      add[3] = add_pair<E>(w[kb].w, add[3]);
     }
+    l += (add[0] + add[1]) + (add[2] + add[3]);
+  };
+  // nothing is moved over these by the compiler
+  auto meet = [&]() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto arrived = [&]() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); };
+
+  if (begin < end) {
+    arrived();
+    meet();
+    int buffer = 0;   // step % 3, counted from the first
+    auto behind = [&](int n) { return buffer + n < 3 ? buffer + n : buffer + n - 3; };
+    // Logits of the next step (where there is none, nobody looks at them), products of this one, and the loads of those behind them among both.  Operands are asked for eight
+    // products ahead: the LDS takes 150 to 200 cycles, a product 32.  A load ahead of all products would keep the wave for 100.
+    auto multiply = [&](int step) {
+      __builtin_amdgcn_s_setprio(1);
+      // past the last step: its rows again, to places that nobody reads
+      const i32x4 k = rows_at(min(step + 3, end - 1), pages_ahead[1], a.c.k), v = rows_at(min(step + 2, end - 1), pages_ahead[0], a.c.v);
+      const uint32_t k_to = lds0 + buffer * HALF, v_to = lds0 + (3 + behind(2)) * HALF;
+      {
+        const int keys = key_at + behind(1) * HALF, values = value_at + (3 + buffer) * HALF;
+        constexpr int P = 2 * KK + 4 * CB, AHEAD = 6;
+        uint4 x[P];
+        auto operand = [&](int i) {
+          return i < 2 * KK ? key_operand(keys, i / 2, i % 2) : value_operand(values, (i - 2 * KK) / CB, (i - 2 * KK) % CB);
+        };
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) x[i] = operand(i);
+        __builtin_amdgcn_sched_group_barrier(kSchedLds, AHEAD, 0);
+        z[0] = z[1] = f32x16{};
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+          if (i < 2 * KK) {
+            z[i % 2] = mfma32<E>(x[i], q[i / 2], z[i % 2]);
+          } else {
+            const int kb = (i - 2 * KK) / CB, c = (i - 2 * KK) % CB;
+            acc[c] = mfma32<E>(x[i], w[kb], acc[c]);
+          }
+          __builtin_amdgcn_sched_group_barrier(kSchedProduct, 1, 0);
+          if (i + AHEAD < P) {
+            x[i + AHEAD] = operand(i + AHEAD);
+            if (i + AHEAD < 2 * KK) __builtin_amdgcn_sched_group_barrier(kSchedLds, 1, 0);
+            else __builtin_amdgcn_sched_group_barrier(kSchedLds, 2, 0);
+          }
+          if (i % (P / 4) == P / 8 && i / (P / 4) < 2 * LOADS) {
+            const int j = i / (P / 4);
+            if (j < LOADS) load_ahead(k_to + j * 1024, key_off[j], k);
+            else load_ahead(v_to + (j - LOADS) * 1024, value_off[j - LOADS], v);
+          }
+        }
+      }
+      __builtin_amdgcn_s_setprio(0);
+    };
+    auto no_page = [&]() { return __any(missing[lane % WAVES]); };
+    logits(0);
+    weights(begin, no_page());
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    meet();
+    // The second half of the waves is a meeting behind the first.
+    if (wave >= WAVES / 2) meet();
+    for (int step = begin; step < end; ++step) {
+      const bool any = no_page();
+      multiply(step);
+      // the loads of the step before have come, those of this step are on their way
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * LOADS) : "memory");
+      meet();
+      pages_ahead[0] = pages_ahead[1];
+      pages_ahead[1] = page_of(step + 4);
+      if (pages_ahead[1] < 0 && lane == 0) missing[wave] = 1;   // three steps before it matters
+      weights(step + 1, any);
+      meet();
+      buffer = behind(1);
+    }
+    if (wave < WAVES / 2) meet();
   }
 
+  arrived();   // loads that nobody reads
   l += __shfl_xor(l, 32, kWave);
+  exact += __shfl_xor(exact, 32, kWave);
   bool whole = true;
 #pragma unroll
   for (int c = 0; c < CB; ++c)
@@ -200,6 +327,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_kvp_tiles_kernel(KvpAttend
     if (g == 0) {
       a.tile_m[part] = m;
       a.tile_l[part] = l;
+      if (LSE) a.tile_exact[part] = exact;
     }
 #pragma unroll
     for (int c = 0; c < CB; ++c)
@@ -210,7 +338,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_kvp_tiles_kernel(KvpAttend
   } else if (valid) {
     const int64_t at = out_row(a, s, h, row);
     const float inverse = l == 0.0f ? 0.0f : 1.0f / l;
-    if (g == 0) store_lse(a, at, m, l);
+    if (LSE && g == 0) store_lse(a, at, m, exact);
 #pragma unroll
     for (int c = 0; c < CB; ++c)
 #pragma unroll
@@ -227,13 +355,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_kvp_tiles_kernel(KvpAttend
       const int r = row0 + 32 * w + __builtin_ctz(left);
       if (r >= R) break;
       float mr, lr, o;
-      careful_row<E, D, kTileStep>(a, s, pages, h, r, steps, begin, end, reinterpret_cast<float*>(smem), &mr, &lr, &o);
+      careful_row<E, D, kTileStep, 64 * WAVES>(a, s, pages, h, r, steps, begin, end, reinterpret_cast<float*>(smem), &mr, &lr, &o);
       if (a.pieces > 1) {
         const size_t to = ((size_t)blockIdx.x * a.pieces + blockIdx.y) * BM + r - row0;
         if (threadIdx.x < D) a.tile_o[to * D + threadIdx.x] = o;
         if (threadIdx.x == 0) {
           a.tile_m[to] = mr;
           a.tile_l[to] = lr;
+          if (LSE) a.tile_exact[to] = lr;
         }
       } else {
         const int64_t at = out_row(a, s, h, r);
@@ -244,52 +373,73 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_kvp_tiles_kernel(KvpAttend
   }
 }
 
-// The pieces of a tile's rows put together, a wave a row.
+// The pieces of a tile's rows put together, a wave a row at a time and a workgroup 16 rows.
 template <class E, int D>
 __global__ __launch_bounds__(256) void kvp_join_tiles_kernel(KvpAttend a) {
-  const int lane = threadIdx.x & 63, BM = a.tile_rows;
-  for (int64_t each = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); each < (int64_t)a.tiles * a.c.H * BM;
-       each += (int64_t)gridDim.x * 4) {   // row of a tile of a head
-    const int block = (int)(each / BM), r0 = (int)(each - (int64_t)block * BM);
+  constexpr int C = D / 64, N = 4;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, BM = a.tile_rows, parts = BM / 16;
+  for (int64_t each = blockIdx.x; each < (int64_t)a.tiles * a.c.H * parts; each += gridDim.x) {
+    const int block = (int)(each / parts), first = (int)(each - (int64_t)block * parts) * 16;
     const int h = block % a.c.H, tile = a.tiles - 1 - block / a.c.H;
     const int b = sentence_of_tile(a, tile, BM);
     const Sentence s = sentence(a, b);
     const int R = s.rows * a.G;
-    const int64_t local = tile - tile_start(a, b, BM);
-    if (R <= a.few || local < 0 || local * BM + r0 >= R) continue;
-    const size_t from = (size_t)block * a.pieces * BM + r0, next = BM;
-    const float m = lane < a.pieces ? a.tile_m[from + lane * next] : -INFINITY, l = lane < a.pieces ? a.tile_l[from + lane * next] : 0.0f;
-    float top = m;
-  #pragma unroll
-    for (int off = 1; off < 64; off <<= 1) top = fmaxf(top, __shfl_xor(top, off, kWave));
-    const float factor = m == -INFINITY ? (l != 0.0f ? NAN : 0.0f) : __builtin_amdgcn_exp2f(m - top);
-    const float total = wave_sum(m == -INFINITY ? l : l * factor);
-    float sum[D / 64] = {};
-    for (int i = 0; i < a.pieces; ++i) {
-      const float f = __shfl(factor, i, kWave);
-      const float* o = a.tile_o + (from + i * next) * D + lane * (D / 64);
-  #pragma unroll
-      for (int c = 0; c < D / 64; ++c) sum[c] += f == 0.0f ? 0.0f : f * o[c];
+    const int64_t row0 = (tile - tile_start(a, b, BM)) * BM;
+    if (R <= a.few || row0 < 0 || row0 + first >= R) continue;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int r0 = first + 4 * k + wave;
+      if (row0 + r0 >= R) break;
+      const size_t from = (size_t)block * a.pieces * BM + r0, next = BM;
+      const float m = lane < a.pieces ? a.tile_m[from + lane * next] : -INFINITY, l = lane < a.pieces ? a.tile_l[from + lane * next] : 0.0f;
+      float top = m, sum[C] = {};
+#pragma unroll
+      for (int off = 1; off < 64; off <<= 1) top = fmaxf(top, __shfl_xor(top, off, kWave));
+      const float factor = m == -INFINITY ? (l != 0.0f ? NAN : 0.0f) : __builtin_amdgcn_exp2f(m - top);
+      const float total = wave_sum(m == -INFINITY ? l : l * factor);
+      float exact = 0.0f;
+      if (a.lse) {
+        exact = lane < a.pieces ? a.tile_exact[from + lane * next] : 0.0f;
+        exact = wave_sum(m == -INFINITY ? exact : exact * factor);
+      }
+      for (int i0 = 0; i0 < a.pieces; i0 += N) {
+        float o[N][C];
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (i0 + i < a.pieces) __builtin_memcpy(o[i], a.tile_o + (from + (i0 + i) * next) * D + lane * C, sizeof(o[i]));
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          if (i0 + i >= a.pieces) continue;
+          const float f = __shfl(factor, i0 + i, kWave);
+#pragma unroll
+          for (int c = 0; c < C; ++c) sum[c] += f == 0.0f ? 0.0f : f * o[i][c];
+        }
+      }
+      const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
+      const int64_t at = out_row(a, s, h, (int)row0 + r0);
+      typename E::T* dst = reinterpret_cast<typename E::T*>(a.out) + at * D + lane * C;
+      if constexpr (C == 2) *reinterpret_cast<uint32_t*>(dst) = pair_of<E>(sum[0] * inverse, sum[1] * inverse);
+      else dst[0] = from_float<E>(sum[0] * inverse);
+      if (lane == 0) store_lse(a, at, top, exact);
     }
-    const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
-    const int64_t at = out_row(a, s, h, (int)local * BM + r0);
-    typename E::T* dst = reinterpret_cast<typename E::T*>(a.out) + at * D + lane * (D / 64);
-  #pragma unroll
-    for (int c = 0; c < D / 64; ++c) dst[c] = from_float<E>(sum[c] * inverse);
-    if (lane == 0) store_lse(a, at, top, total);
   }
 }
 
 template <class E, int D, int WAVES>
 int launch_tiles(const KvpAttend& a, hipStream_t s) {
-  static std::atomic<uint64_t> seen{0};
-  const size_t lds = 4 * kTileStep * 2 * D;
-  const int rc = allow_dynamic_lds(seen, reinterpret_cast<const void*>(&gemm_kvp_tiles_kernel<E, D, WAVES>), lds);
+  const size_t lds = 6 * kTileStep * 2 * D;
+  auto launch = [&](auto kernel, std::atomic<uint64_t>& seen) -> int {
+    const int rc = allow_dynamic_lds(seen, reinterpret_cast<const void*>(kernel), lds);
+    if (rc != CI_OK) return rc;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(a.tiles * a.c.H), (unsigned)a.pieces), dim3(64 * WAVES), lds, s, a);
+    CI_HIP_CHECK_LAUNCH();
+    return CI_OK;
+  };
+  static std::atomic<uint64_t> with{0}, without{0};
+  const int rc = a.lse ? launch(gemm_kvp_tiles_kernel<E, D, WAVES, true>, with) : launch(gemm_kvp_tiles_kernel<E, D, WAVES, false>, without);
   if (rc != CI_OK) return rc;
-  hipLaunchKernelGGL((gemm_kvp_tiles_kernel<E, D, WAVES>), dim3((unsigned)(a.tiles * a.c.H), (unsigned)a.pieces), dim3(64 * WAVES), lds, s, a);
-  CI_HIP_CHECK_LAUNCH();
   if (a.pieces > 1) {
-    hipLaunchKernelGGL((kvp_join_tiles_kernel<E, D>), dim3(join_blocks((int64_t)a.tiles * a.c.H * a.tile_rows)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((kvp_join_tiles_kernel<E, D>), dim3(join_blocks((int64_t)a.tiles * a.c.H * (a.tile_rows / 16))), dim3(256), 0, s, a);
     CI_HIP_CHECK_LAUNCH();
   }
   return CI_OK;

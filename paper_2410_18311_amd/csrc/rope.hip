@@ -70,7 +70,7 @@ __device__ __forceinline__ Place place_of(const RopeCall& a, int t) {
   p.pos = (int)slot;
   if (slot >= 0 && slot < (a.cache.most << a.cache.shift)) {
     const int64_t page = a.cache.table[b * a.cache.most + (slot >> a.cache.shift)];
-    if (page >= 0 && page < a.cache.pages)
+    if ((uint64_t)page < a.cache.pages)
       p.at = ((page * a.cache.H << a.cache.shift) + (slot & ((1 << a.cache.shift) - 1))) * a.D;
   }
   return p;
