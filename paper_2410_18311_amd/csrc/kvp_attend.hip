@@ -16,7 +16,7 @@ struct AttendPlan {
   size_t place, m, l, o, tile_m, tile_l, tile_exact, tile_o, bytes;   // places in the workspace
 };
 
-constexpr int kTileRows = 256;
+constexpr int kTileRows = 128;
 
 // Most steps of `step` slots that the rows of a sentence see something of.
 int64_t most_steps(int64_t step, int64_t rows, int64_t max_len, int64_t window, int64_t sinks) {
@@ -57,7 +57,7 @@ AttendPlan attend_plan(const ci_kvp& c, int64_t T, int64_t G, int64_t max_rows, 
     p.tiles = (int)(T * G / kTileRows + c.B);   // see tile_start
     const int64_t full = std::max<int64_t>(1, T * G / kTileRows) * c.H, steps = most_steps(64, max_rows, max_len, window, sinks);
     // No piece below eight steps.
-    p.pieces = (int)std::max<int64_t>(1, std::min<int64_t>({kCus / full, steps / 8, kMaxPieces}));
+    p.pieces = (int)std::max<int64_t>(1, std::min<int64_t>({2 * kCus / full, steps / 8, kMaxPieces}));
     if (p.pieces > 1) {
       const size_t rows = (size_t)p.tiles * c.H * p.pieces * kTileRows;
       p.tile_m = take(rows);

@@ -5,7 +5,7 @@
 namespace ci {
 template <> int launch_kvp_attend_type<BF16>(const KvpAttend& a, int D, bool rows, bool tiles, hipStream_t s) {
   int rc = CI_OK;
-  if (tiles) rc = D == 64 ? launch_tiles<BF16, 64, 8>(a, s) : launch_tiles<BF16, 128, 8>(a, s);
+  if (tiles) rc = D == 64 ? launch_tiles<BF16, 64, 4>(a, s) : launch_tiles<BF16, 128, 4>(a, s);
   if (rows && rc == CI_OK) rc = D == 64 ? launch_rows<BF16, 64>(a, s) : launch_rows<BF16, 128>(a, s);
   return rc;
 }

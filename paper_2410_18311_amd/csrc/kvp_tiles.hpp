@@ -66,7 +66,7 @@ template <class E, int D, int WAVES, bool LSE>
 __global__ __launch_bounds__(64 * WAVES, 2) void gemm_kvp_tiles_kernel(KvpAttend a) {
   constexpr int BM = 32 * WAVES, ROW = 2 * D, HALF = kTileStep * ROW, KK = D / 16, CB = D / 32;
   constexpr int LOADS = HALF / 1024 / WAVES, ROWS = 1024 / ROW;   // loads of a wave and tensor, rows of a load
-  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];   // three steps' keys and three steps' values, 64 rows each
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];   // two steps' keys and two steps' values, 64 rows each
   __shared__ unsigned broken[WAVES];
   __shared__ int missing[WAVES];   // whether a wave has met slots without a page
   const int lane = threadIdx.x & 63, n = lane & 31, g = lane >> 5;
@@ -130,17 +130,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_kvp_tiles_kernel(KvpAttend
     for (int i = 0; i < LOADS; ++i) load_ahead(lds0 + place * HALF + i * 1024, keys ? key_off[i] : value_off[i], rsrc);
   };
   auto page_of = [&](int step) { return pages.of(a, steps.slot(min(step, end - 1)) + fetch_from); };
-  int pages_ahead[2] = {0, 0};   // of the step whose values are fetched next, of the one behind it, whose keys are
+  int page1 = 0, page2 = 0;   // of the step whose values are fetched next, of the one behind it, whose keys are
   if (begin < end) {
-    const int page0 = page_of(begin), page1 = page_of(begin + 1);
-    pages_ahead[0] = page_of(begin + 2);
-    pages_ahead[1] = page_of(begin + 3);
+    const int page0 = page_of(begin);
+    page1 = page_of(begin + 1);
+    page2 = page_of(begin + 2);
     fetch(begin, page0, a.c.k, 0, true);
-    fetch(begin, page0, a.c.v, 3, false);
+    fetch(begin, page0, a.c.v, 2, false);
     fetch(min(begin + 1, end - 1), page1, a.c.k, 1, true);
-    fetch(min(begin + 1, end - 1), page1, a.c.v, 4, false);
-    fetch(min(begin + 2, end - 1), pages_ahead[0], a.c.k, 2, true);
-    if (lane == 0) missing[wave] = (page0 | page1 | pages_ahead[0] | pages_ahead[1]) < 0;
+    if (lane == 0) missing[wave] = (page0 | page1 | page2) < 0;
   }
   // here, not at their first use in the loop, where the wait would be for the loads of the next step as well
 #pragma unroll
@@ -175,7 +173,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_kvp_tiles_kernel(KvpAttend
       for (int i = 0; i < 2; ++i) z[i] = mfma32<E>(key_operand(key_at + buffer * HALF, kk, i), q[kk], z[i]);
   };
   // The logits as weights of the products with the values.  any: some slot has no page.
-  auto weights = [&](int step, bool any) {
+  // load(i), i = 0 .. 3: what else is to be done on the way.
+  auto weights = [&](int step, bool any, auto load) {
     const int t = steps.slot(step);
     if (any || step >= end || t + kTileStep - 1 > p_low || (a.window && t <= p_high - a.window && t + kTileStep - 1 >= a.sinks)) {
       // of the lane's first slot: how far it is behind the row, its window and the sinks' end, against constants
@@ -230,6 +229,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_kvp_tiles_kernel(KvpAttend
       add[1] = add_pair<E>(w[kb].y, add[1]);
       add[2] = add_pair<E>(w[kb].z, add[2]);
       add[3] = add_pair<E>(w[kb].w, add[3]);
+      load(kb);
     }
     l += (add[0] + add[1]) + (add[2] + add[3]);
   };
@@ -246,70 +246,59 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_kvp_tiles_kernel(KvpAttend
   if (begin < end) {
     arrived();
     meet();
-    int buffer = 0;   // step % 3, counted from the first
-    auto behind = [&](int n) { return buffer + n < 3 ? buffer + n : buffer + n - 3; };
-    // Logits of the next step (where there is none, nobody looks at them), products of this one, and the loads of those behind them among both.  Operands are asked for eight
-    // products ahead: the LDS takes 150 to 200 cycles, a product 32.  A load ahead of all products would keep the wave for 100.
-    auto multiply = [&](int step) {
+    int buffer = 0;   // of this step
+    auto no_page = [&]() { return __any(missing[lane % WAVES]); };
+    logits(0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    meet();
+    for (int step = begin; step < end; ++step) {
+      // The next step's values and the keys of the one behind it (past the last step: its rows again, to places that nobody reads) go to
+      // where this step's keys and the values of the one before were.
+      const i32x4 k = rows_at(min(step + 2, end - 1), page2, a.c.k), v = rows_at(min(step + 1, end - 1), page1, a.c.v);
+      const uint32_t k_to = lds0 + buffer * HALF, v_to = lds0 + (2 + (buffer ^ 1)) * HALF;
+      weights(step, no_page(), [&](int i) {
+#pragma unroll
+        for (int j = i * LOADS / 4; j < (i + 1) * LOADS / 4; ++j) {
+          load_ahead(k_to + j * 1024, key_off[j], k);
+          load_ahead(v_to + j * 1024, value_off[j], v);
+        }
+      });
+      page1 = page2;
+      page2 = page_of(step + 3);
+      if (page2 < 0 && lane == 0) missing[wave] = 1;   // two steps before it matters
+      // Logits of the next step (where there is none, nobody looks at them) and products of this one.  Operands are asked for eight
+      // products ahead: the LDS takes 150 to 200 cycles, a product 32.
       __builtin_amdgcn_s_setprio(1);
-      // past the last step: its rows again, to places that nobody reads
-      const i32x4 k = rows_at(min(step + 3, end - 1), pages_ahead[1], a.c.k), v = rows_at(min(step + 2, end - 1), pages_ahead[0], a.c.v);
-      const uint32_t k_to = lds0 + buffer * HALF, v_to = lds0 + (3 + behind(2)) * HALF;
-      {
-        const int keys = key_at + behind(1) * HALF, values = value_at + (3 + buffer) * HALF;
-        constexpr int P = 2 * KK + 4 * CB, AHEAD = 6;
-        uint4 x[P];
-        auto operand = [&](int i) {
-          return i < 2 * KK ? key_operand(keys, i / 2, i % 2) : value_operand(values, (i - 2 * KK) / CB, (i - 2 * KK) % CB);
-        };
+      const int keys = key_at + (buffer ^ 1) * HALF, values = value_at + (2 + buffer) * HALF;
+      constexpr int P = 2 * KK + 4 * CB, AHEAD = 8;
+      uint4 x[P];
+      auto operand = [&](int i) {
+        return i < 2 * KK ? key_operand(keys, i / 2, i % 2) : value_operand(values, (i - 2 * KK) / CB, (i - 2 * KK) % CB);
+      };
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) x[i] = operand(i);
-        __builtin_amdgcn_sched_group_barrier(kSchedLds, AHEAD, 0);
-        z[0] = z[1] = f32x16{};
+      for (int i = 0; i < AHEAD; ++i) x[i] = operand(i);
+      __builtin_amdgcn_sched_group_barrier(kSchedLds, AHEAD, 0);
+      z[0] = z[1] = f32x16{};
 #pragma unroll
-        for (int i = 0; i < P; ++i) {
-          if (i < 2 * KK) {
-            z[i % 2] = mfma32<E>(x[i], q[i / 2], z[i % 2]);
-          } else {
-            const int kb = (i - 2 * KK) / CB, c = (i - 2 * KK) % CB;
-            acc[c] = mfma32<E>(x[i], w[kb], acc[c]);
-          }
-          __builtin_amdgcn_sched_group_barrier(kSchedProduct, 1, 0);
-          if (i + AHEAD < P) {
-            x[i + AHEAD] = operand(i + AHEAD);
-            if (i + AHEAD < 2 * KK) __builtin_amdgcn_sched_group_barrier(kSchedLds, 1, 0);
-            else __builtin_amdgcn_sched_group_barrier(kSchedLds, 2, 0);
-          }
-          if (i % (P / 4) == P / 8 && i / (P / 4) < 2 * LOADS) {
-            const int j = i / (P / 4);
-            if (j < LOADS) load_ahead(k_to + j * 1024, key_off[j], k);
-            else load_ahead(v_to + (j - LOADS) * 1024, value_off[j - LOADS], v);
-          }
+      for (int i = 0; i < P; ++i) {
+        if (i < 2 * KK) {
+          z[i % 2] = mfma32<E>(x[i], q[i / 2], z[i % 2]);
+        } else {
+          const int kb = (i - 2 * KK) / CB, c = (i - 2 * KK) % CB;
+          acc[c] = mfma32<E>(x[i], w[kb], acc[c]);
+        }
+        __builtin_amdgcn_sched_group_barrier(kSchedProduct, 1, 0);
+        if (i + AHEAD < P) {
+          x[i + AHEAD] = operand(i + AHEAD);
+          if (i + AHEAD < 2 * KK) __builtin_amdgcn_sched_group_barrier(kSchedLds, 1, 0);
+          else __builtin_amdgcn_sched_group_barrier(kSchedLds, 2, 0);
         }
       }
       __builtin_amdgcn_s_setprio(0);
-    };
-    auto no_page = [&]() { return __any(missing[lane % WAVES]); };
-    logits(0);
-    weights(begin, no_page());
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    meet();
-    // The second half of the waves is a meeting behind the first.
-    if (wave >= WAVES / 2) meet();
-    for (int step = begin; step < end; ++step) {
-      const bool any = no_page();
-      multiply(step);
-      // the loads of the step before have come, those of this step are on their way
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * LOADS) : "memory");
+      arrived();
       meet();
-      pages_ahead[0] = pages_ahead[1];
-      pages_ahead[1] = page_of(step + 4);
-      if (pages_ahead[1] < 0 && lane == 0) missing[wave] = 1;   // three steps before it matters
-      weights(step + 1, any);
-      meet();
-      buffer = behind(1);
+      buffer ^= 1;
     }
-    if (wave < WAVES / 2) meet();
   }
 
   arrived();   // loads that nobody reads
@@ -427,7 +416,7 @@ __global__ __launch_bounds__(256) void kvp_join_tiles_kernel(KvpAttend a) {
 
 template <class E, int D, int WAVES>
 int launch_tiles(const KvpAttend& a, hipStream_t s) {
-  const size_t lds = 6 * kTileStep * 2 * D;
+  const size_t lds = 4 * kTileStep * 2 * D;
   auto launch = [&](auto kernel, std::atomic<uint64_t>& seen) -> int {
     const int rc = allow_dynamic_lds(seen, reinterpret_cast<const void*>(kernel), lds);
     if (rc != CI_OK) return rc;

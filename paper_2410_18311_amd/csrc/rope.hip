@@ -3,7 +3,7 @@
 //
 // Both are bound by their bytes, or by the latency of one launch.  A lane holds two vectors of 16 bytes of a head, the two halves of its pairs
 // (neighbouring pairs: two vectors of whole pairs), so a head is D / 2 elements' lanes and its norm a sum over them.  The sines and cosines are a token's,
-// not a head's: a workgroup takes one to four tokens, computes each pair's once (one pair a thread) and hands them round through the LDS.
+// not a head's: a workgroup takes one or two tokens, computes each pair's once (one pair a thread) and hands them round through the LDS.
 //
 // Angles are whole 2^-64ths of a turn, so position times frequency is one 64-bit product whose overflow is whole turns: exact at any position.
 // Its nearest quarter turn is taken off as bits; what is left, at most an eighth of a turn, goes through the Taylor series, whose
@@ -117,13 +117,33 @@ template <class E, bool APPEND, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void rope_kernel(RopeCall a) {
   constexpr int V = E::VEC;
   extern __shared__ __attribute__((aligned(16))) float turned[];   // [tokens][cos, sin][rot / 2]
-  __shared__ Place places[4];
+  __shared__ Place places[2];
   const int t0 = blockIdx.x * a.tokens, pairs = a.rot / 2;
+  const int groups = 256 / a.lanes, lane = threadIdx.x & (a.lanes - 1), group = threadIdx.x / a.lanes;
+  const int token = group & (a.tokens - 1), t = t0 + token, turning = a.rot / (2 * V);   // lanes that turn pairs
+  const int from = blockIdx.y * a.per_group, to = min(a.heads, from + a.per_group), stride = groups / a.tokens;
+  const bool live = t < a.T && 2 * V * lane < a.D;
+  // channels of the two vectors
+  const int first = lane < turning ? lane * V : a.rot + (lane - turning) * V;
+  const int second = first + (lane < turning ? a.rot : a.D - a.rot) / 2;
+  // A head's vectors are requested while the one before is worked on, the first before the angles are known.
+  auto load = [&](int h, uint4* u, uint4* w) {
+    if (!live || h >= to) return;
+    int head = h;
+    const Heads& k = a.kind[APPEND ? kind_of(a, &head) : 0];
+    const typename E::T* x = source<E>(a, k, t, head);
+    *u = ld16(x + first);
+    *w = ld16(x + second);
+  };
+  int h = from + group / a.tokens;
+  uint4 u = make_uint4(0, 0, 0, 0), w = u, next_u = u, next_w = u;
+  load(h, &u, &w);
+
   if constexpr (APPEND) {
     const int wave = threadIdx.x >> 6;
-    if (wave < a.tokens && t0 + wave < a.T) {
-      const Place p = place_of(a, t0 + wave);
-      if ((threadIdx.x & 63) == 0) places[wave] = p;
+    for (int i = wave; i < a.tokens && t0 + i < a.T; i += 4) {
+      const Place p = place_of(a, t0 + i);
+      if ((threadIdx.x & 63) == 0) places[i] = p;
     }
     __syncthreads();
   }
@@ -137,27 +157,15 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeCall a) {
   }
   __syncthreads();
 
-  const int groups = 256 / a.lanes, lane = threadIdx.x & (a.lanes - 1), group = threadIdx.x / a.lanes;
-  const int token = group & (a.tokens - 1), t = t0 + token, turning = a.rot / (2 * V);   // lanes that turn pairs
-  const int from = blockIdx.y * a.per_group, to = min(a.heads, from + a.per_group);
-  const bool live = t < a.T && 2 * V * lane < a.D;
-  // channels of the two vectors
-  const int first = lane < turning ? lane * V : a.rot + (lane - turning) * V;
-  const int second = first + (lane < turning ? a.rot : a.D - a.rot) / 2;
   Place p{-1, 0, 0};
   if (APPEND && live) p = places[token];
   const float* cs = turned + 2 * token * pairs;
-  for (int h = from + group / a.tokens; h - group / a.tokens < to; h += groups / a.tokens) {
+  for (; h - group / a.tokens < to; h += stride) {
     int head = h;
     const int which = APPEND ? kind_of(a, &head) : 0;
     const Heads& k = a.kind[which];
     const bool here = live && h < to;
-    uint4 u = make_uint4(0, 0, 0, 0), w = u;
-    if (here) {
-      const typename E::T* x = source<E>(a, k, t, head);
-      u = ld16(x + first);
-      w = ld16(x + second);
-    }
+    load(h + stride, &next_u, &next_w);
     if (k.turned || k.norm) {
       float xa[V], xb[V];
       unpack<E>(u, xa);
@@ -209,6 +217,8 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeCall a) {
         *reinterpret_cast<uint4*>(y + second) = w;
       }
     }
+    u = next_u;
+    w = next_w;
   }
 }
 
@@ -288,9 +298,12 @@ int launch_type(RopeCall& a, int style, hipStream_t s) {
   a.lanes = 1;
   while (a.lanes * 2 * V < a.D) a.lanes *= 2;
   const int groups = 256 / a.lanes;
-  a.tokens = a.T >= 1024 ? 4 : 1;
+  // Few tokens: one a workgroup, and as many heads as it has lanes for.  Many: two, and up to eight rounds of heads, so that the angles and the
+  // first loads' time are shared: 3584 tokens of 96 heads to pages 39.5 us; one round 46, four tokens 48 to 52.
+  a.tokens = a.T >= 1024 && groups >= 2 ? 2 : 1;
   const int once = groups / a.tokens;   // heads of a workgroup and token at a time
-  a.per_group = a.tokens == 4 ? (a.heads + once - 1) / once * once : once;
+  const int rounds = a.T >= 1024 ? std::min(8, (a.heads + once - 1) / once) : 1;
+  a.per_group = rounds * once;
   const dim3 grid((unsigned)((a.T + a.tokens - 1) / a.tokens), (unsigned)((a.heads + a.per_group - 1) / a.per_group));
   const size_t lds = (size_t)a.tokens * a.rot * sizeof(float);
   if (style == CI_ROPE_INTERLEAVED)
