@@ -39,9 +39,10 @@ AttendPlan attend_plan(const ci_kvp& c, int64_t T, int64_t G, int64_t max_rows, 
   };
   if (p.rows) {
     const int64_t tiles = (std::min<int64_t>(R, p.few) + 15) / 16, steps = most_steps(32, max_rows, max_len, window, sinks);
-    // Three workgroups a compute unit, what the registers leave room for; no piece below two steps a wave.
-    const int64_t wanted = 3 * kCus;
-    p.least = 8;
+    // Four workgroups a compute unit, of which two are at work at once and the others balance them (eight sentences to 65536 slots 178 us;
+    // two 202, three 190, six 182); no piece below three steps a wave (4096 slots of 40 heads 20.5 us, two 22.7).
+    const int64_t wanted = 4 * kCus;
+    p.least = 12;
     p.wanted = heads * tiles * 2 > wanted || steps <= p.least ? 0 : (int)(wanted / tiles);
     p.blocks = (int)heads + p.wanted;
     p.row_tiles = (int)std::min<int64_t>(tiles, 65535);   // beyond, a workgroup takes several
@@ -55,9 +56,9 @@ AttendPlan attend_plan(const ci_kvp& c, int64_t T, int64_t G, int64_t max_rows, 
   }
   if (p.in_tiles) {
     p.tiles = (int)(T * G / kTileRows + c.B);   // see tile_start
-    const int64_t full = std::max<int64_t>(1, T * G / kTileRows) * c.H, steps = most_steps(64, max_rows, max_len, window, sinks);
-    // No piece below eight steps.
-    p.pieces = (int)std::max<int64_t>(1, std::min<int64_t>({2 * kCus / full, steps / 8, kMaxPieces}));
+    const int64_t full = (T * G + kTileRows - 1) / kTileRows * c.H, steps = most_steps(64, max_rows, max_len, window, sinks);
+    // As many workgroups as fit at once (three a compute unit of 64 channels, two of 128); no piece below eight steps.
+    p.pieces = (int)std::max<int64_t>(1, std::min<int64_t>({(c.D == 64 ? 3 : 2) * kCus / full, steps / 8, kMaxPieces}));
     if (p.pieces > 1) {
       const size_t rows = (size_t)p.tiles * c.H * p.pieces * kTileRows;
       p.tile_m = take(rows);

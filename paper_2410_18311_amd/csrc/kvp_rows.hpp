@@ -117,7 +117,7 @@ __device__ __forceinline__ void load_query(const KvpAttend& a, const Sentence& s
 }
 
 template <class E, int D>
-__global__ __launch_bounds__(256, E::BYTES == 4 ? 2 : 3) void gemm_kvp_rows_kernel(KvpAttend a) {
+__global__ __launch_bounds__(256, 2) void gemm_kvp_rows_kernel(KvpAttend a) {
   using S32 = Step32<E, D>;
   constexpr int K = S32::K, CH = S32::CH, VW = S32::V;
   __shared__ float ml[2][4][16];
@@ -150,32 +150,32 @@ __global__ __launch_bounds__(256, E::BYTES == 4 ? 2 : 3) void gemm_kvp_rows_kern
     S32 x;
     auto find_pages = [&](int step) {
       const int t = steps.slot(min(step, end - 1));
-  #pragma unroll
+#pragma unroll
       for (int i = 0; i < 2; ++i) x.page[i] = pages.of(a, t + 16 * i);
     };
     auto load_keys = [&](int step, const int (&page)[2]) {
       const int t = steps.slot(step);
-  #pragma unroll
+#pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int slot = min(t + 16 * i + n, pages.last) & inside;
         const typename E::T* src = reinterpret_cast<const typename E::T*>(a.c.k) + page_start<D>(a, page[i], h) + slot * D + g * E::VEC;
-  #pragma unroll
+#pragma unroll
         for (int j = 0; j < K; ++j) x.k[i][j] = ld16(src + 4 * j * E::VEC);
       }
     };
     auto load_values = [&](int step, const int (&page)[2]) {
       const int t = steps.slot(step);
-  #pragma unroll
+#pragma unroll
       for (int i = 0; i < 2; ++i) {
         const typename E::T* src = reinterpret_cast<const typename E::T*>(a.c.v) + page_start<D>(a, page[i], h) + n * CH;
-  #pragma unroll
+#pragma unroll
         for (int r = 0; r < 4; ++r) ld_words<VW>(src + (min(t + 16 * i + 4 * g + r, pages.last) & inside) * D, x.v[4 * i + r]);
       }
     };
 
     float m = -INFINITY, l = 0.0f;   // l: of the lane's own slots
     f32x4 acc[CH];
-  #pragma unroll
+#pragma unroll
     for (int c = 0; c < CH; ++c) acc[c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
     int step = begin + wave;
@@ -190,9 +190,9 @@ __global__ __launch_bounds__(256, E::BYTES == 4 ? 2 : 3) void gemm_kvp_rows_kern
         const int next[2] = {x.page[0], x.page[1]};
         const bool more = step + 4 < end;
         f32x4 z[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
-  #pragma unroll
+#pragma unroll
         for (int j = 0; j < K; ++j)
-  #pragma unroll
+#pragma unroll
           for (int i = 0; i < 2; ++i) {
             if constexpr (E::BYTES == 2) {
               z[i] = product16<E>(x.k[i][j], q[j], z[i]);
@@ -200,15 +200,15 @@ __global__ __launch_bounds__(256, E::BYTES == 4 ? 2 : 3) void gemm_kvp_rows_kern
               float kf[4], qf[4];
               unpack<F32>(x.k[i][j], kf);
               unpack<F32>(q[j], qf);
-  #pragma unroll
+#pragma unroll
               for (int c = 0; c < 4; ++c) z[i] = product16_f32(kf[c], qf[c], z[i]);
             }
           }
         if (more) load_keys(step + 4, next);
         const bool masked = page[0] < 0 || page[1] < 0 || t + 31 > p_low || (a.window && t <= p_high - a.window && t + 31 >= a.sinks);
-  #pragma unroll
+#pragma unroll
         for (int i = 0; i < 2; ++i)
-  #pragma unroll
+#pragma unroll
           for (int r = 0; r < 4; ++r) {
             z[i][r] *= a.scale;
             if (masked) z[i][r] = ((page[i] >= 0) & sees(a, p, t + 16 * i + 4 * g + r)) ? z[i][r] : -INFINITY;
@@ -221,13 +221,13 @@ __global__ __launch_bounds__(256, E::BYTES == 4 ? 2 : 3) void gemm_kvp_rows_kern
           const float raised = fmaxf(m, top), was = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - raised);
           m = raised;
           l *= was;
-  #pragma unroll
+#pragma unroll
           for (int c = 0; c < CH; ++c) acc[c] *= was;
         }
         const float ref = m == -INFINITY ? 0.0f : m;
-  #pragma unroll
+#pragma unroll
         for (int i = 0; i < 2; ++i)
-  #pragma unroll
+#pragma unroll
           for (int r = 0; r < 4; ++r) {
             z[i][r] = __builtin_amdgcn_exp2f(z[i][r] - ref);
             l += z[i][r];
@@ -238,7 +238,7 @@ __global__ __launch_bounds__(256, E::BYTES == 4 ? 2 : 3) void gemm_kvp_rows_kern
           two_pieces<E>(z[0][2], z[0][3], &high.y, &low.y);
           two_pieces<E>(z[1][0], z[1][1], &high.z, &low.z);
           two_pieces<E>(z[1][2], z[1][3], &high.w, &low.w);
-  #pragma unroll
+#pragma unroll
           for (int c = 0; c < CH; ++c) {
             const uint32_t half = c % 2 ? 0x07060302u : 0x05040100u;
             const uint4 e = make_uint4(__builtin_amdgcn_perm(x.v[1][c / 2], x.v[0][c / 2], half), __builtin_amdgcn_perm(x.v[3][c / 2], x.v[2][c / 2], half),
@@ -247,9 +247,9 @@ __global__ __launch_bounds__(256, E::BYTES == 4 ? 2 : 3) void gemm_kvp_rows_kern
             acc[c] = product16<E>(e, low, acc[c]);
           }
         } else {
-  #pragma unroll
+#pragma unroll
           for (int c = 0; c < CH; ++c)
-  #pragma unroll
+#pragma unroll
             for (int i = 0; i < 8; ++i) acc[c] = product16_f32(u2f(x.v[i][c]), z[i / 4][i % 4], acc[c]);
         }
         if (more) {
@@ -270,13 +270,13 @@ __global__ __launch_bounds__(256, E::BYTES == 4 ? 2 : 3) void gemm_kvp_rows_kern
     }
     __syncthreads();
     float top = ml[0][0][n];
-  #pragma unroll
+#pragma unroll
     for (int w = 1; w < 4; ++w) top = fmaxf(top, ml[0][w][n]);
     const float own = m == -INFINITY ? (l != 0.0f ? NAN : 0.0f) : __builtin_amdgcn_exp2f(m - top);
     if (row0 + n < R) {
-  #pragma unroll
+#pragma unroll
       for (int r = 0; r < 4; ++r)
-  #pragma unroll
+#pragma unroll
         for (int c = 0; c < CH; c += 4)
           *reinterpret_cast<float4*>(&sums[wave][n][CH * (4 * g + r) + c]) =
               make_float4(acc[c][r] * own, acc[c + 1][r] * own, acc[c + 2][r] * own, acc[c + 3][r] * own);
@@ -288,12 +288,12 @@ __global__ __launch_bounds__(256, E::BYTES == 4 ? 2 : 3) void gemm_kvp_rows_kern
     for (int e = threadIdx.x; e < live * (D / 4); e += 256) {
       const int r = e / (D / 4), d = e % (D / 4) * 4;
       float t = -INFINITY, total = 0.0f, v[4];
-  #pragma unroll
+#pragma unroll
       for (int w = 0; w < 4; ++w) t = fmaxf(t, ml[0][w][r]);
-  #pragma unroll
+#pragma unroll
       for (int w = 0; w < 4; ++w)
         total += ml[0][w][r] == -INFINITY ? ml[1][w][r] : ml[1][w][r] * __builtin_amdgcn_exp2f(ml[0][w][r] - t);
-  #pragma unroll
+#pragma unroll
       for (int i = 0; i < 4; ++i) v[i] = (sums[0][r][d + i] + sums[1][r][d + i]) + (sums[2][r][d + i] + sums[3][r][d + i]);
       if (!(finite(v[0]) && finite(v[1]) && finite(v[2]) && finite(v[3]))) atomicOr(&broken, 1u << r);
       if (a.wanted) {
@@ -304,7 +304,7 @@ __global__ __launch_bounds__(256, E::BYTES == 4 ? 2 : 3) void gemm_kvp_rows_kern
         }
       } else {
         const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
-  #pragma unroll
+#pragma unroll
         for (int i = 0; i < 4; ++i) v[i] *= inverse;
         const int64_t at = out_row(a, s, h, row0 + r);
         store_row4<E>(a, D, at, d, v);

@@ -311,30 +311,53 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_kvp_tiles_kernel(KvpAttend
     for (int e = 0; e < 16; ++e) whole = whole && finite(acc[c][e]);
   const uint64_t bad = __ballot(!whole);
   const bool valid = live && mine0 + n < R;
-  const size_t part = ((size_t)blockIdx.x * a.pieces + blockIdx.y) * BM + 32 * wave + n;
-  if (valid && a.pieces > 1) {
-    if (g == 0) {
-      a.tile_m[part] = m;
-      a.tile_l[part] = l;
-      if (LSE) a.tile_exact[part] = exact;
+  const size_t part = ((size_t)blockIdx.x * a.pieces + blockIdx.y) * BM + 32 * wave;
+  if (valid && g == 0) {
+    if (a.pieces > 1) {
+      a.tile_m[part + n] = m;
+      a.tile_l[part + n] = l;
+      if (LSE) a.tile_exact[part + n] = exact;
+    } else if (LSE) {
+      store_lse(a, out_row(a, s, h, row), m, exact);
     }
+  }
+  // Through the wave's part of the LDS, so that 16 neighbouring bytes of a row go to a lane and whole rows to neighbouring lanes: 32 channels at a
+  // time, in fp32 where the sums are to be joined.
+  meet();
+  constexpr int PITCH = 32 * 4 + 16;   // of a row; 32 rows of four waves are below the buffers' size
+  unsigned char* mine = smem + wave * 32 * PITCH;
+  const float inverse = a.pieces > 1 ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
+  if (a.pieces > 1) {
 #pragma unroll
-    for (int c = 0; c < CB; ++c)
+    for (int c = 0; c < CB; ++c) {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        *reinterpret_cast<float4*>(a.tile_o + part * D + 32 * c + 8 * j + 4 * g) =
-            make_float4(acc[c][4 * j], acc[c][4 * j + 1], acc[c][4 * j + 2], acc[c][4 * j + 3]);
-  } else if (valid) {
-    const int64_t at = out_row(a, s, h, row);
-    const float inverse = l == 0.0f ? 0.0f : 1.0f / l;
-    if (LSE && g == 0) store_lse(a, at, m, exact);
+        *reinterpret_cast<float4*>(mine + n * PITCH + 16 * (2 * j + g)) = make_float4(acc[c][4 * j], acc[c][4 * j + 1], acc[c][4 * j + 2], acc[c][4 * j + 3]);
 #pragma unroll
-    for (int c = 0; c < CB; ++c)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float v[4] = {acc[c][4 * j] * inverse, acc[c][4 * j + 1] * inverse, acc[c][4 * j + 2] * inverse, acc[c][4 * j + 3] * inverse};
-        store_row4<E>(a, D, at, 32 * c + 8 * j + 4 * g, v);
+      for (int i = 0; i < 4; ++i) {
+        const int r = 8 * i + lane / 8;
+        const float4 v = *reinterpret_cast<const float4*>(mine + r * PITCH + 16 * (lane % 8));
+        if (mine0 + r < R) *reinterpret_cast<float4*>(a.tile_o + (part + r) * D + 32 * c + 4 * (lane % 8)) = v;
       }
+    }
+  } else {
+#pragma unroll
+    for (int c = 0; c < CB; c += 2) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          *reinterpret_cast<uint2*>(mine + n * PITCH + 64 * k + 8 * (2 * j + g)) =
+              make_uint2(pair_of<E>(acc[c + k][4 * j] * inverse, acc[c + k][4 * j + 1] * inverse),
+                         pair_of<E>(acc[c + k][4 * j + 2] * inverse, acc[c + k][4 * j + 3] * inverse));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = 8 * i + lane / 8;
+        const uint4 v = *reinterpret_cast<const uint4*>(mine + r * PITCH + 16 * (lane % 8));
+        if (mine0 + r < R)
+          *reinterpret_cast<uint4*>(reinterpret_cast<typename E::T*>(a.out) + out_row(a, s, h, mine0 + r) * D + 32 * c + 8 * (lane % 8)) = v;
+      }
+    }
   }
   if (lane == 0) broken[wave] = (unsigned)bad | (unsigned)(bad >> 32);
   __syncthreads();
@@ -362,55 +385,61 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_kvp_tiles_kernel(KvpAttend
   }
 }
 
-// The pieces of a tile's rows put together, a wave a row at a time and a workgroup 16 rows.
+// The pieces of a tile's rows put together, eight channels of a row a thread, all pieces' requests at once, eight at a time.
 template <class E, int D>
 __global__ __launch_bounds__(256) void kvp_join_tiles_kernel(KvpAttend a) {
-  constexpr int C = D / 64, N = 4;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, BM = a.tile_rows, parts = BM / 16;
+  constexpr int LANES = D / 8, ROWS = 256 / LANES, N = 8;   // lanes of a row, rows of a workgroup
+  const int BM = a.tile_rows, parts = BM / ROWS, lane = threadIdx.x % LANES;
   for (int64_t each = blockIdx.x; each < (int64_t)a.tiles * a.c.H * parts; each += gridDim.x) {
-    const int block = (int)(each / parts), first = (int)(each - (int64_t)block * parts) * 16;
+    const int block = (int)(each / parts), r0 = (int)(each - (int64_t)block * parts) * ROWS + threadIdx.x / LANES;
     const int h = block % a.c.H, tile = a.tiles - 1 - block / a.c.H;
     const int b = sentence_of_tile(a, tile, BM);
     const Sentence s = sentence(a, b);
     const int R = s.rows * a.G;
-    const int64_t row0 = (tile - tile_start(a, b, BM)) * BM;
-    if (R <= a.few || row0 < 0 || row0 + first >= R) continue;
+    const int64_t row = (tile - tile_start(a, b, BM)) * BM + r0;
+    if (R <= a.few || row < r0 || row >= R) continue;
+    const size_t from = (size_t)block * a.pieces * BM + r0;
+    float top = -INFINITY, total = 0.0f, exact = 0.0f, sum[8] = {};
+    for (int i0 = 0; i0 < a.pieces; i0 += N) {
+      float m[N], l[N], x[N];
+      float4 o[N][2];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int r0 = first + 4 * k + wave;
-      if (row0 + r0 >= R) break;
-      const size_t from = (size_t)block * a.pieces * BM + r0, next = BM;
-      const float m = lane < a.pieces ? a.tile_m[from + lane * next] : -INFINITY, l = lane < a.pieces ? a.tile_l[from + lane * next] : 0.0f;
-      float top = m, sum[C] = {};
-#pragma unroll
-      for (int off = 1; off < 64; off <<= 1) top = fmaxf(top, __shfl_xor(top, off, kWave));
-      const float factor = m == -INFINITY ? (l != 0.0f ? NAN : 0.0f) : __builtin_amdgcn_exp2f(m - top);
-      const float total = wave_sum(m == -INFINITY ? l : l * factor);
-      float exact = 0.0f;
-      if (a.lse) {
-        exact = lane < a.pieces ? a.tile_exact[from + lane * next] : 0.0f;
-        exact = wave_sum(m == -INFINITY ? exact : exact * factor);
+      for (int i = 0; i < N; ++i) {
+        const size_t at = from + (size_t)min(i0 + i, a.pieces - 1) * BM;
+        m[i] = i0 + i < a.pieces ? a.tile_m[at] : -INFINITY;
+        l[i] = i0 + i < a.pieces ? a.tile_l[at] : 0.0f;
+        x[i] = a.lse ? a.tile_exact[at] : 0.0f;
+        const float4* src = reinterpret_cast<const float4*>(a.tile_o + at * D + 8 * lane);
+        o[i][0] = src[0];
+        o[i][1] = src[1];
       }
-      for (int i0 = 0; i0 < a.pieces; i0 += N) {
-        float o[N][C];
+      float next = top;
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-          if (i0 + i < a.pieces) __builtin_memcpy(o[i], a.tile_o + (from + (i0 + i) * next) * D + lane * C, sizeof(o[i]));
+      for (int i = 0; i < N; ++i) next = fmaxf(next, m[i]);
+      const float was = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top - next);
+      top = next;
+      if (total != 0.0f) total *= was;   // a NaN that came without a maximum stays
+      exact *= was;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          if (i0 + i >= a.pieces) continue;
-          const float f = __shfl(factor, i0 + i, kWave);
+      for (int c = 0; c < 8; ++c) sum[c] = was == 0.0f ? (total != total ? NAN : 0.0f) : sum[c] * was;
 #pragma unroll
-          for (int c = 0; c < C; ++c) sum[c] += f == 0.0f ? 0.0f : f * o[i][c];
-        }
+      for (int i = 0; i < N; ++i) {
+        // a piece without a maximum saw nothing, or nothing but NaN
+        const float f = m[i] == -INFINITY ? (l[i] != 0.0f ? NAN : 0.0f) : __builtin_amdgcn_exp2f(m[i] - top);
+        if (f == 0.0f) continue;
+        total = __builtin_fmaf(l[i], f, total);
+        exact = __builtin_fmaf(x[i], f, exact);
+        const float v[8] = {o[i][0].x, o[i][0].y, o[i][0].z, o[i][0].w, o[i][1].x, o[i][1].y, o[i][1].z, o[i][1].w};
+#pragma unroll
+        for (int c = 0; c < 8; ++c) sum[c] = __builtin_fmaf(v[c], f, sum[c]);
       }
-      const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
-      const int64_t at = out_row(a, s, h, (int)row0 + r0);
-      typename E::T* dst = reinterpret_cast<typename E::T*>(a.out) + at * D + lane * C;
-      if constexpr (C == 2) *reinterpret_cast<uint32_t*>(dst) = pair_of<E>(sum[0] * inverse, sum[1] * inverse);
-      else dst[0] = from_float<E>(sum[0] * inverse);
-      if (lane == 0) store_lse(a, at, top, exact);
     }
+    const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
+    const int64_t at = out_row(a, s, h, (int)row);
+    *reinterpret_cast<uint4*>(reinterpret_cast<typename E::T*>(a.out) + at * D + 8 * lane) =
+        make_uint4(pair_of<E>(sum[0] * inverse, sum[1] * inverse), pair_of<E>(sum[2] * inverse, sum[3] * inverse),
+                   pair_of<E>(sum[4] * inverse, sum[5] * inverse), pair_of<E>(sum[6] * inverse, sum[7] * inverse));
+    if (lane == 0) store_lse(a, at, top, exact);
   }
 }
 
@@ -428,7 +457,7 @@ int launch_tiles(const KvpAttend& a, hipStream_t s) {
   const int rc = a.lse ? launch(gemm_kvp_tiles_kernel<E, D, WAVES, true>, with) : launch(gemm_kvp_tiles_kernel<E, D, WAVES, false>, without);
   if (rc != CI_OK) return rc;
   if (a.pieces > 1) {
-    hipLaunchKernelGGL((kvp_join_tiles_kernel<E, D>), dim3(join_blocks((int64_t)a.tiles * a.c.H * (a.tile_rows / 16))), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((kvp_join_tiles_kernel<E, D>), dim3(join_blocks((int64_t)a.tiles * a.c.H * (a.tile_rows / (256 / (D / 8))))), dim3(256), 0, s, a);
     CI_HIP_CHECK_LAUNCH();
   }
   return CI_OK;
