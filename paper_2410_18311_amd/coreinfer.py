@@ -926,8 +926,8 @@ def rope_angles(rot: int, base: float = 10000.0, style: str = "half", scaling: s
     return RopeAngles(turns, float(scale), int(rot), style)
 
 
-def _check_norm(norm: Optional[torch.Tensor], D: int, dtype: torch.dtype):
-    assert norm is None or (norm.shape == (D,) and norm.dtype == dtype and norm.is_contiguous())
+def _check_norm(norm: torch.Tensor, D: int, dtype: torch.dtype):
+    assert norm.shape == (D,) and norm.dtype is dtype and norm.is_contiguous()
 
 
 def rope(x: torch.Tensor, pos: Optional[torch.Tensor], angles: Optional[RopeAngles], norm: Optional[torch.Tensor] = None,
@@ -935,15 +935,17 @@ def rope(x: torch.Tensor, pos: Optional[torch.Tensor], angles: Optional[RopeAngl
     """coreinfer_rope: x [T, H, D] (any strides, channels contiguous), normed by head with `norm` [D] and turned by the
     positions pos [T] int32.  backward: the gradient of the rotation.  out: any strides; may be x."""
     T, H, D = shape = x.shape
-    dtype = x.dtype
+    dtype, s = x.dtype, x.stride()
     if out is None:
         out = torch.empty(shape, dtype=dtype, device=x.device)
-    s, o = x.stride(), out.stride()
-    assert s[2] == 1 and out.shape == shape and out.dtype == dtype and o[2] == 1
-    assert pos is None or (pos.dtype == torch.int32 and pos.shape == (T,) and pos.is_contiguous())
-    _check_norm(norm, D, dtype)
-    status = _rope_call(x.data_ptr(), s[0], s[1], T, H, D, DTYPE_CODE[dtype], _ptr(norm), float(eps),
-                        None if angles is None else angles.ptr, _ptr(pos), int(bool(backward)), out.data_ptr(), o[0], o[1], _stream(x))
+    o = out.stride()
+    assert s[2] == 1 and o[2] == 1 and out.shape == shape and out.dtype is dtype
+    assert pos is None or (pos.dtype is torch.int32 and pos.shape == (T,) and pos.is_contiguous())
+    if norm is not None:
+        _check_norm(norm, D, dtype)
+    status = _rope_call(x.data_ptr(), s[0], s[1], T, H, D, DTYPE_CODE[dtype], None if norm is None else norm.data_ptr(), eps,
+                        None if angles is None else angles.ptr, None if pos is None else pos.data_ptr(), 1 if backward else 0,
+                        out.data_ptr(), o[0], o[1], _stream(x))
     if status != CI_OK:
         raise CoreInferError(status, "coreinfer_rope")
     return out
@@ -958,6 +960,7 @@ class KvpCache:
         self.k, self.v, self.table, self.dtype = k, v, table, k.dtype
         self.pages, self.H, self.page, self.D = k.shape
         self.B, self.most = table.shape
+        self._shape, self._first, self._lens = (self.H, self.D), (self.B + 1,), (self.B,)   # what calls are compared with
         self.desc = ci_kvp(_ptr(k), _ptr(v), _ptr(table), self.pages, self.most, self.B, self.H, self.page, self.D, DTYPE_CODE[k.dtype])
         self.ptr = ctypes.addressof(self.desc)
 
@@ -971,8 +974,8 @@ def kvp_cache(pages: int, H: int, page: int, D: int, dtype: torch.dtype, table: 
 
 
 def _check_packed(cache: KvpCache, first: torch.Tensor, lens: torch.Tensor):
-    assert first.dtype == torch.int32 and first.shape == (cache.B + 1,) and first.is_contiguous()
-    assert lens.dtype == torch.int32 and lens.shape == (cache.B,) and lens.is_contiguous()
+    assert first.dtype is torch.int32 and first.shape == cache._first and first.is_contiguous()
+    assert lens.dtype is torch.int32 and lens.shape == cache._lens and lens.is_contiguous()
 
 
 def kvp_append(cache: KvpCache, k: torch.Tensor, v: torch.Tensor, first: torch.Tensor, lens: torch.Tensor,
@@ -981,26 +984,32 @@ def kvp_append(cache: KvpCache, k: torch.Tensor, v: torch.Tensor, first: torch.T
                q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
     """coreinfer_kvp_append: the packed tokens' k, v [T, H, D] (the same strides, channels contiguous) to their slots, keys normed
     and turned on the way; q [T, Hq, D] goes the same way to q_out, which is returned."""
-    T, H, D = shape = k.shape
-    dtype, s = k.dtype, k.stride()
-    assert v.shape == shape and v.dtype == dtype and v.stride() == s and s[2] == 1
-    assert (H, D, dtype) == (cache.H, cache.D, cache.dtype)
+    shape, dtype, s = k.shape, k.dtype, k.stride()
+    T, D = shape[0], cache.D
+    assert v.shape == shape and v.dtype is dtype and v.stride() == s and s[2] == 1
+    assert shape[1:] == cache._shape and dtype is cache.dtype
     _check_packed(cache, first, lens)
-    assert pos is None or (pos.dtype == torch.int32 and pos.shape == (T,) and pos.is_contiguous())
-    _check_norm(k_norm, D, dtype)
-    _check_norm(q_norm, D, dtype)
-    Hq, qs = 0, (0, 0, 1)
+    assert pos is None or (pos.dtype is torch.int32 and pos.shape == (T,) and pos.is_contiguous())
+    if k_norm is not None:
+        _check_norm(k_norm, D, dtype)
     if q is not None:
-        Hq, qs = q.shape[1], q.stride()
-        assert q.shape == (T, Hq, D) and q.dtype == dtype and qs[2] == 1
+        _, Hq, _ = q_shape = q.shape
+        q0, q1, last = q.stride()
+        assert q_shape == (T, Hq, D) and q.dtype is dtype and last == 1
+        if q_norm is not None:
+            _check_norm(q_norm, D, dtype)
         if q_out is None:
-            q_out = torch.empty((T, Hq, D), dtype=dtype, device=q.device)
-        assert q_out.shape == q.shape and q_out.dtype == dtype and q_out.is_contiguous()
+            q_out = torch.empty(q_shape, dtype=dtype, device=q.device)
+        assert q_out.shape == q_shape and q_out.dtype is dtype and q_out.is_contiguous()
+        q_ptr, q_out_ptr = q.data_ptr(), q_out.data_ptr()
     else:
         assert q_out is None and q_norm is None
-    status = _kvp_append_call(cache.ptr, k.data_ptr(), v.data_ptr(), s[0], s[1], T, first.data_ptr(), lens.data_ptr(), _ptr(pos),
-                              None if angles is None else angles.ptr, _ptr(k_norm), float(eps), _ptr(q), Hq, qs[0], qs[1], _ptr(q_norm),
-                              _ptr(q_out), _stream(k))
+        Hq = q0 = q1 = 0
+        q_ptr = q_out_ptr = None
+    status = _kvp_append_call(cache.ptr, k.data_ptr(), v.data_ptr(), s[0], s[1], T, first.data_ptr(), lens.data_ptr(),
+                              None if pos is None else pos.data_ptr(), None if angles is None else angles.ptr,
+                              None if k_norm is None else k_norm.data_ptr(), eps, q_ptr, Hq, q0, q1,
+                              None if q_norm is None else q_norm.data_ptr(), q_out_ptr, _stream(k))
     if status != CI_OK:
         raise CoreInferError(status, "coreinfer_kvp_append")
     return q_out
@@ -1021,20 +1030,22 @@ def kvp_attend(q: torch.Tensor, cache: KvpCache, first: torch.Tensor, lens: torc
     rows and the table's slots by default; the launches are chosen and sized by them).  scale: 1 / sqrt(D) by default."""
     T, Hq, D = shape = q.shape
     dtype, s = q.dtype, q.stride()
-    assert (D, dtype) == (cache.D, cache.dtype) and s[2] == 1
+    assert D == cache.D and dtype is cache.dtype and s[2] == 1
     _check_packed(cache, first, lens)
-    max_rows = max(T, 1) if max_rows is None else max_rows
-    max_len = cache.most * cache.page if max_len is None else max_len
+    if max_rows is None:
+        max_rows = max(T, 1)
+    if max_len is None:
+        max_len = cache.most * cache.page
     if out is None:
         out = torch.empty(shape, dtype=dtype, device=q.device)
-    assert out.shape == shape and out.dtype == dtype and out.is_contiguous()
-    assert lse is None or (lse.shape == (T, Hq) and lse.dtype == torch.float32 and lse.is_contiguous())
+    assert out.shape == shape and out.dtype is dtype and out.is_contiguous()
+    assert lse is None or (lse.shape == (T, Hq) and lse.dtype is torch.float32 and lse.is_contiguous())
     if ws is None:
         need = kvp_attend_workspace_size(cache, T, Hq, max_rows, max_len, window, sinks)
         ws = _workspace(need, q) if need else None
     status = _kvp_attend_call(cache.ptr, q.data_ptr(), Hq, s[0], s[1], T, first.data_ptr(), lens.data_ptr(), max_rows, max_len, window,
-                              sinks, D ** -0.5 if scale is None else float(scale), out.data_ptr(), _ptr(lse), _ptr(ws),
-                              0 if ws is None else ws.numel(), _stream(q))
+                              sinks, D ** -0.5 if scale is None else scale, out.data_ptr(), None if lse is None else lse.data_ptr(),
+                              None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _stream(q))
     if status != CI_OK:
         raise CoreInferError(status, "coreinfer_kvp_attend")
     return out

@@ -27,9 +27,11 @@ int64_t most_steps(int64_t step, int64_t rows, int64_t max_len, int64_t window, 
 AttendPlan attend_plan(const ci_kvp& c, int64_t T, int64_t G, int64_t max_rows, int64_t max_len, int64_t window, int64_t sinks) {
   AttendPlan p = {};
   const int64_t heads = c.B * c.H, R = max_rows * G;
-  // Prompts of 16-bit types go in tiles.  Where all sentences may be prompts the tiles take short ones too; beside single
-  // tokens they leave those of up to 16 rows.
-  p.in_tiles = c.dtype != CI_F32 && R > 64;
+  // Rows of 16-bit types go in tiles where a head has more than 64; from 17 on where the others' rereading of the cache, once for 16 rows, is
+  // 192k slots or more (32 heads, rows kernel and tiles: 64 rows over 1000 slots 22.5 and 23.4 us, over 4000 46.8 and 28.3, over 16000
+  // 156 and 65; 24 rows over 1000 15.4 and 22.5, over 16000 89.6 and 60.8).  Where all sentences may be prompts the tiles take short ones too;
+  // beside single tokens they leave those of up to 16 rows.
+  p.in_tiles = c.dtype != CI_F32 && (R > 64 || (R > 16 && heads * ((R + 15) / 16) * max_len >= (int64_t)192 << 10));
   p.rows = !p.in_tiles || T < c.B * max_rows;
   p.few = !p.in_tiles ? 1 << 30 : p.rows ? 16 : 0;
   auto take = [&](size_t words) {
@@ -57,8 +59,9 @@ AttendPlan attend_plan(const ci_kvp& c, int64_t T, int64_t G, int64_t max_rows, 
   if (p.in_tiles) {
     p.tiles = (int)(T * G / kTileRows + c.B);   // see tile_start
     const int64_t full = (T * G + kTileRows - 1) / kTileRows * c.H, steps = most_steps(64, max_rows, max_len, window, sinks);
-    // As many workgroups as fit at once (three a compute unit of 64 channels, two of 128); no piece below eight steps.
-    p.pieces = (int)std::max<int64_t>(1, std::min<int64_t>({(c.D == 64 ? 3 : 2) * kCus / full, steps / 8, kMaxPieces}));
+    // As many workgroups as fit at once (three a compute unit of 64 channels, two of 128); no piece below eight steps, and no more partial
+    // results than of 8 kCus tiles, however many sentences there may be.
+    p.pieces = (int)std::max<int64_t>(1, std::min<int64_t>({(c.D == 64 ? 3 : 2) * kCus / full, steps / 8, kMaxPieces, 8 * kCus / (p.tiles * c.H)}));
     if (p.pieces > 1) {
       const size_t rows = (size_t)p.tiles * c.H * p.pieces * kTileRows;
       p.tile_m = take(rows);

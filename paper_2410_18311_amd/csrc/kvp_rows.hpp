@@ -131,10 +131,9 @@ __global__ __launch_bounds__(256, 2) void gemm_kvp_rows_kernel(KvpAttend a) {
   const int piece = ((int)blockIdx.x - found.before) / a.c.H, h = (int)blockIdx.x - found.before - piece * a.c.H;
   const Sentence s = found.s;
   const int R = s.rows * a.G;
-  const Steps<32> steps(a, max(s.slot, 0), s.slot + s.rows - 1, s.len);
+  const Steps<32> all(a, max(s.slot, 0), s.slot + s.rows - 1, s.len);
   if (a.wanted && (int)blockIdx.x == found.before && blockIdx.y == 0 && threadIdx.x == 0)
     a.place[b] = make_int2(found.before, found.pieces);   // for the join
-  const int begin = min(steps.total, piece * found.chunk), end = min(steps.total, begin + min(found.chunk, steps.total));
   const Pages pages(a, b, s.len);
   const int inside = (1 << a.c.shift) - 1;
   for (int tile = blockIdx.y; tile * 16 < R; tile += gridDim.y) {
@@ -142,6 +141,9 @@ __global__ __launch_bounds__(256, 2) void gemm_kvp_rows_kernel(KvpAttend a) {
     const int row = min(row0 + n, R - 1);   // rows past the last repeat it
     const int p = s.slot + row / a.G;
     const int p_low = s.slot + row0 / a.G, p_high = s.slot + min(row0 + 15, R - 1) / a.G;   // of the tile's rows
+    // a piece of the sentence's steps, or all of the tile's own
+    const Steps<32> steps = found.pieces > 1 ? all : Steps<32>(a, max(p_low, 0), p_high, s.len);
+    const int begin = min(steps.total, piece * found.chunk), end = min(steps.total, begin + min(found.chunk, steps.total));
 
     if (threadIdx.x == 0) broken = 0;
     uint4 q[K];

@@ -62,9 +62,24 @@ struct Place {
 };
 __device__ __forceinline__ Place place_of(const RopeCall& a, int t) {
   Place p{-1, 0, 0};
-  const int b = sentence_of(a.first, a.cache.B, t);
-  const int from = clamp_row(a.first[b], a.T), to = clamp_row(a.first[b + 1], a.T);
-  const int64_t slot = (int64_t)a.lens[b] - (to - from) + (t - from);
+  int b, from, to, len;
+  if (a.cache.B <= 64) {
+    // everything that the sentence may be asked for comes with the search
+    const int lane = threadIdx.x & 63, own = a.first[min(lane, a.cache.B)], next = a.first[min(lane + 1, a.cache.B)],
+              held = a.lens[min(lane, a.cache.B - 1)];
+    b = __popcll(__ballot(lane == 0 || (lane < a.cache.B && own <= t))) - 1;
+    from = __builtin_amdgcn_readlane(own, b);
+    to = __builtin_amdgcn_readlane(next, b);
+    len = __builtin_amdgcn_readlane(held, b);
+  } else {
+    b = sentence_of(a.first, a.cache.B, t);
+    from = a.first[b];
+    to = a.first[b + 1];
+    len = a.lens[b];
+  }
+  from = clamp_row(from, a.T);
+  to = clamp_row(to, a.T);
+  const int64_t slot = (int64_t)len - (to - from) + (t - from);
   if (t < from || t >= to) return p;
   p.mine = 1;
   p.pos = (int)slot;

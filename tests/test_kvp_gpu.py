@@ -15,7 +15,7 @@ DEV = "cuda:0"
 F16, BF16, F32 = torch.float16, torch.bfloat16, torch.float32
 HALF = {F32: 2.0 ** -24, F16: 2.0 ** -11, BF16: 2.0 ** -8}
 TINY = {F32: 2.0 ** -150, F16: 2.0 ** -25, BF16: 2.0 ** -134}
-FEW = 64   # rows of a head of the cache up to which probabilities enter in two pieces
+FEW = 64   # rows of a head of the cache up to which probabilities enter in two pieces (16 where contexts are long)
 
 
 def _rand(shape, dtype, seed, std=1.0):
@@ -224,8 +224,8 @@ def _bound(dtype, want, size, reach, D, n, rows_share):
 
 
 def _check_attend(lib, lens, rows, H, G, D, page, dtype, window=0, sinks=0, seed=0, qstd=1.0, max_rows=None, max_len=None, tail=0,
-                  table_edit=None, edit=None, odd=0, scale=None):
-    cache, table = _cache(lib, H, page, D, dtype, lens, seed)
+                  table_edit=None, edit=None, odd=0, scale=None, share=None, ahead=1):
+    cache, table = _cache(lib, H, page, D, dtype, lens, seed, ahead=ahead)
     _fill(cache, table, lens, seed + 50)
     if table_edit:
         table_edit(table)
@@ -245,7 +245,7 @@ def _check_attend(lib, lens, rows, H, G, D, page, dtype, window=0, sinks=0, seed
     got, got_lse = f64(out), f64(lse)
     mine = ~np.isnan(want_lse)
     assert np.all(got[~mine] == 5.0) and np.all(got_lse[~mine] == 5.0)
-    share = max(rows) * G
+    share = share or max(rows) * G
     ok = np.abs(got - want)[mine] <= _bound(dtype, want, size, reach, D, max(seen), share)[mine]
     assert ok.all(), (np.abs(got - want)[mine] / _bound(dtype, want, size, reach, D, max(seen), share)[mine]).max()
     none = mine & np.isneginf(want_lse)
@@ -304,6 +304,14 @@ def test_slots_shared_out_over_the_chip(lib, B, dtype):
 def test_a_long_context(lib):
     for dtype in (F16, BF16):
         _check_attend(lib, [16000, 3000], [1, 2], 1, 2, 128, 64, dtype, seed=1, qstd=2.0)
+
+
+def test_some_rows_over_a_long_context(lib):
+    """Few rows that go in tiles all the same, whose probabilities are rounded once."""
+    for dtype in (F16, BF16, F32):
+        _check_attend(lib, [4200, 50], [48, 17], 8, 1, 64, 16, dtype, seed=21, share=FEW + 1)
+        _check_attend(lib, [2100, 700, 9], [5, 5, 0], 4, 8, 128, 64, dtype, 600, 70, seed=22, share=FEW + 1, max_len=6000, ahead=61)
+        _check_attend(lib, [1000, 90], [17, 1], 2, 1, 64, 16, dtype, seed=23, share=FEW + 1, max_len=1 << 17, ahead=1 << 13)
 
 
 def test_a_mixed_batch(lib):

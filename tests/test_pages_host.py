@@ -119,6 +119,17 @@ def test_every_call_refuses_a_bad_cache(lib, name):
             assert call(_cache(lib, **kw)) == lib.CI_ERR_BAD_LAYOUT, kw
 
 
+def test_workspaces_stay_small_however_many_sentences(lib):
+    """Partial results are a few thousand tiles' at most: 128 MiB and some for B = 1, not that for each sentence."""
+    for dtype in (lib.CI_F16, lib.CI_F32):
+        for B in (1, 7, 100, 1000, 8000):
+            for T, rows in ((B, 1), (B + 500, 500), (1 << 16, 1 << 16)):
+                for most in (4, 1 << 12, 1 << 18):
+                    cache = _cache(lib, B=B, H=8, D=128, page=64, most=most, dtype=dtype)
+                    rc, n = _size(lib, cache, T, 16, min(rows, T), most * 64)
+                    assert rc == 0 and n <= 300 << 20, (B, T, rows, most, n)
+
+
 def test_append_refuses(lib):
     q = dict(q=F, Hq=2, qst=STRIDE, qo=2 * F)
     assert _append(lib, rope=_rope(lib, style=5)) == lib.CI_ERR_BAD_DTYPE
