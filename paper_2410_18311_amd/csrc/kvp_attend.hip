@@ -1,4 +1,5 @@
-// Attention over a cache in pages: how a call is split over the chip (the kernels are in kvp_rows.hpp and kvp_tiles.hpp).
+// Attention over a cache in pages: how a call is split over the chip (the kernels are in kvp_rows.hpp, kvp_tiles.hpp and
+// kvp_mixed.hpp).
 #include <algorithm>
 
 #include "kvp_attend.hpp"
@@ -59,8 +60,9 @@ AttendPlan attend_plan(const ci_kvp& c, int64_t T, int64_t G, int64_t max_rows, 
   if (p.in_tiles) {
     p.tiles = (int)(T * G / kTileRows + c.B);   // see tile_start
     const int64_t full = (T * G + kTileRows - 1) / kTileRows * c.H, steps = most_steps(64, max_rows, max_len, window, sinks);
-    // As many workgroups as fit at once (three a compute unit of 64 channels, two of 128); no piece below eight steps, and no more partial
-    // results than of 8 kCus tiles, however many sentences there may be.
+    // As many workgroups as fit at once (three a compute unit of 64 channels, two of 128: 512 rows over 16384 slots of 32 heads in 4 pieces 53 us,
+    // in 3 56, in 5 70, in 8 65); no piece below eight steps, and no more partial results than of 8 kCus tiles, however many sentences
+    // there may be.
     p.pieces = (int)std::max<int64_t>(1, std::min<int64_t>({(c.D == 64 ? 3 : 2) * kCus / full, steps / 8, kMaxPieces, 8 * kCus / (p.tiles * c.H)}));
     if (p.pieces > 1) {
       const size_t rows = (size_t)p.tiles * c.H * p.pieces * kTileRows;

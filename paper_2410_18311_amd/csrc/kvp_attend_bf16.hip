@@ -1,12 +1,8 @@
-// Attention over a cache in pages: the bf16 kernels (kvp_rows.hpp, kvp_tiles.hpp).
-#include "kvp_rows.hpp"
-#include "kvp_tiles.hpp"
+// Attention over a cache in pages: the bf16 kernels.
+#include "kvp_mixed.hpp"
 
 namespace ci {
 template <> int launch_kvp_attend_type<BF16>(const KvpAttend& a, int D, bool rows, bool tiles, hipStream_t s) {
-  int rc = CI_OK;
-  if (tiles) rc = D == 64 ? launch_tiles<BF16, 64, 4>(a, s) : launch_tiles<BF16, 128, 4>(a, s);
-  if (rows && rc == CI_OK) rc = D == 64 ? launch_rows<BF16, 64>(a, s) : launch_rows<BF16, 128>(a, s);
-  return rc;
+  return D == 64 ? launch_16bit<BF16, 64>(a, rows, tiles, s) : launch_16bit<BF16, 128>(a, rows, tiles, s);
 }
 }  // namespace ci

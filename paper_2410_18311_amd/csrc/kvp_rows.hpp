@@ -116,27 +116,34 @@ __device__ __forceinline__ void load_query(const KvpAttend& a, const Sentence& s
   }
 }
 
+template <int D>
+struct RowsLds {
+  float ml[2][4][16];
+  __attribute__((aligned(16))) float sums[4][16][D + 4];
+  unsigned broken;   // rows, a bit each
+};
+
+// Piece `block` of all, the tiles from tile0 on that are `stride` apart.
 template <class E, int D>
-__global__ __launch_bounds__(256, 2) void gemm_kvp_rows_kernel(KvpAttend a) {
+__device__ __forceinline__ void rows_block(const KvpAttend& a, int block, int tile0, int stride, RowsLds<D>& lds) {
   using S32 = Step32<E, D>;
   constexpr int K = S32::K, CH = S32::CH, VW = S32::V;
-  __shared__ float ml[2][4][16];
-  __shared__ __attribute__((aligned(16))) float sums[4][16][D + 4];
-  __shared__ unsigned broken;   // rows, a bit each
+  auto& ml = lds.ml;
+  auto& sums = lds.sums;
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Piece found(a, blockIdx.x);
+  const Piece found(a, block);
   const int b = found.b;
   if (b >= a.c.B) return;
-  const int piece = ((int)blockIdx.x - found.before) / a.c.H, h = (int)blockIdx.x - found.before - piece * a.c.H;
+  const int piece = (block - found.before) / a.c.H, h = block - found.before - piece * a.c.H;
   const Sentence s = found.s;
   const int R = s.rows * a.G;
   const Steps<32> all(a, max(s.slot, 0), s.slot + s.rows - 1, s.len);
-  if (a.wanted && (int)blockIdx.x == found.before && blockIdx.y == 0 && threadIdx.x == 0)
+  if (a.wanted && block == found.before && tile0 == 0 && threadIdx.x == 0)
     a.place[b] = make_int2(found.before, found.pieces);   // for the join
   const Pages pages(a, b, s.len);
   const int inside = (1 << a.c.shift) - 1;
-  for (int tile = blockIdx.y; tile * 16 < R; tile += gridDim.y) {
+  for (int tile = tile0; tile * 16 < R; tile += stride) {
     const int row0 = tile * 16;
     const int row = min(row0 + n, R - 1);   // rows past the last repeat it
     const int p = s.slot + row / a.G;
@@ -145,7 +152,7 @@ __global__ __launch_bounds__(256, 2) void gemm_kvp_rows_kernel(KvpAttend a) {
     const Steps<32> steps = found.pieces > 1 ? all : Steps<32>(a, max(p_low, 0), p_high, s.len);
     const int begin = min(steps.total, piece * found.chunk), end = min(steps.total, begin + min(found.chunk, steps.total));
 
-    if (threadIdx.x == 0) broken = 0;
+    if (threadIdx.x == 0) lds.broken = 0;
     uint4 q[K];
     load_query<E, D>(a, s, h, row, q);
 
@@ -286,7 +293,7 @@ __global__ __launch_bounds__(256, 2) void gemm_kvp_rows_kernel(KvpAttend a) {
     __syncthreads();
 
     const int live = min(16, R - row0);
-    const size_t part = a.wanted ? ((size_t)blockIdx.x * a.row_tiles + tile) * 16 : 0;
+    const size_t part = a.wanted ? ((size_t)block * a.row_tiles + tile) * 16 : 0;
     for (int e = threadIdx.x; e < live * (D / 4); e += 256) {
       const int r = e / (D / 4), d = e % (D / 4) * 4;
       float t = -INFINITY, total = 0.0f, v[4];
@@ -297,7 +304,7 @@ __global__ __launch_bounds__(256, 2) void gemm_kvp_rows_kernel(KvpAttend a) {
         total += ml[0][w][r] == -INFINITY ? ml[1][w][r] : ml[1][w][r] * __builtin_amdgcn_exp2f(ml[0][w][r] - t);
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[i] = (sums[0][r][d + i] + sums[1][r][d + i]) + (sums[2][r][d + i] + sums[3][r][d + i]);
-      if (!(finite(v[0]) && finite(v[1]) && finite(v[2]) && finite(v[3]))) atomicOr(&broken, 1u << r);
+      if (!(finite(v[0]) && finite(v[1]) && finite(v[2]) && finite(v[3]))) atomicOr(&lds.broken, 1u << r);
       if (a.wanted) {
         *reinterpret_cast<float4*>(a.o + (part + r) * D + d) = make_float4(v[0], v[1], v[2], v[3]);
         if (d == 0) {
@@ -315,7 +322,7 @@ __global__ __launch_bounds__(256, 2) void gemm_kvp_rows_kernel(KvpAttend a) {
     }
     __syncthreads();
     // an infinity or a NaN among the values, seen or not
-    for (unsigned left = broken; left; left &= left - 1) {
+    for (unsigned left = lds.broken; left; left &= left - 1) {
       const int r = __builtin_ctz(left);
       float mr, lr, o;
       careful_row<E, D, 32, 256>(a, s, pages, h, row0 + r, steps, begin, end, &sums[0][0][0], &mr, &lr, &o);
@@ -335,13 +342,19 @@ __global__ __launch_bounds__(256, 2) void gemm_kvp_rows_kernel(KvpAttend a) {
   }
 }
 
+template <class E, int D>
+__global__ __launch_bounds__(256, 2) void gemm_kvp_rows_kernel(KvpAttend a) {
+  __shared__ RowsLds<D> lds;
+  rows_block<E, D>(a, blockIdx.x, blockIdx.y, gridDim.y, lds);
+}
+
 // The pieces of a row put together, a workgroup a row: a wave takes every fourth, all of which it requests at once.
 template <class E, int D>
-__global__ __launch_bounds__(256) void kvp_join_kernel(KvpAttend a) {
+__device__ __forceinline__ void join_rows(const KvpAttend& a, int64_t block, int64_t blocks) {
   constexpr int N = kMaxPieces / 4, C = D / 64;
   __shared__ float sums[4][D];
   const int Hq = a.c.H * a.G, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  for (int64_t each = blockIdx.x; each < (int64_t)a.c.B * a.join_rows * Hq; each += gridDim.x) {
+  for (int64_t each = block; each < (int64_t)a.c.B * a.join_rows * Hq; each += blocks) {
     const int b = (int)(each / (a.join_rows * Hq)), in = (int)(each - (int64_t)b * a.join_rows * Hq);
     const int i = in / Hq, head = in - i * Hq, h = head / a.G;
     const Sentence s = sentence(a, b);
@@ -383,11 +396,15 @@ __global__ __launch_bounds__(256) void kvp_join_kernel(KvpAttend a) {
 }
 
 template <class E, int D>
+__global__ __launch_bounds__(256) void kvp_join_kernel(KvpAttend a) { join_rows<E, D>(a, blockIdx.x, gridDim.x); }
+inline unsigned join_rows_blocks(const KvpAttend& a) { return join_blocks((int64_t)a.c.B * a.join_rows * a.c.H * a.G); }
+
+template <class E, int D>
 int launch_rows(const KvpAttend& a, hipStream_t s) {
   hipLaunchKernelGGL((gemm_kvp_rows_kernel<E, D>), dim3((unsigned)a.blocks, (unsigned)a.row_tiles), dim3(256), 0, s, a);
   CI_HIP_CHECK_LAUNCH();
   if (a.wanted) {
-    hipLaunchKernelGGL((kvp_join_kernel<E, D>), dim3(join_blocks((int64_t)a.c.B * a.join_rows * a.c.H * a.G)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((kvp_join_kernel<E, D>), dim3(join_rows_blocks(a)), dim3(256), 0, s, a);
     CI_HIP_CHECK_LAUNCH();
   }
   return CI_OK;

@@ -62,8 +62,9 @@ __device__ __forceinline__ int sentence_of_tile(const KvpAttend& a, int tile, in
   return __builtin_amdgcn_readfirstlane(lo);
 }
 
+// Piece `piece` of the steps of a tile of a head.
 template <class E, int D, int WAVES, bool LSE>
-__global__ __launch_bounds__(64 * WAVES, 2) void gemm_kvp_tiles_kernel(KvpAttend a) {
+__device__ __forceinline__ void tile_block(const KvpAttend& a, int block, int piece) {
   constexpr int BM = 32 * WAVES, ROW = 2 * D, HALF = kTileStep * ROW, KK = D / 16, CB = D / 32;
   constexpr int LOADS = HALF / 1024 / WAVES, ROWS = 1024 / ROW;   // loads of a wave and tensor, rows of a load
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];   // two steps' keys and two steps' values, 64 rows each
@@ -71,7 +72,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_kvp_tiles_kernel(KvpAttend
   __shared__ int missing[WAVES];   // whether a wave has met slots without a page
   const int lane = threadIdx.x & 63, n = lane & 31, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int h = blockIdx.x % a.c.H, tile = a.tiles - 1 - (int)(blockIdx.x / a.c.H);   // the last tiles of a prompt see most
+  const int h = block % a.c.H, tile = a.tiles - 1 - block / a.c.H;   // the last tiles of a prompt see most
   const int b = sentence_of_tile(a, tile, BM);
   const Sentence s = uniform(sentence(a, b));
   const int R = s.rows * a.G;
@@ -82,7 +83,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_kvp_tiles_kernel(KvpAttend
   const int row = min(mine0 + n, R - 1), p = s.slot + row / a.G;
   const int p_low = s.slot + min(mine0, R - 1) / a.G, p_high = s.slot + min(mine0 + 31, R - 1) / a.G;
   const Steps<kTileStep> steps(a, max(s.slot + row0 / a.G, 0), s.slot + min(row0 + BM - 1, R - 1) / a.G, s.len);
-  const int begin = (int)((int64_t)steps.total * blockIdx.y / a.pieces), end = (int)((int64_t)steps.total * (blockIdx.y + 1) / a.pieces);
+  const int begin = (int)((int64_t)steps.total * piece / a.pieces), end = (int)((int64_t)steps.total * (piece + 1) / a.pieces);
   const Pages pages(a, b, s.len);
   const int inside = (1 << a.c.shift) - 1;
 
@@ -311,7 +312,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_kvp_tiles_kernel(KvpAttend
     for (int e = 0; e < 16; ++e) whole = whole && finite(acc[c][e]);
   const uint64_t bad = __ballot(!whole);
   const bool valid = live && mine0 + n < R;
-  const size_t part = ((size_t)blockIdx.x * a.pieces + blockIdx.y) * BM + 32 * wave;
+  const size_t part = ((size_t)block * a.pieces + piece) * BM + 32 * wave;
   if (valid && g == 0) {
     if (a.pieces > 1) {
       a.tile_m[part + n] = m;
@@ -369,7 +370,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_kvp_tiles_kernel(KvpAttend
       float mr, lr, o;
       careful_row<E, D, kTileStep, 64 * WAVES>(a, s, pages, h, r, steps, begin, end, reinterpret_cast<float*>(smem), &mr, &lr, &o);
       if (a.pieces > 1) {
-        const size_t to = ((size_t)blockIdx.x * a.pieces + blockIdx.y) * BM + r - row0;
+        const size_t to = ((size_t)block * a.pieces + piece) * BM + r - row0;
         if (threadIdx.x < D) a.tile_o[to * D + threadIdx.x] = o;
         if (threadIdx.x == 0) {
           a.tile_m[to] = mr;
@@ -385,12 +386,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_kvp_tiles_kernel(KvpAttend
   }
 }
 
+template <class E, int D, int WAVES, bool LSE>
+__global__ __launch_bounds__(64 * WAVES, 2) void gemm_kvp_tiles_kernel(KvpAttend a) { tile_block<E, D, WAVES, LSE>(a, blockIdx.x, blockIdx.y); }
+
 // The pieces of a tile's rows put together, eight channels of a row a thread, all pieces' requests at once, eight at a time.
 template <class E, int D>
-__global__ __launch_bounds__(256) void kvp_join_tiles_kernel(KvpAttend a) {
+__device__ __forceinline__ void join_tiles(const KvpAttend& a, int64_t first, int64_t blocks) {
   constexpr int LANES = D / 8, ROWS = 256 / LANES, N = 8;   // lanes of a row, rows of a workgroup
   const int BM = a.tile_rows, parts = BM / ROWS, lane = threadIdx.x % LANES;
-  for (int64_t each = blockIdx.x; each < (int64_t)a.tiles * a.c.H * parts; each += gridDim.x) {
+  for (int64_t each = first; each < (int64_t)a.tiles * a.c.H * parts; each += blocks) {
     const int block = (int)(each / parts), r0 = (int)(each - (int64_t)block * parts) * ROWS + threadIdx.x / LANES;
     const int h = block % a.c.H, tile = a.tiles - 1 - block / a.c.H;
     const int b = sentence_of_tile(a, tile, BM);
@@ -443,6 +447,11 @@ __global__ __launch_bounds__(256) void kvp_join_tiles_kernel(KvpAttend a) {
   }
 }
 
+template <class E, int D>
+__global__ __launch_bounds__(256) void kvp_join_tiles_kernel(KvpAttend a) { join_tiles<E, D>(a, blockIdx.x, gridDim.x); }
+template <int D>
+unsigned join_tiles_blocks(const KvpAttend& a) { return join_blocks((int64_t)a.tiles * a.c.H * (a.tile_rows / (256 / (D / 8)))); }
+
 template <class E, int D, int WAVES>
 int launch_tiles(const KvpAttend& a, hipStream_t s) {
   const size_t lds = 4 * kTileStep * 2 * D;
@@ -457,7 +466,7 @@ int launch_tiles(const KvpAttend& a, hipStream_t s) {
   const int rc = a.lse ? launch(gemm_kvp_tiles_kernel<E, D, WAVES, true>, with) : launch(gemm_kvp_tiles_kernel<E, D, WAVES, false>, without);
   if (rc != CI_OK) return rc;
   if (a.pieces > 1) {
-    hipLaunchKernelGGL((kvp_join_tiles_kernel<E, D>), dim3(join_blocks((int64_t)a.tiles * a.c.H * (a.tile_rows / (256 / (D / 8))))), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((kvp_join_tiles_kernel<E, D>), dim3(join_tiles_blocks<D>(a)), dim3(256), 0, s, a);
     CI_HIP_CHECK_LAUNCH();
   }
   return CI_OK;
