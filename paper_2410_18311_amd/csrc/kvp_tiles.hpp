@@ -1,8 +1,19 @@
-// Attention of prompts over a cache in pages (kvp_attend.hpp), 16-bit types: bound by the matrix cores and what feeds them.
+// Attention of prompts over a cache in pages (kvp_attend.hpp), 16-bit types: bound by the matrix cores and the vector instructions between products.
 //
-// A workgroup takes a tile of rows of a head, 32 to a wave, and steps of 64 slots, which go from the pages straight into the LDS, a step ahead.  Products
+// A workgroup takes a tile of 128 rows of a head, 32 to a wave, and steps of 64 slots, which go from the pages straight into the LDS, a step ahead.  Products
 // of 32 x 32: the logits of 32 rows come out with a row's 32 slots in two lanes, and the values are read from the LDS transposed, four slots of a
-// channel to a lane, in the order in which the probabilities lie.
+// channel to a lane, in the order in which the probabilities lie, so that nothing is exchanged between lanes but a new maximum.  Two workgroups
+// of 128 channels, three of 64, share a compute unit: one's softmax runs beside the other's products.
+//
+// Weights are rounded to the cache's type, as the matrix cores take it: half a unit of a weight, averaged over the slots.  Their sum is that
+// of the rounded ones, so that a row's weights add up to 1; the log-sum, when asked for, is of the exact ones.
+//
+// 4096 tokens of 32 heads of 128, fp16, causal: 150 to 154 us, 0.9 PFLOP/s of the visible half, where a large product of the library reaches 1.2.  The matrix
+// cores are busy for 44 % of the cycles and vector instructions (4.5 a logit, one of them an exponential) take most of the others; the two
+// overlap little: of 32 products in 1030 cycles, reading their operands from the LDS makes 1290 and the next step's loads 1540.
+// Also measured, the same case: 256 rows in eight waves, whose halves take turns at products and softmax, 161 us; 64 rows a wave, one wave a SIMD,
+// 225; steps of 32 slots in a pipeline, 180; operands 6 or 12 products ahead instead of 8, the same; without the waves' raised priority in
+// products 154 where it was 149.  64 channels, 777 rows over 8192 slots, 32 heads: 90 us, where products are a third of the time.
 #pragma once
 
 #include "gemm_tile.hpp"
