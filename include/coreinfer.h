@@ -659,8 +659,8 @@ int coreinfer_rope_turns(int64_t rot, double base, int scaling, double factor, d
  *   NULL where nothing is turned).
  * backward != 0: the angles' signs are turned, which is the gradient (the transpose) of
  * the rotation and, up to scale^2, its inverse; with a norm CI_ERR_INVALID_ARG.
- * Everything in fp32, rounded once.  y (any strides) may be x itself with x's strides, and must not
- * overlap it otherwise.  x and y are aligned to their elements; it is fastest
+ * Everything in fp32, rounded once.  y (any strides at which its rows lie apart, none between another's
+ * heads) may be x itself with x's strides, and must not overlap it otherwise.  x and y are aligned to their elements; it is fastest
  * where they and norm are aligned to 16 bytes, strides included, and D and rot are multiples of 32 bytes.
  * 1 <= H <= 65535, 1 <= D <= CI_MAX_ROPE_CHANNELS.
  */

@@ -986,7 +986,9 @@ def kvp_append(cache: KvpCache, k: torch.Tensor, v: torch.Tensor, first: torch.T
     and turned on the way; q [T, Hq, D] goes the same way to q_out, which is returned."""
     shape, dtype, s = k.shape, k.dtype, k.stride()
     T, D = shape[0], cache.D
-    assert v.shape == shape and v.dtype is dtype and v.stride() == s and s[2] == 1
+    assert v.shape == shape and v.dtype is dtype and s[2] == 1
+    # strides of lengths of one say nothing
+    assert v.stride() == s or all(n == 1 or x == y for n, x, y in zip(shape, v.stride(), s))
     assert shape[1:] == cache._shape and dtype is cache.dtype
     _check_packed(cache, first, lens)
     assert pos is None or (pos.dtype is torch.int32 and pos.shape == (T,) and pos.is_contiguous())

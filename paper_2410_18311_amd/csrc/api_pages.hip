@@ -17,6 +17,12 @@ bool strides_ok(const int64_t* stride) {
     if (stride[i] < 0 || stride[i] > ((int64_t)1 << 40)) return false;
   return true;
 }
+// Whether two of a, b rows that are stride[0], stride[1] apart, D elements each, share an element (or lie in one another).
+bool rows_overlap(const int64_t* stride, int64_t a, int64_t b, int64_t D) {
+  const bool swap = stride[0] < stride[1];
+  const int64_t inner = swap ? stride[0] : stride[1], outer = swap ? stride[1] : stride[0], n = swap ? a : b, m = swap ? b : a;
+  return (n > 1 && inner < D) || (m > 1 && outer < (n > 1 ? (n - 1) * inner : 0) + D);
+}
 
 int rope_status(const ci_rope* r, int64_t D) {
   if (!r) return CI_OK;
@@ -80,6 +86,7 @@ int coreinfer_rope(const void* x, const int64_t* stride, int64_t T, int64_t H, i
   if (!strides_ok(stride) || !strides_ok(y_stride) || !elem_aligned(x, dtype) || !elem_aligned(y, dtype) || !elem_aligned(norm, dtype) ||
       !word_aligned(pos))
     return CI_ERR_BAD_LAYOUT;
+  if (rows_overlap(y_stride, T, H, D)) return CI_ERR_BAD_LAYOUT;
   if (x == y && (stride[0] != y_stride[0] || stride[1] != y_stride[1])) return CI_ERR_BAD_LAYOUT;
   return launch_rope(x, {stride[0], stride[1]}, T, H, D, dtype, norm, eps, rope, pos, backward != 0, y, {y_stride[0], y_stride[1]},
                      (hipStream_t)stream);

@@ -48,7 +48,8 @@ AttendPlan attend_plan(const ci_kvp& c, int64_t T, int64_t G, int64_t max_rows, 
     p.least = 12;
     p.wanted = heads * tiles * 2 > wanted || steps <= p.least ? 0 : (int)(wanted / tiles);
     p.blocks = (int)heads + p.wanted;
-    p.row_tiles = (int)std::min<int64_t>(tiles, 65535);   // beyond, a workgroup takes several
+    // Beyond 64 workgroups a compute unit one takes several tiles: only the sentences that have so many rows need them.
+    p.row_tiles = (int)std::min<int64_t>({tiles, 65535, std::max<int64_t>(1, 64 * kCus / p.blocks)});
     if (p.wanted) {
       const size_t rows = (size_t)p.blocks * p.row_tiles * 16;
       p.place = take(2 * (size_t)c.B);

@@ -185,6 +185,16 @@ def test_append_without_queries_and_without_rotation_copies(lib):
         assert torch.equal(have[table[0][0], :, :7].transpose(0, 1).contiguous().view(torch.int16), want.view(torch.int16))
 
 
+def test_append_of_one_token_whose_values_lie_elsewhere(lib):
+    """Strides of lengths of one are not compared."""
+    cache, table = _cache(lib, 2, 16, 64, F16, [5])
+    k, v = _rand((1, 2, 64), F16, 1), _rand((1, 6, 64), F16, 2)[:, 4:]
+    lib.kvp_append(cache, k, v, _ints(0, 1), _ints(5))
+    assert torch.equal(cache.k[table[0][0], :, 4], k[0]) and torch.equal(cache.v[table[0][0], :, 4], v[0])
+    with pytest.raises(AssertionError):
+        lib.kvp_append(cache, k.expand(2, 2, 64), v.expand(2, 2, 64).contiguous(), _ints(0, 2), _ints(5))
+
+
 def test_slots_far_into_a_large_pool(lib):
     """Offsets past 2^31 elements."""
     H, page, D = 8, 256, 128
@@ -318,6 +328,13 @@ def test_a_mixed_batch(lib):
     for dtype in (F16, BF16, F32):
         _check_attend(lib, [150, 900, 40, 0, 333], [150, 1, 1, 0, 2], 2, 2, 128, 16, dtype, seed=2, tail=1)
         _check_attend(lib, [350, 900, 40, 5, 333], [300, 1, 1, 1, 2], 2, 1, 64, 16, dtype, 100, 4, seed=3)
+
+
+def test_many_sentences_beside_one_of_many_rows(lib):
+    """More rows than there are workgroups for in a launch of many sentences' pieces."""
+    lens, rows = [230] + [5] * 250 + [90], [200] + [1] * 250 + [33]
+    for dtype in (F32, F16):
+        _check_attend(lib, lens, rows, 8, 1, 64, 16, dtype, seed=24)
 
 
 def test_rows_ahead_of_the_first_slot_see_nothing(lib):

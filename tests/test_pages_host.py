@@ -77,6 +77,11 @@ def test_rope_refuses(lib):
         assert _call_rope(lib, **kw) == lib.CI_ERR_BAD_LAYOUT, kw
 
 
+def test_rope_refuses_results_that_overlap(lib):
+    for T, H, yst in ((4, 2, (0, 64)), (4, 2, (128, 63)), (4, 2, (127, 64)), (4, 2, (64, 255)), (4, 1, (63, 0)), (1, 2, (0, 0))):
+        assert _call_rope(lib, T=T, H=H, yst=_strides(*yst)) == lib.CI_ERR_BAD_LAYOUT, (T, H, yst)
+
+
 def test_no_rows_is_nothing_to_do(lib):
     assert _call_rope(lib, T=0, x=None, y=None, pos=None) == lib.CI_OK
     assert _append(lib, T=0, k=None, v=None, first=None, lens=None) == lib.CI_OK
