@@ -902,6 +902,7 @@ class RopeAngles:
         self.turns, self.scale, self.rot, self.style = turns, scale, rot, style
         self.desc = ci_rope(_ptr(turns), scale, rot, ROPE_STYLE[style])
         self.ptr = ctypes.addressof(self.desc)
+        self.device = turns.get_device()
 
 
 def rope_turns(rot: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, original: float = 0.0,
@@ -926,8 +927,12 @@ def rope_angles(rot: int, base: float = 10000.0, style: str = "half", scaling: s
     return RopeAngles(turns, float(scale), int(rot), style)
 
 
-def _check_norm(norm: torch.Tensor, D: int, dtype: torch.dtype):
-    assert norm.shape == (D,) and norm.dtype is dtype and norm.is_contiguous()
+def _check_norm(norm: torch.Tensor, D: int, dtype: torch.dtype, device: int):
+    assert norm.shape == (D,) and norm.dtype is dtype and norm.is_contiguous() and norm.get_device() == device
+
+
+def _check_pos(pos: torch.Tensor, T: int, device: int):
+    assert pos.dtype is torch.int32 and pos.shape == (T,) and pos.is_contiguous() and pos.get_device() == device
 
 
 def rope(x: torch.Tensor, pos: Optional[torch.Tensor], angles: Optional[RopeAngles], norm: Optional[torch.Tensor] = None,
@@ -939,10 +944,13 @@ def rope(x: torch.Tensor, pos: Optional[torch.Tensor], angles: Optional[RopeAngl
     if out is None:
         out = torch.empty(shape, dtype=dtype, device=x.device)
     o = out.stride()
-    assert s[2] == 1 and o[2] == 1 and out.shape == shape and out.dtype is dtype
-    assert pos is None or (pos.dtype is torch.int32 and pos.shape == (T,) and pos.is_contiguous())
+    device = x.get_device()
+    assert s[2] == 1 and o[2] == 1 and out.shape == shape and out.dtype is dtype and out.get_device() == device
+    assert angles is None or angles.device == device
+    if pos is not None:
+        _check_pos(pos, T, device)
     if norm is not None:
-        _check_norm(norm, D, dtype)
+        _check_norm(norm, D, dtype, device)
     status = _rope_call(x.data_ptr(), s[0], s[1], T, H, D, DTYPE_CODE[dtype], None if norm is None else norm.data_ptr(), eps,
                         None if angles is None else angles.ptr, None if pos is None else pos.data_ptr(), 1 if backward else 0,
                         out.data_ptr(), o[0], o[1], _stream(x))
@@ -957,9 +965,11 @@ class KvpCache:
     def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor):
         assert k.dim() == 4 and v.shape == k.shape and v.dtype == k.dtype and k.is_contiguous() and v.is_contiguous()
         assert table.dim() == 2 and table.dtype == torch.int32 and table.is_contiguous()
+        assert k.get_device() == v.get_device() == table.get_device()
         self.k, self.v, self.table, self.dtype = k, v, table, k.dtype
         self.pages, self.H, self.page, self.D = k.shape
         self.B, self.most = table.shape
+        self.device = k.get_device()
         self._shape, self._first, self._lens = (self.H, self.D), (self.B + 1,), (self.B,)   # what calls are compared with
         self.desc = ci_kvp(_ptr(k), _ptr(v), _ptr(table), self.pages, self.most, self.B, self.H, self.page, self.D, DTYPE_CODE[k.dtype])
         self.ptr = ctypes.addressof(self.desc)
@@ -973,7 +983,8 @@ def kvp_cache(pages: int, H: int, page: int, D: int, dtype: torch.dtype, table: 
     return KvpCache(k, v, table)
 
 
-def _check_packed(cache: KvpCache, first: torch.Tensor, lens: torch.Tensor):
+def _check_packed(cache: KvpCache, rows: torch.Tensor, first: torch.Tensor, lens: torch.Tensor):
+    assert rows.get_device() == first.get_device() == lens.get_device() == cache.device
     assert first.dtype is torch.int32 and first.shape == cache._first and first.is_contiguous()
     assert lens.dtype is torch.int32 and lens.shape == cache._lens and lens.is_contiguous()
 
@@ -990,19 +1001,22 @@ def kvp_append(cache: KvpCache, k: torch.Tensor, v: torch.Tensor, first: torch.T
     # strides of lengths of one say nothing
     assert v.stride() == s or all(n == 1 or x == y for n, x, y in zip(shape, v.stride(), s))
     assert shape[1:] == cache._shape and dtype is cache.dtype
-    _check_packed(cache, first, lens)
-    assert pos is None or (pos.dtype is torch.int32 and pos.shape == (T,) and pos.is_contiguous())
+    _check_packed(cache, k, first, lens)
+    device = cache.device
+    assert v.get_device() == device and (angles is None or angles.device == device)
+    if pos is not None:
+        _check_pos(pos, T, device)
     if k_norm is not None:
-        _check_norm(k_norm, D, dtype)
+        _check_norm(k_norm, D, dtype, device)
     if q is not None:
         _, Hq, _ = q_shape = q.shape
         q0, q1, last = q.stride()
-        assert q_shape == (T, Hq, D) and q.dtype is dtype and last == 1
+        assert q_shape == (T, Hq, D) and q.dtype is dtype and last == 1 and q.get_device() == device
         if q_norm is not None:
-            _check_norm(q_norm, D, dtype)
+            _check_norm(q_norm, D, dtype, device)
         if q_out is None:
             q_out = torch.empty(q_shape, dtype=dtype, device=q.device)
-        assert q_out.shape == q_shape and q_out.dtype is dtype and q_out.is_contiguous()
+        assert q_out.shape == q_shape and q_out.dtype is dtype and q_out.is_contiguous() and q_out.get_device() == device
         q_ptr, q_out_ptr = q.data_ptr(), q_out.data_ptr()
     else:
         assert q_out is None and q_norm is None
@@ -1033,15 +1047,17 @@ def kvp_attend(q: torch.Tensor, cache: KvpCache, first: torch.Tensor, lens: torc
     T, Hq, D = shape = q.shape
     dtype, s = q.dtype, q.stride()
     assert D == cache.D and dtype is cache.dtype and s[2] == 1
-    _check_packed(cache, first, lens)
+    _check_packed(cache, q, first, lens)
     if max_rows is None:
         max_rows = max(T, 1)
     if max_len is None:
         max_len = cache.most * cache.page
     if out is None:
         out = torch.empty(shape, dtype=dtype, device=q.device)
-    assert out.shape == shape and out.dtype is dtype and out.is_contiguous()
-    assert lse is None or (lse.shape == (T, Hq) and lse.dtype is torch.float32 and lse.is_contiguous())
+    device = cache.device
+    assert out.shape == shape and out.dtype is dtype and out.is_contiguous() and out.get_device() == device
+    assert lse is None or (lse.shape == (T, Hq) and lse.dtype is torch.float32 and lse.is_contiguous() and lse.get_device() == device)
+    assert ws is None or ws.get_device() == device
     if ws is None:
         need = kvp_attend_workspace_size(cache, T, Hq, max_rows, max_len, window, sinks)
         ws = _workspace(need, q) if need else None

@@ -553,3 +553,24 @@ def test_a_prompt_in_chunks_and_token_by_token_is_the_prompt_at_once(lib, dtype)
     slack = 2.0 * 8.0 * HALF[dtype] * reach[..., None] * size
     err = np.abs(f64(got) - want)
     assert np.all(err <= _bound(dtype, want, size, reach, D, n, n * G) + slack)
+
+
+def test_tensors_of_another_device_are_refused(lib):
+    """Host tensors among the device's would be read by the kernels at the host's addresses."""
+    cache, table = _cache(lib, 2, 16, 64, F16, [5])
+    x, first, lens = _rand((1, 2, 64), F16, 1), _ints(0, 1), _ints(5)
+    angles, host = lib.rope_angles(64, device=DEV), lib.rope_angles(64, device="cpu")
+    norm, pos = torch.ones(64, dtype=F16), torch.zeros(1, dtype=torch.int32)
+    for kw in (dict(k=x.cpu()), dict(v=x.cpu()), dict(first=first.cpu()), dict(lens=lens.cpu()), dict(angles=host), dict(pos=pos),
+               dict(k_norm=norm), dict(q=x.cpu()), dict(q=x, q_norm=norm), dict(q=x, q_out=torch.empty(1, 2, 64, dtype=F16))):
+        with pytest.raises(AssertionError):
+            lib.kvp_append(**{**dict(cache=cache, k=x, v=x, first=first, lens=lens), **kw})
+    for kw in (dict(q=x.cpu()), dict(first=first.cpu()), dict(lens=lens.cpu()), dict(out=torch.empty(1, 2, 64, dtype=F16)),
+               dict(lse=torch.empty(1, 2)), dict(ws=torch.empty(1 << 20, dtype=torch.uint8))):
+        with pytest.raises(AssertionError):
+            lib.kvp_attend(**{**dict(q=x, cache=cache, first=first, lens=lens), **kw})
+    for kw in (dict(pos=pos), dict(angles=host), dict(norm=norm), dict(out=torch.empty(1, 2, 64, dtype=F16))):
+        with pytest.raises(AssertionError):
+            lib.rope(**{**dict(x=x, pos=_ints(0), angles=angles), **kw})
+    with pytest.raises(AssertionError):
+        lib.kvp_cache(1, 2, 16, 64, F16, torch.zeros(1, 1, dtype=torch.int32)).__class__(cache.k, cache.v, torch.zeros(1, 1, dtype=torch.int32))
