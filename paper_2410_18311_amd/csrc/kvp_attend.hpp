@@ -77,6 +77,11 @@ __device__ __forceinline__ void two_pieces(float x, float y, uint32_t* high, uin
   *low = pair_of<E>(x - t[0], y - t[1]);
 }
 
+// A row's running reference m is below the largest logit so far by this to begin with, and follows it when one passes m by kRaise: weights of up to
+// 2^15 are numbers of every type, and in fp16, whose smallest step is 2^-24, those of 2^-31 of the largest still count when there are very many.
+template <class E> constexpr float kBelow = __is_same(E, F16) ? 7.0f : 0.0f;
+template <class E> constexpr float kRaise = kBelow<E> + 8.0f;
+
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }   // false for NaN
 
 // A sentence's rows: they begin at packed row `first`, `rows` of them are this call's, the first in slot `slot` (negative: ahead of the

@@ -231,11 +231,11 @@ __device__ __forceinline__ void rows_block(const KvpAttend& a, int block, int ti
             if (masked) z[i][r] = ((page[i] >= 0) & sees(a, p, t + 16 * i + 4 * g + r)) ? z[i][r] : -INFINITY;
           }
         float top = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])), fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3])));
-        // The maximum is raised only when a logit passes it by 2^8; the sums hold that range in fp32.
-        if (__any(top > m + 8.0f)) {
+        // m is raised only when a logit passes it by kRaise; the sums hold that range in fp32.
+        if (__any(top > m + kRaise<E>)) {
           top = fmaxf(top, __shfl_xor(top, 16, kWave));
           top = fmaxf(top, __shfl_xor(top, 32, kWave));
-          const float raised = fmaxf(m, top), was = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - raised);
+          const float raised = fmaxf(m, top - kBelow<E>), was = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - raised);
           m = raised;
           l *= was;
 #pragma unroll

@@ -212,10 +212,10 @@ __device__ __forceinline__ void tile_block(const KvpAttend& a, int block, int pi
       for (int e = 1; e < 8; ++e) tops[j] = fmaxf(tops[j], z[j / 2][8 * (j % 2) + e]);
     }
     float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * a.scale;
-    // The maximum is raised only when a logit passes it by 2^8; the sums hold that range in fp32, and so do probabilities of 16 bits.
-    if (__any(top > m + 8.0f)) {
+    // m is raised only when a logit passes it by kRaise; the sums hold that range in fp32, and so do weights of 16 bits.
+    if (__any(top > m + kRaise<E>)) {
       top = fmaxf(top, __shfl_xor(top, 32, kWave));
-      const float raised = fmaxf(m, top), was = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - raised);
+      const float raised = fmaxf(m, top - kBelow<E>), was = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - raised);
       m = raised;
       l *= was;
       exact *= was;

@@ -442,6 +442,27 @@ def test_maxima_that_rise_all_the_way(lib):
             _check_attend(lib, [300], [rows], 1, 1, 64, 16, dtype, seed=10, edit=edit, scale=1.0)
 
 
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("rows", [1, 65])
+def test_very_many_slots_of_next_to_no_weight(lib, rows, dtype):
+    """2^18 slots of 2^-25.2 of the first one's weight are 0.7 % of the sum together."""
+    n, D, page = 1 << 18, 64, 256
+    cache = lib.kvp_cache(n // page, 1, page, D, dtype, torch.arange(n // page, dtype=torch.int32, device=DEV).reshape(1, -1))
+    cache.k.zero_()
+    cache.v.fill_(1.0)
+    cache.k[0, 0, 0, 0] = 17.5     # logits 17.5 and 0; 17.5 log2(e) = 25.25
+    cache.v[0, 0, 0] = -1.0
+    q = torch.zeros((rows, 1, D), dtype=dtype, device=DEV)
+    q[..., 0] = 1.0
+    got = f64(lib.kvp_attend(q, cache, _ints(0, rows), _ints(n), scale=1.0))
+    small = np.exp(-17.5) * (n - rows + np.arange(rows, dtype=np.float64))
+    want = ((small - 1.0) / (small + 1.0))[:, None, None]
+    # the result's rounding; a weight's own, of the small ones' sum; fp32 sums of n / 4 terms at most, of the small ones' sum too, and exponentials of
+    # 25 within 2^-24 of it
+    rel = HALF[dtype] + 2.0 ** -24 * (n / 4.0 + 100.0)
+    assert np.all(np.abs(got - want) <= HALF[dtype] + 2.0 * rel * small[:, None, None] + 2.0 ** -20)
+
+
 def test_strided_and_misaligned_queries(lib):
     for odd in (1, 8):
         _check_attend(lib, [40, 70], [3, 1], 2, 2, 64, 16, F16, seed=11, odd=odd)
