@@ -19,12 +19,23 @@ namespace ci {
 namespace {
 
 // How the slots are shared out: pieces of `chunk` steps, so that a long sentence among short ones has as many workgroups as its
-// length asks for.  Everything follows from first and lens, in every wave for itself, a sentence a lane.
+// length asks for; or a head's slots in one piece where there are enough heads.  Everything follows from first and lens, in every
+// wave for itself, a sentence a lane.
 struct Piece {
   Sentence s;
-  int b, before, pieces, steps;   // the sentence, the pieces before its own, how many a head has, the steps of all; b = B: no such piece
+  int b, before, pieces;   // the sentence, the pieces before its own, how many a head has; b = B: no such piece
   int chunk;
   __device__ Piece(const KvpAttend& a, int at) {
+    if (!a.wanted) {
+      // nothing to look for: one token of 4000 sentences of 64 slots, 8 heads, 297 us, and 1127 when their pieces were counted all the same
+      b = at / a.c.H;
+      before = b * a.c.H;
+      pieces = 1;
+      chunk = 1 << 30;
+      s = uniform(sentence(a, b));
+      if (s.rows == 0 || (int64_t)s.rows * a.G > a.few) b = a.c.B;
+      return;
+    }
     const int lane = threadIdx.x & 63;
     Sentence own{0, 0, 0, 0};
     int mine = -1;   // steps of the lane's sentence; -1: another's work, or none
@@ -36,27 +47,24 @@ struct Piece {
         mine = Steps<32>(a, max(own.slot, 0), own.slot + own.rows - 1, own.len).total;
     };
     look(0);
-    chunk = 1 << 30;
-    if (a.wanted) {
-      int64_t total = 0;
-      int longest = 0;
-      for (int b0 = 0;;) {
-        const int v = max(mine, 0);
-        if (a.c.B == 1) {
-          total = longest = __builtin_amdgcn_readfirstlane(v);
-        } else {
-          total += __builtin_amdgcn_readlane(scan_add(v), 63);
-          longest = max(longest, __builtin_amdgcn_readlane(scan_max(v), 63));
-        }
-        b0 += 64;
-        if (b0 >= a.c.B) break;
-        look(b0);
+    int64_t total = 0;
+    int longest = 0;
+    for (int b0 = 0;;) {
+      const int v = max(mine, 0);
+      if (a.c.B == 1) {
+        total = longest = __builtin_amdgcn_readfirstlane(v);
+      } else {
+        total += __builtin_amdgcn_readlane(scan_add(v), 63);
+        longest = max(longest, __builtin_amdgcn_readlane(scan_max(v), 63));
       }
-      if (a.c.B > 64) look(0);
-      // all pieces together are at most wanted + B H: a sentence's last one need not be full
-      const int64_t even = (total * a.c.H + a.wanted - 1) / a.wanted, least = max(a.least, (longest + kMaxPieces - 1) / kMaxPieces);
-      chunk = (int)((max(even, least) + 3) / 4 * 4);
+      b0 += 64;
+      if (b0 >= a.c.B) break;
+      look(b0);
     }
+    if (a.c.B > 64) look(0);
+    // all pieces together are at most wanted + B H: a sentence's last one need not be full
+    const int64_t even = (total * a.c.H + a.wanted - 1) / a.wanted, least = max(a.least, (longest + kMaxPieces - 1) / kMaxPieces);
+    chunk = (int)((max(even, least) + 3) / 4 * 4);
     int base = 0;
     for (int b0 = 0;;) {
       // at least one piece: it writes the zeros of rows that see nothing
@@ -67,7 +75,6 @@ struct Piece {
         b = b0 + hit;
         pieces = __builtin_amdgcn_readlane(count, hit);
         before = base + (__builtin_amdgcn_readlane(upto, hit) - pieces) * a.c.H;
-        steps = __builtin_amdgcn_readlane(mine, hit);
         s = Sentence{__builtin_amdgcn_readlane(own.first, hit), __builtin_amdgcn_readlane(own.rows, hit),
                      __builtin_amdgcn_readlane(own.len, hit), __builtin_amdgcn_readlane(own.slot, hit)};
         return;
