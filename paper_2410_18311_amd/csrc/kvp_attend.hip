@@ -46,7 +46,12 @@ AttendPlan attend_plan(const ci_kvp& c, int64_t T, int64_t G, int64_t max_rows, 
     // two 202, three 190, six 182); no piece below three steps a wave (4096 slots of 40 heads 20.5 us, two 22.7).
     const int64_t wanted = 4 * kCus;
     p.least = 12;
-    p.wanted = heads * tiles * 2 > wanted || steps <= p.least ? 0 : (int)(wanted / tiles);
+    // A head's slots stay together where they are few, or few for so many heads (whole and in pieces: 8 heads over 500 slots 11.0 and 14.5 us, over
+    // 2000 22 and 14.5; 256 heads over 2000 48.7 and 55.7, over 12000 of one sentence and 300 of the others 111 and 24.5; 2400 heads over 4000 of one and
+    // 300 of the others 89 and 125), where there would be more pieces than partial results are worth, and in fp32 prompts, whose tiles see only part
+    // of the slots each.
+    const bool whole = steps <= 16 || steps <= std::min<int64_t>(128, heads * tiles / 2) || heads * tiles > (tiles > 4 ? 2 : 16) * kCus;
+    p.wanted = whole ? 0 : (int)(wanted / tiles);
     p.blocks = (int)heads + p.wanted;
     // Beyond 64 workgroups a compute unit one takes several tiles: only the sentences that have so many rows need them.
     p.row_tiles = (int)std::min<int64_t>({tiles, 65535, std::max<int64_t>(1, 64 * kCus / p.blocks)});

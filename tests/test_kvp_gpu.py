@@ -311,6 +311,18 @@ def test_slots_shared_out_over_the_chip(lib, B, dtype):
     _check_attend(lib, lens, [min(n, 1) for n in lens], 2, 1, 64, 16, dtype, 200, 5, seed=B + 1)
 
 
+@pytest.mark.parametrize("dtype", [F16, F32])
+@pytest.mark.parametrize("B", [65, 200])
+def test_one_long_sentence_among_many(lib, B, dtype):
+    """Pieces whose sentence is looked for in several rounds."""
+    rng = np.random.default_rng(B)
+    lens = [int(n) for n in rng.integers(0, 90, B)]
+    lens[B - 3], lens[3] = 5000, 1500
+    rows = [min(n, 1 + b % 2) for b, n in enumerate(lens)]
+    _check_attend(lib, lens, rows, 1, 2, 64, 32, dtype, seed=B + 30)
+    _check_attend(lib, lens, rows, 1, 1, 128, 16, dtype, 4500, 5, seed=B + 31)
+
+
 def test_a_long_context(lib):
     for dtype in (F16, BF16):
         _check_attend(lib, [16000, 3000], [1, 2], 1, 2, 128, 64, dtype, seed=1, qstd=2.0)
