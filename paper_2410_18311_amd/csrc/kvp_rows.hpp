@@ -1,6 +1,6 @@
 // Attention of few rows of a head over a cache in pages (kvp_attend.hpp), one token a sentence above all: bound by the cache's bytes.
 //
-// The slots of all sentences are shared out by length over four workgroups a compute unit, whose waves take every fourth step of 32 slots, each with
+// The slots of all sentences are shared out by length over four workgroups a compute unit (or a head's stay together), whose waves take every fourth step of 32 slots, each with
 // its own running maximum; a second launch joins the pieces.  A wave reads keys and values as they lie, 16 bytes a lane, a step
 // ahead, without the LDS, which would only add a wait: nobody else of the workgroup reads them.  A lane's channels of eight slots are
 // turned into operands of one channel by one permutation a word.  Logits and sums are fp32; probabilities enter the product as two 16-bit

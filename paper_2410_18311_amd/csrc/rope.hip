@@ -9,8 +9,8 @@
 // Its nearest quarter turn is taken off as bits; what is left, at most an eighth of a turn, goes through the Taylor series, whose
 // first terms left out are below 2^-28.
 //
-// 4096 tokens of 40 heads of 128, bf16: 16.5 to 18 us for 84 MB, 5.1 TB/s, the rate of a large copy; 3584 tokens of 96 heads to pages 39.5 us for 176 MB.
-// One token: 2.4 us of the kernel, 4.7 with the search for its sentence and page, the rest of a call's 5 to 7 us its launch.
+// 4096 tokens of 40 heads of 128, bf16: 16.2 to 18 us for 84 MB, 4.7 to 5.2 TB/s, the rate of a large copy; 3584 tokens of 96 heads to pages 39.5 us for 176 MB.
+// One token: 2.5 us of the kernel, 4.9 with the search for its sentence and page, the rest of a call's 5 to 7 us its launch.
 #include <algorithm>
 
 #include "kvp.hpp"
