@@ -187,8 +187,9 @@ __device__ __forceinline__ void careful_row(const KvpAttend& a, const Sentence& 
     __syncthreads();
     for (int w = 0; w < THREADS / 64; ++w) top = fmaxf(top, lds[THREADS + w]);
     const float next = fmaxf(m, top), ref = next == -INFINITY ? 0.0f : next;
-    // seen, but too small for fp32: not nothing, as it is multiplied by what may be infinite
-    lds[tid] = z == -INFINITY ? 0.0f : z != z ? z : fmaxf(__builtin_amdgcn_exp2f(z - ref), 1e-37f);
+    // seen, but too small for fp32: not nothing, as it is multiplied by what may be infinite; NaN for z = ref = infinity, which fmaxf would drop
+    const float weight = __builtin_amdgcn_exp2f(z - ref);
+    lds[tid] = z == -INFINITY ? 0.0f : weight != weight ? weight : fmaxf(weight, 1e-37f);
     __syncthreads();
     const float was = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - ref);
     m = next;

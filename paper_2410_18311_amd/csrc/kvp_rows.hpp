@@ -319,7 +319,8 @@ __device__ __forceinline__ void rows_block(const KvpAttend& a, int block, int ti
         total += ml[0][w][r] == -INFINITY ? ml[1][w][r] : ml[1][w][r] * __builtin_amdgcn_exp2f(ml[0][w][r] - t);
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[i] = (sums[0][r][d + i] + sums[1][r][d + i]) + (sums[2][r][d + i] + sums[3][r][d + i]);
-      if (!(finite(v[0]) && finite(v[1]) && finite(v[2]) && finite(v[3]))) atomicOr(&lds.broken, 1u << r);
+      // a logit of +infinity or NaN makes the row's sum NaN, and with it the row: nothing of it is to be done again
+      if (total == total && !(finite(v[0]) && finite(v[1]) && finite(v[2]) && finite(v[3]))) atomicOr(&lds.broken, 1u << r);
       if (a.wanted) {
         *reinterpret_cast<float4*>(a.o + (part + r) * D + d) = make_float4(v[0], v[1], v[2], v[3]);
         if (d == 0) {

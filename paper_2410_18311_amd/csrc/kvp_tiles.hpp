@@ -321,7 +321,7 @@ __device__ __forceinline__ void tile_block(const KvpAttend& a, int block, int pi
   for (int c = 0; c < CB; ++c)
 #pragma unroll
     for (int e = 0; e < 16; ++e) whole = whole && finite(acc[c][e]);
-  const uint64_t bad = __ballot(!whole);
+  const uint64_t bad = __ballot(!whole && l == l);   // a logit of +infinity or NaN makes l NaN, and with it the row
   const bool valid = live && mine0 + n < R;
   const size_t part = ((size_t)block * a.pieces + piece) * BM + 32 * wave;
   if (valid && g == 0) {

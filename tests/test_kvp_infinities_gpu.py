@@ -1,0 +1,59 @@
+"""Attention over pages where what a row sees is infinite or NaN: what the definition in 64 bits gives, however the call is split."""
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import pages_oracle as orc
+from tests._util import f64
+from tests.test_kvp_gpu import BF16, DEV, F16, F32, _bound, _cache, _fill, _first, _ints, _rand
+
+pytestmark = pytest.mark.gpu
+
+
+def _run(lib, cache, q, lens, rows, window=0, sinks=0, scale=None):
+    lse = torch.full(q.shape[:2], 5.0, dtype=F32, device=DEV)
+    out = lib.kvp_attend(q, cache, _ints(*_first(rows)), _ints(*lens), max_rows=max(rows), max_len=max(lens), window=window, sinks=sinks,
+                         scale=scale, lse=lse)
+    return f64(out), f64(lse)
+
+
+def _check(lib, cache, table, q, lens, rows, window=0, sinks=0):
+    """Against the definition: NaN where it is NaN, the same infinities, and the other results within the usual bounds, whose logits' size is
+    that of the finite factors.  Slots outside the sentences are NaN in the cache and not seen."""
+    got, got_lse = _run(lib, cache, q, lens, rows, window, sinks)
+    first, D, scale = _first(rows), cache.D, cache.D ** -0.5
+    qq, k, v = f64(q), f64(cache.k), f64(cache.v)
+    cut = lambda x: np.where(np.isfinite(x), x, 0.0)  # noqa: E731
+    with np.errstate(all="ignore"):
+        want, want_lse, _, _ = orc.attend(qq, k, v, table, first, lens, window, sinks, scale)
+        _, _, size, reach = orc.attend(cut(qq), cut(k), cut(v), table, first, lens, window, sinks, scale)
+    assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(np.isnan(got_lse), np.isnan(want_lse))
+    ok = np.isfinite(want)
+    assert np.array_equal(np.where(ok | np.isnan(want), 0.0, got), np.where(ok | np.isnan(want), 0.0, want))   # infinities
+    size = np.maximum(size, np.abs(cut(v)).max())      # weights are not those of the cut logits
+    bound = _bound(cache.dtype, cut(want), size, reach, D, max(lens), max(rows) * (q.shape[1] // cache.H))
+    assert np.all(np.abs(got - want)[ok] <= bound[ok])
+    return want, want_lse
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("n,rows", [(60, 1), (256, 1), (300, 1), (513, 1), (3000, 1), (60, 60), (200, 130), (300, 300), (1500, 70)])
+@pytest.mark.parametrize("what", ["first", "last", "query"])
+def test_an_infinite_key_or_query(lib, n, rows, what, dtype):
+    """Products of both signs: a logit of +infinity makes its row NaN, one of -infinity takes its slot's weight only."""
+    H, G, D, page = 1, 2, 64, 16
+    cache, table = _cache(lib, H, page, D, dtype, [n], 1)
+    _fill(cache, table, [n], 2)
+    q = _rand((rows, G, D), dtype, 3)
+    q[:, 0, 3], q[:, 1, 3] = 1.0, -1.0
+    if what == "query":
+        q[rows // 2, 0, 5] = math.inf
+        q[rows - 1, 1, 5] = -math.inf
+    else:
+        slot = 1 if what == "first" else n - 1
+        cache.k[table[0][slot // page], 0, slot % page, 3] = math.inf
+    want, _ = _check(lib, cache, table, q, [n], [rows])
+    assert np.isnan(want).any() and (what == "query" and rows == 1 or np.isfinite(want).any())
