@@ -83,6 +83,9 @@ template <class E> constexpr float kBelow = __is_same(E, F16) ? 7.0f : 0.0f;
 template <class E> constexpr float kRaise = kBelow<E> + 8.0f;
 
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }   // false for NaN
+// The factor of a sum of weighted values that brings it to another maximum.  Weights are above 0, however small next to others: where fp32 has 0 for
+// the factor, an infinite sum stays infinite.
+__device__ __forceinline__ float factor_of(float sum, float factor) { return factor == 0.0f && !finite(sum) ? 1.0f : factor; }
 
 // A sentence's rows: they begin at packed row `first`, `rows` of them are this call's, the first in slot `slot` (negative: ahead of the
 // first slot, where it sees nothing).
@@ -194,7 +197,7 @@ __device__ __forceinline__ void careful_row(const KvpAttend& a, const Sentence& 
     const float was = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - ref);
     m = next;
     l *= was;
-    o *= was;
+    o *= factor_of(o, was);
     for (int e = 0; e < THREADS && from + e < slots; ++e) {
       const float w = lds[e];
       if (w == 0.0f) continue;

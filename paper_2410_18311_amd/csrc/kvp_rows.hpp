@@ -396,7 +396,7 @@ __device__ __forceinline__ void join_rows(const KvpAttend& a, int64_t block, int
       if (wave + 4 * n >= place.y) continue;
       const float f = __shfl(factor, wave + 4 * n, kWave);
 #pragma unroll
-      for (int c = 0; c < C; ++c) sum[c] += f == 0.0f ? 0.0f : f * o[n][c];
+      for (int c = 0; c < C; ++c) sum[c] = __builtin_fmaf(o[n][c], factor_of(o[n][c], f), sum[c]);
     }
 #pragma unroll
     for (int c = 0; c < C; ++c) sums[wave][lane * C + c] = sum[c];

@@ -433,20 +433,20 @@ __device__ __forceinline__ void join_tiles(const KvpAttend& a, int64_t first, in
       for (int i = 0; i < N; ++i) next = fmaxf(next, m[i]);
       const float was = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top - next);
       top = next;
-      if (total != 0.0f) total *= was;   // a NaN that came without a maximum stays
+      total *= was;   // a NaN that came without a maximum stays
       exact *= was;
 #pragma unroll
-      for (int c = 0; c < 8; ++c) sum[c] = was == 0.0f ? (total != total ? NAN : 0.0f) : sum[c] * was;
+      for (int c = 0; c < 8; ++c) sum[c] *= factor_of(sum[c], was);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
+        if (i0 + i >= a.pieces) break;
         // a piece without a maximum saw nothing, or nothing but NaN
         const float f = m[i] == -INFINITY ? (l[i] != 0.0f ? NAN : 0.0f) : __builtin_amdgcn_exp2f(m[i] - top);
-        if (f == 0.0f) continue;
         total = __builtin_fmaf(l[i], f, total);
         exact = __builtin_fmaf(x[i], f, exact);
         const float v[8] = {o[i][0].x, o[i][0].y, o[i][0].z, o[i][0].w, o[i][1].x, o[i][1].y, o[i][1].z, o[i][1].w};
 #pragma unroll
-        for (int c = 0; c < 8; ++c) sum[c] = __builtin_fmaf(v[c], f, sum[c]);
+        for (int c = 0; c < 8; ++c) sum[c] = __builtin_fmaf(v[c], factor_of(v[c], f), sum[c]);
       }
     }
     const float inverse = total == 0.0f ? 0.0f : 1.0f / total;

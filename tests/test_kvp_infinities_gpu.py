@@ -57,3 +57,34 @@ def test_an_infinite_key_or_query(lib, n, rows, what, dtype):
         cache.k[table[0][slot // page], 0, slot % page, 3] = math.inf
     want, _ = _check(lib, cache, table, q, [n], [rows])
     assert np.isnan(want).any() and (what == "query" and rows == 1 or np.isfinite(want).any())
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("n,rows", [(4000, 1), (4000, 100), (300, 1), (300, 100), (700, 66)])
+@pytest.mark.parametrize("low_first", [True, False])
+def test_an_infinite_value_of_next_to_no_weight(lib, n, rows, low_first, dtype):
+    """Seen at 2^-216 of the largest weight, in another piece of its row, in another round, or in the same one: it is not finite all the same."""
+    D, page, low = 64, 16, -150.0
+    cache, table = _cache(lib, 1, page, D, dtype, [n], 1)
+    _fill(cache, table, [n], 2)
+    half, slot = n // 2 - 60, 10
+    for t in range(n):
+        cache.k[table[0][t // page], 0, t % page] = 0.0
+        cache.k[table[0][t // page], 0, t % page, 0] = low if (t < half) == low_first else 0.0
+    if not low_first:
+        slot = n - rows - 5
+    q = torch.zeros((rows, 1, D), dtype=dtype, device=DEV)
+    q[..., 0] = 1.0
+    clean, clean_lse = _run(lib, cache, q, [n], [rows], scale=1.0)
+    at = cache.v[table[0][slot // page], 0, slot % page]
+    for channel, x in ((7, math.inf), (9, -math.inf), (11, math.nan)):
+        at[channel] = x
+    got, got_lse = _run(lib, cache, q, [n], [rows], scale=1.0)
+    assert np.all(got[..., 7] == math.inf) and np.all(got[..., 9] == -math.inf) and np.isnan(got[..., 11]).all()
+    rest = np.delete(np.arange(D), [7, 9, 11])
+    # both ways have the bounds of a clean call: every logit is 0 or `low`, so a row is off by its weights' rounding (half a unit of the largest value
+    # each, and none of `low` counts) and fp32 sums, and by the result's rounding
+    bound = _bound(dtype, clean[..., rest], np.full(clean[..., rest].shape, np.abs(f64(cache.v)[np.isfinite(f64(cache.v))]).max()),
+                   np.zeros((rows, 1)), D, n, rows)
+    assert np.all(np.abs(got[..., rest] - clean[..., rest]) <= 2.0 * bound)
+    assert np.all(np.abs(got_lse - clean_lse) <= 2.0 ** -24 * (32.0 + n / 4.0 + 4.0 * np.abs(clean_lse)))
