@@ -705,7 +705,8 @@ int coreinfer_kvp_append(const ci_kvp* cache, const void* k, const void* v, cons
  *     out[r, i] = sum_t p_t v_t,   p = softmax over t of scale (q . k_t).
  * The row in slot p sees the slots t <= p; with window > 0 of those only t > p - window
  * and t < sinks.  A row that sees none gives zeros.  What it does not see, infinities and NaN
- * included, does not touch it.  A logit of +infinity or NaN that it sees gives NaN, in lse too.
+ * included, does not touch it.  A logit of +infinity or NaN that it sees gives NaN, in lse too;
+ * where all that it sees are -infinity, it gives NaN, and lse -infinity.
  *   max_rows  the most rows of a sentence, max_len the most slots (<= most * page): they choose
  *             and size the launches.  lens beyond 0 .. max_len are taken as its ends; rows
  *             of a sentence from max_rows on are left as they are.

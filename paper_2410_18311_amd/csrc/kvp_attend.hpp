@@ -134,6 +134,22 @@ struct Pages {
     return (uint32_t)n < a.c.pages ? n : -1;   // pages below 2^31
   }
 };
+// What a row in slot p gives that has no weights: 0 if it sees no slot, as none of its pages is one, else NaN, its logits being all -infinity.
+__device__ __forceinline__ float without_weights(const KvpAttend& a, const Pages& pages, int p) {
+  const int low = a.window ? max(0, p - a.window + 1) : 0;
+  bool any = false;
+  auto look = [&](int from, int to) {   // pages from .. to, eight requests at once
+    for (int n = from; n <= to && !any; n += 8)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) any |= (uint32_t)pages.table[min(n + j, to)] < a.c.pages;
+  };
+  if (p >= 0) {
+    look(low >> a.c.shift, p >> a.c.shift);
+    look(0, (min(a.sinks, low) - 1) >> a.c.shift);
+  }
+  return any ? NAN : 0.0f;
+}
+
 // Elements from the pages' start to the first slot of a head in a page; page -1: of page 0, whatever lies there.
 template <int D>
 __device__ __forceinline__ int64_t page_start(const KvpAttend& a, int page, int h) {
@@ -149,7 +165,8 @@ __device__ __forceinline__ void store_row4(const KvpAttend& a, int D, int64_t at
     *reinterpret_cast<uint2*>(dst) = make_uint2(pair_of<E>(v[0], v[1]), pair_of<E>(v[2], v[3]));
 }
 __device__ __forceinline__ void store_lse(const KvpAttend& a, int64_t at, float m, float l) {
-  if (a.lse) a.lse[at] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+  // a maximum of infinity beside no weights is a logit beyond fp32
+  if (a.lse) a.lse[at] = l == 0.0f && m != INFINITY ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
 }
 // Workgroups for that many pieces of work; beyond, one takes several.
 inline unsigned join_blocks(int64_t n) { return (unsigned)(n < 262144 ? n : 262144); }
@@ -174,9 +191,11 @@ __device__ __forceinline__ void careful_row(const KvpAttend& a, const Sentence& 
   auto slot_of = [&](int n) { return steps.slot(begin + n / STEP) + n % STEP; };
   for (int from = 0; from < slots; from += THREADS) {
     float z = -INFINITY;
+    bool seen = false;
     if (from + tid < slots) {
       const int t = slot_of(from + tid), page = t < s.len ? pages.of(a, t) : -1;
-      if (page >= 0 && sees(a, p, t)) {
+      seen = page >= 0 && sees(a, p, t);
+      if (seen) {
         const T* k = reinterpret_cast<const T*>(a.c.k) + page_start<D>(a, page, h) + (t & inside) * D;
         float sum = 0.0f;
         for (int d = 0; d < D; ++d) sum = __builtin_fmaf(to_float<E>(k[d]), to_float<E>(q[d]), sum);
@@ -190,9 +209,10 @@ __device__ __forceinline__ void careful_row(const KvpAttend& a, const Sentence& 
     __syncthreads();
     for (int w = 0; w < THREADS / 64; ++w) top = fmaxf(top, lds[THREADS + w]);
     const float next = fmaxf(m, top), ref = next == -INFINITY ? 0.0f : next;
-    // seen, but too small for fp32: not nothing, as it is multiplied by what may be infinite; NaN for z = ref = infinity, which fmaxf would drop
+    // Below 0: not seen.  Seen, but too small for fp32: not nothing, as it is multiplied by what may be infinite; that by 0 is NaN.  NaN for
+    // z = ref = infinity, which fmaxf would drop.
     const float weight = __builtin_amdgcn_exp2f(z - ref);
-    lds[tid] = z == -INFINITY ? 0.0f : weight != weight ? weight : fmaxf(weight, 1e-37f);
+    lds[tid] = !seen ? -1.0f : z == -INFINITY ? 0.0f : weight != weight ? weight : fmaxf(weight, 1e-37f);
     __syncthreads();
     const float was = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - ref);
     m = next;
@@ -200,7 +220,7 @@ __device__ __forceinline__ void careful_row(const KvpAttend& a, const Sentence& 
     o *= factor_of(o, was);
     for (int e = 0; e < THREADS && from + e < slots; ++e) {
       const float w = lds[e];
-      if (w == 0.0f) continue;
+      if (w < 0.0f) continue;
       l += w;
       if (tid < D) {
         const int t = slot_of(from + e);

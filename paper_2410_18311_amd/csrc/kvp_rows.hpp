@@ -328,7 +328,7 @@ __device__ __forceinline__ void rows_block(const KvpAttend& a, int block, int ti
           a.l[part + r] = total;
         }
       } else {
-        const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
+        const float inverse = total == 0.0f ? without_weights(a, pages, s.slot + (row0 + r) / a.G) : 1.0f / total;
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] *= inverse;
         const int64_t at = out_row(a, s, h, row0 + r);
@@ -350,7 +350,7 @@ __device__ __forceinline__ void rows_block(const KvpAttend& a, int block, int ti
         }
       } else {
         const int64_t at = out_row(a, s, h, row0 + r);
-        if (threadIdx.x < D) reinterpret_cast<typename E::T*>(a.out)[at * D + threadIdx.x] = from_float<E>(lr == 0.0f ? 0.0f : o / lr);
+        if (threadIdx.x < D) reinterpret_cast<typename E::T*>(a.out)[at * D + threadIdx.x] = from_float<E>(lr == 0.0f ? without_weights(a, pages, s.slot + (row0 + r) / a.G) : o / lr);
         if (threadIdx.x == 0) store_lse(a, at, mr, lr);
       }
     }
@@ -404,7 +404,7 @@ __device__ __forceinline__ void join_rows(const KvpAttend& a, int64_t block, int
     if (threadIdx.x < D) {
       const int d = threadIdx.x;
       const float v = (sums[0][d] + sums[1][d]) + (sums[2][d] + sums[3][d]);
-      reinterpret_cast<typename E::T*>(a.out)[at * D + d] = from_float<E>(total == 0.0f ? 0.0f : v * (1.0f / total));
+      reinterpret_cast<typename E::T*>(a.out)[at * D + d] = from_float<E>(total == 0.0f ? without_weights(a, Pages(a, b, s.len), s.slot + i) : v * (1.0f / total));
       if (d == 0) store_lse(a, at, top, total);
     }
     __syncthreads();

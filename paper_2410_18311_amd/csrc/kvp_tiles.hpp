@@ -338,7 +338,7 @@ __device__ __forceinline__ void tile_block(const KvpAttend& a, int block, int pi
   meet();
   constexpr int PITCH = 32 * 4 + 16;   // of a row; 32 rows of four waves are below the buffers' size
   unsigned char* mine = smem + wave * 32 * PITCH;
-  const float inverse = a.pieces > 1 ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
+  const float inverse = a.pieces > 1 ? 1.0f : l == 0.0f ? without_weights(a, pages, p) : 1.0f / l;
   if (a.pieces > 1) {
 #pragma unroll
     for (int c = 0; c < CB; ++c) {
@@ -390,7 +390,7 @@ __device__ __forceinline__ void tile_block(const KvpAttend& a, int block, int pi
         }
       } else {
         const int64_t at = out_row(a, s, h, r);
-        if (threadIdx.x < D) reinterpret_cast<typename E::T*>(a.out)[at * D + threadIdx.x] = from_float<E>(lr == 0.0f ? 0.0f : o / lr);
+        if (threadIdx.x < D) reinterpret_cast<typename E::T*>(a.out)[at * D + threadIdx.x] = from_float<E>(lr == 0.0f ? without_weights(a, pages, s.slot + r / a.G) : o / lr);
         if (threadIdx.x == 0) store_lse(a, at, mr, lr);
       }
     }
@@ -449,7 +449,7 @@ __device__ __forceinline__ void join_tiles(const KvpAttend& a, int64_t first, in
         for (int c = 0; c < 8; ++c) sum[c] = __builtin_fmaf(v[c], factor_of(v[c], f), sum[c]);
       }
     }
-    const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
+    const float inverse = total == 0.0f ? without_weights(a, Pages(a, b, s.len), s.slot + (int)row / a.G) : 1.0f / total;
     const int64_t at = out_row(a, s, h, (int)row);
     *reinterpret_cast<uint4*>(reinterpret_cast<typename E::T*>(a.out) + at * D + 8 * lane) =
         make_uint4(pair_of<E>(sum[0] * inverse, sum[1] * inverse), pair_of<E>(sum[2] * inverse, sum[3] * inverse),

@@ -88,3 +88,41 @@ def test_an_infinite_value_of_next_to_no_weight(lib, n, rows, low_first, dtype):
                    np.zeros((rows, 1)), D, n, rows)
     assert np.all(np.abs(got[..., rest] - clean[..., rest]) <= 2.0 * bound)
     assert np.all(np.abs(got_lse - clean_lse) <= 2.0 ** -24 * (32.0 + n / 4.0 + 4.0 * np.abs(clean_lse)))
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("n,rows", [(1, 1), (60, 1), (300, 1), (4000, 1), (60, 60), (300, 300), (4000, 80)])
+def test_rows_whose_logits_are_all_minus_infinity(lib, n, rows, dtype):
+    """0 / 0, and not the zeros of a row that sees nothing; the logarithm of their sum is that of 0."""
+    D, page = 64, 16
+    lens = [n, rows - 1]
+    cache, table = _cache(lib, 1, page, D, dtype, lens, 1)
+    _fill(cache, table, lens, 2)
+    cache.k[..., 3] = math.inf
+    q = _rand((2 * rows, 1, D), dtype, 3)
+    q[..., 3] = -1.0
+    if rows > 1:
+        q[1, 0, 3] = 1.0       # this one has logits of +infinity
+    got, got_lse = _run(lib, cache, q, lens, [rows, rows])
+    assert np.isnan(got[:rows]).all()
+    assert np.isneginf(np.delete(got_lse[:rows], 1 if rows > 1 else [])).all() and (rows == 1 or math.isnan(got_lse[1, 0]))
+    # the second sentence's first row is ahead of its first slot
+    assert np.all(got[rows] == 0.0) and math.isinf(got_lse[rows, 0]) and np.isnan(got[rows + 1:]).all()
+    # a page that is none is not seen, whatever its number would have held
+    cache.table.fill_(-1)
+    got, got_lse = _run(lib, cache, q, lens, [rows, rows])
+    assert np.all(got == 0.0) and np.isneginf(got_lse).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("n,rows", [(60, 1), (300, 1), (4000, 1), (60, 60), (300, 300)])
+def test_an_infinite_value_behind_a_logit_of_minus_infinity(lib, n, rows, dtype):
+    """0 times infinity."""
+    D, page = 64, 16
+    cache, table = _cache(lib, 1, page, D, dtype, [n], 1)
+    _fill(cache, table, [n], 2)
+    cache.k[table[0][0], 0, 5, 3] = math.inf
+    cache.v[table[0][0], 0, 5, 8] = math.inf
+    q = _rand((rows, 1, D), dtype, 3)
+    q[..., 3] = -1.0
+    _check(lib, cache, table, q, [n], [rows])
