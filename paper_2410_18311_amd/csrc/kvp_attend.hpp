@@ -150,6 +150,8 @@ __device__ __forceinline__ float without_weights(const KvpAttend& a, const Pages
   return any ? NAN : 0.0f;
 }
 
+__device__ __forceinline__ bool rarely(bool x) { return __builtin_expect(x, false); }
+
 // Elements from the pages' start to the first slot of a head in a page; page -1: of page 0, whatever lies there.
 template <int D>
 __device__ __forceinline__ int64_t page_start(const KvpAttend& a, int page, int h) {
@@ -175,64 +177,6 @@ inline unsigned join_blocks(int64_t n) { return (unsigned)(n < 262144 ? n : 2621
 __device__ __forceinline__ int64_t out_row(const KvpAttend& a, const Sentence& s, int h, int r) {
   const int i = r / a.G;
   return ((int64_t)s.first + i) * a.c.H * a.G + h * a.G + (r - i * a.G);
-}
-
-// One row over steps begin .. end - 1 by a whole workgroup, slot by slot, without the slots that it does not see: what the matrix cores cannot leave
-// out when a value that a row does not see is infinite or NaN, because they multiply it by 0.  o: of the D threads that have a channel each.
-// lds: THREADS + 16 floats.
-template <class E, int D, int STEP, int THREADS>
-__device__ __forceinline__ void careful_row(const KvpAttend& a, const Sentence& s, const Pages& pages, int h, int r, const Steps<STEP>& steps,
-                                            int begin, int end, float* lds, float* m_out, float* l_out, float* o_out) {
-  using T = typename E::T;
-  const int tid = threadIdx.x, i = r / a.G, p = s.slot + i, inside = (1 << a.c.shift) - 1;
-  const T* q = reinterpret_cast<const T*>(a.q) + (int64_t)(s.first + i) * a.q_t + (int64_t)(h * a.G + r - i * a.G) * a.q_h;
-  float m = -INFINITY, l = 0.0f, o = 0.0f;
-  const int slots = (end - begin) * STEP;   // below 2^25
-  auto slot_of = [&](int n) { return steps.slot(begin + n / STEP) + n % STEP; };
-  for (int from = 0; from < slots; from += THREADS) {
-    float z = -INFINITY;
-    bool seen = false;
-    if (from + tid < slots) {
-      const int t = slot_of(from + tid), page = t < s.len ? pages.of(a, t) : -1;
-      seen = page >= 0 && sees(a, p, t);
-      if (seen) {
-        const T* k = reinterpret_cast<const T*>(a.c.k) + page_start<D>(a, page, h) + (t & inside) * D;
-        float sum = 0.0f;
-        for (int d = 0; d < D; ++d) sum = __builtin_fmaf(to_float<E>(k[d]), to_float<E>(q[d]), sum);
-        z = sum * a.scale;
-      }
-    }
-    float top = z != z ? INFINITY : z;   // a NaN makes everything NaN
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, kWave));
-    if ((tid & 63) == 0) lds[THREADS + (tid >> 6)] = top;
-    __syncthreads();
-    for (int w = 0; w < THREADS / 64; ++w) top = fmaxf(top, lds[THREADS + w]);
-    const float next = fmaxf(m, top), ref = next == -INFINITY ? 0.0f : next;
-    // Below 0: not seen.  Seen, but too small for fp32: not nothing, as it is multiplied by what may be infinite; that by 0 is NaN.  NaN for
-    // z = ref = infinity, which fmaxf would drop.
-    const float weight = __builtin_amdgcn_exp2f(z - ref);
-    lds[tid] = !seen ? -1.0f : z == -INFINITY ? 0.0f : weight != weight ? weight : fmaxf(weight, 1e-37f);
-    __syncthreads();
-    const float was = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - ref);
-    m = next;
-    l *= was;
-    o *= factor_of(o, was);
-    for (int e = 0; e < THREADS && from + e < slots; ++e) {
-      const float w = lds[e];
-      if (w < 0.0f) continue;
-      l += w;
-      if (tid < D) {
-        const int t = slot_of(from + e);
-        const T* v = reinterpret_cast<const T*>(a.c.v) + page_start<D>(a, pages.of(a, t), h) + (t & inside) * D;
-        o += w * to_float<E>(v[tid]);
-      }
-    }
-    __syncthreads();
-  }
-  *m_out = m;
-  *l_out = l;
-  *o_out = o;
 }
 
 }  // namespace

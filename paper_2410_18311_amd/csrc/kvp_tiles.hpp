@@ -17,7 +17,7 @@
 #pragma once
 
 #include "gemm_tile.hpp"
-#include "kvp_attend.hpp"
+#include "kvp_walk.hpp"
 
 namespace ci {
 namespace {
@@ -338,7 +338,7 @@ __device__ __forceinline__ void tile_block(const KvpAttend& a, int block, int pi
   meet();
   constexpr int PITCH = 32 * 4 + 16;   // of a row; 32 rows of four waves are below the buffers' size
   unsigned char* mine = smem + wave * 32 * PITCH;
-  const float inverse = a.pieces > 1 ? 1.0f : l == 0.0f ? without_weights(a, pages, p) : 1.0f / l;
+  const float inverse = a.pieces > 1 ? 1.0f : rarely(l == 0.0f) ? without_weights(a, pages, p) : 1.0f / l;
   if (a.pieces > 1) {
 #pragma unroll
     for (int c = 0; c < CB; ++c) {
@@ -373,27 +373,32 @@ __device__ __forceinline__ void tile_block(const KvpAttend& a, int block, int pi
   }
   if (lane == 0) broken[wave] = (unsigned)bad | (unsigned)(bad >> 32);
   __syncthreads();
-  for (int w = 0; w < WAVES; ++w) {
-    // an infinity or a NaN among the values, seen or not
-    for (unsigned left = broken[w]; left; left &= left - 1) {
-      const int r = row0 + 32 * w + __builtin_ctz(left);
-      if (r >= R) break;
-      float mr, lr, o;
-      careful_row<E, D, kTileStep, 64 * WAVES>(a, s, pages, h, r, steps, begin, end, reinterpret_cast<float*>(smem), &mr, &lr, &o);
-      if (a.pieces > 1) {
-        const size_t to = ((size_t)block * a.pieces + piece) * BM + r - row0;
-        if (threadIdx.x < D) a.tile_o[to * D + threadIdx.x] = o;
-        if (threadIdx.x == 0) {
-          a.tile_m[to] = mr;
-          a.tile_l[to] = lr;
-          if (LSE) a.tile_exact[to] = lr;
-        }
-      } else {
-        const int64_t at = out_row(a, s, h, r);
-        if (threadIdx.x < D) reinterpret_cast<typename E::T*>(a.out)[at * D + threadIdx.x] = from_float<E>(lr == 0.0f ? without_weights(a, pages, s.slot + r / a.G) : o / lr);
-        if (threadIdx.x == 0) store_lse(a, at, mr, lr);
-      }
-    }
+  // an infinity or a NaN among the values, seen or not
+  static_assert(WAVES == 4 && sizeof(RowsLds<D>) <= 4 * HALF);
+  for (int w = 0; w < 2 * WAVES; ++w) {
+    const int first = row0 + 16 * w;
+    const unsigned only = __builtin_amdgcn_readfirstlane(broken[w / 2] >> (16 * (w % 2))) & 0xffffu;
+    if (!rarely(only != 0) || first >= R) continue;
+    sixteen_rows<E, D, true>(
+        a, s, pages, h, first, R, [&](int step) { return steps.slot(step / 2) + 32 * (step % 2); }, 2 * begin, 2 * end, only,
+        *reinterpret_cast<RowsLds<D>*>(smem), [&](int r, int d, float mr, float lr, float (&v)[4]) {
+          if (a.pieces > 1) {
+            const size_t to = ((size_t)block * a.pieces + piece) * BM + 16 * w + r;
+            *reinterpret_cast<float4*>(a.tile_o + to * D + d) = make_float4(v[0], v[1], v[2], v[3]);
+            if (d == 0) {
+              a.tile_m[to] = mr;
+              a.tile_l[to] = lr;
+              if (LSE) a.tile_exact[to] = lr;
+            }
+          } else {
+            const float inverse = lr == 0.0f ? without_weights(a, pages, s.slot + (first + r) / a.G) : 1.0f / lr;
+            const int64_t at = out_row(a, s, h, first + r);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] *= inverse;
+            store_row4<E>(a, D, at, d, v);
+            if (d == 0) store_lse(a, at, mr, lr);
+          }
+        });
   }
 }
 
@@ -439,22 +444,28 @@ __device__ __forceinline__ void join_tiles(const KvpAttend& a, int64_t first, in
       for (int c = 0; c < 8; ++c) sum[c] *= factor_of(sum[c], was);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        if (i0 + i >= a.pieces) break;
         // a piece without a maximum saw nothing, or nothing but NaN
         const float f = m[i] == -INFINITY ? (l[i] != 0.0f ? NAN : 0.0f) : __builtin_amdgcn_exp2f(m[i] - top);
+        const float v[8] = {o[i][0].x, o[i][0].y, o[i][0].z, o[i][0].w, o[i][1].x, o[i][1].y, o[i][1].z, o[i][1].w};
+        if (f == 0.0f) {   // only what is not finite counts
+          if (i0 + i >= a.pieces) continue;
+          total += l[i] * 0.0f;
+#pragma unroll
+          for (int c = 0; c < 8; ++c) sum[c] += finite(v[c]) ? 0.0f : v[c];
+          continue;
+        }
         total = __builtin_fmaf(l[i], f, total);
         exact = __builtin_fmaf(x[i], f, exact);
-        const float v[8] = {o[i][0].x, o[i][0].y, o[i][0].z, o[i][0].w, o[i][1].x, o[i][1].y, o[i][1].z, o[i][1].w};
 #pragma unroll
-        for (int c = 0; c < 8; ++c) sum[c] = __builtin_fmaf(v[c], factor_of(v[c], f), sum[c]);
+        for (int c = 0; c < 8; ++c) sum[c] = __builtin_fmaf(v[c], f, sum[c]);
       }
     }
-    const float inverse = total == 0.0f ? without_weights(a, Pages(a, b, s.len), s.slot + (int)row / a.G) : 1.0f / total;
+    const float inverse = rarely(total == 0.0f) ? without_weights(a, Pages(a, b, s.len), s.slot + (int)row / a.G) : 1.0f / total;
     const int64_t at = out_row(a, s, h, (int)row);
     *reinterpret_cast<uint4*>(reinterpret_cast<typename E::T*>(a.out) + at * D + 8 * lane) =
         make_uint4(pair_of<E>(sum[0] * inverse, sum[1] * inverse), pair_of<E>(sum[2] * inverse, sum[3] * inverse),
                    pair_of<E>(sum[4] * inverse, sum[5] * inverse), pair_of<E>(sum[6] * inverse, sum[7] * inverse));
-    if (lane == 0) store_lse(a, at, top, exact);
+    if (lane == 0) store_lse(a, at, top, total != total ? total : exact);
   }
 }
 
