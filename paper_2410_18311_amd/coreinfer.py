@@ -927,6 +927,9 @@ def rope_angles(rot: int, base: float = 10000.0, style: str = "half", scaling: s
     return RopeAngles(turns, float(scale), int(rot), style)
 
 
+_HOST = "tensors in host memory, which a kernel would read at the host's addresses"
+
+
 def _check_norm(norm: torch.Tensor, D: int, dtype: torch.dtype, device: int):
     assert norm.shape == (D,) and norm.dtype is dtype and norm.is_contiguous() and norm.get_device() == device
 
@@ -951,6 +954,7 @@ def rope(x: torch.Tensor, pos: Optional[torch.Tensor], angles: Optional[RopeAngl
         _check_pos(pos, T, device)
     if norm is not None:
         _check_norm(norm, D, dtype, device)
+    assert device >= 0, _HOST
     status = _rope_call(x.data_ptr(), s[0], s[1], T, H, D, DTYPE_CODE[dtype], None if norm is None else norm.data_ptr(), eps,
                         None if angles is None else angles.ptr, None if pos is None else pos.data_ptr(), 1 if backward else 0,
                         out.data_ptr(), o[0], o[1], _stream(x))
@@ -1022,6 +1026,7 @@ def kvp_append(cache: KvpCache, k: torch.Tensor, v: torch.Tensor, first: torch.T
         assert q_out is None and q_norm is None
         Hq = q0 = q1 = 0
         q_ptr = q_out_ptr = None
+    assert device >= 0, _HOST
     status = _kvp_append_call(cache.ptr, k.data_ptr(), v.data_ptr(), s[0], s[1], T, first.data_ptr(), lens.data_ptr(),
                               None if pos is None else pos.data_ptr(), None if angles is None else angles.ptr,
                               None if k_norm is None else k_norm.data_ptr(), eps, q_ptr, Hq, q0, q1,
@@ -1058,6 +1063,7 @@ def kvp_attend(q: torch.Tensor, cache: KvpCache, first: torch.Tensor, lens: torc
     assert out.shape == shape and out.dtype is dtype and out.is_contiguous() and out.get_device() == device
     assert lse is None or (lse.shape == (T, Hq) and lse.dtype is torch.float32 and lse.is_contiguous() and lse.get_device() == device)
     assert ws is None or ws.get_device() == device
+    assert device >= 0, _HOST
     if ws is None:
         need = kvp_attend_workspace_size(cache, T, Hq, max_rows, max_len, window, sinks)
         ws = _workspace(need, q) if need else None

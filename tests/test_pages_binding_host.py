@@ -1,0 +1,39 @@
+"""What the Python calls of rotary positions and the cache in pages refuse by themselves, without a GPU.  No call here may reach a launch."""
+
+import pytest
+import torch
+
+F16, F32, I32 = torch.float16, torch.float32, torch.int32
+
+
+def _host(lib, T=4):
+    cache = lib.kvp_cache(8, 3, 16, 64, F16, torch.zeros((2, 4), dtype=I32))
+    x = torch.zeros((T, 3, 64), dtype=F16)
+    return cache, x, torch.zeros(3, dtype=I32), torch.zeros(2, dtype=I32), torch.zeros(T, dtype=I32)
+
+
+@pytest.mark.parametrize("T", [0, 4])
+def test_calls_on_host_memory_are_refused(lib, T):
+    """All of a call's tensors are in host memory: they agree, and a kernel would read the host's addresses."""
+    cache, x, first, lens, pos = _host(lib, T)
+    angles = lib.rope_angles(64, device="cpu")
+    norm = torch.ones(64, dtype=F16)
+    for call in (lambda: lib.rope(x, pos, angles), lambda: lib.rope(x, None, None, norm=norm), lambda: lib.rope(x, pos, angles, out=x),
+                 lambda: lib.kvp_append(cache, x, x, first, lens), lambda: lib.kvp_append(cache, x, x, first, lens, angles, pos, norm, q=x, q_norm=norm),
+                 lambda: lib.kvp_attend(x, cache, first, lens), lambda: lib.kvp_attend(x, cache, first, lens, lse=torch.zeros(T, 3))):
+        with pytest.raises(AssertionError, match="host memory"):
+            call()
+
+
+def test_other_refusals_come_before_that_one(lib):
+    cache, x, first, lens, pos = _host(lib)
+    for bad in (lambda: lib.kvp_append(cache, x, x.float(), first, lens), lambda: lib.kvp_append(cache, x[:, :2], x[:, :2], first, lens),
+                lambda: lib.kvp_append(cache, x, x, lens, lens), lambda: lib.kvp_append(cache, x, x, first, first),
+                lambda: lib.kvp_append(cache, x, x, first.long(), lens), lambda: lib.kvp_append(cache, x, x, first, lens, q_norm=x[0, 0]),
+                lambda: lib.kvp_append(cache, x, x, first, lens, k_norm=x[0]), lambda: lib.kvp_append(cache, x, x, first, lens, pos=first),
+                lambda: lib.kvp_attend(x.float(), cache, first, lens), lambda: lib.kvp_attend(x, cache, first, lens, out=x[:3]),
+                lambda: lib.kvp_attend(x, cache, first, lens, lse=x), lambda: lib.rope(x, first, None),
+                lambda: lib.rope(x, None, None, norm=x[0, 0].float()), lambda: lib.rope(x.transpose(1, 2), None, None)):
+        with pytest.raises(AssertionError) as e:
+            bad()
+        assert "host memory" not in str(e.value)
