@@ -896,9 +896,10 @@ ROPE_SCALING = {"none": 0, "linear": 1, "base": 2, "parts": 3}
 
 
 class RopeAngles:
-    """Frequencies of rotary positions on the device (rope_angles)."""
+    """Frequencies of rotary positions on the device (rope_angles): turns [rot / 2] int64."""
 
     def __init__(self, turns: torch.Tensor, scale: float, rot: int, style: str):
+        assert rot >= 0 and rot % 2 == 0 and turns.shape == (rot // 2,) and turns.dtype is torch.int64 and turns.is_contiguous()
         self.turns, self.scale, self.rot, self.style = turns, scale, rot, style
         self.desc = ci_rope(_ptr(turns), scale, rot, ROPE_STYLE[style])
         self.ptr = ctypes.addressof(self.desc)

@@ -37,3 +37,14 @@ def test_other_refusals_come_before_that_one(lib):
         with pytest.raises(AssertionError) as e:
             bad()
         assert "host memory" not in str(e.value)
+
+
+def test_angles_of_another_size_or_type_are_refused(lib):
+    """A kernel reads rot / 2 of them."""
+    turns = lib.rope_turns(64)
+    lib.RopeAngles(turns, 1.0, 64, "half")
+    lib.RopeAngles(turns[:0], 1.0, 0, "half")
+    for bad, rot in ((turns[:31], 64), (turns, 66), (turns, 62), (turns.int(), 64), (turns.double(), 64), (turns.reshape(1, 32), 64),
+                     (lib.rope_turns(128)[::2], 64), (turns, 65), (turns[:0], -2), (turns[:1].expand(32), 64)):
+        with pytest.raises(AssertionError):
+            lib.RopeAngles(bad, 1.0, rot, "half")
