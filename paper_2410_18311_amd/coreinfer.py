@@ -900,10 +900,12 @@ class RopeAngles:
 
     def __init__(self, turns: torch.Tensor, scale: float, rot: int, style: str):
         assert rot >= 0 and rot % 2 == 0 and turns.shape == (rot // 2,) and turns.dtype is torch.int64 and turns.is_contiguous()
-        self.turns, self.scale, self.rot, self.style = turns, scale, rot, style
+        self._turns, self.scale, self.rot, self.style = turns, scale, rot, style
         self.desc = ci_rope(_ptr(turns), scale, rot, ROPE_STYLE[style])
         self.ptr = ctypes.addressof(self.desc)
         self.device = turns.get_device()
+
+    turns = property(lambda self: self._turns)   # calls go by its address: written to, not replaced
 
 
 def rope_turns(rot: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, original: float = 0.0,
@@ -971,13 +973,16 @@ class KvpCache:
         assert k.dim() == 4 and v.shape == k.shape and v.dtype == k.dtype and k.is_contiguous() and v.is_contiguous()
         assert table.dim() == 2 and table.dtype == torch.int32 and table.is_contiguous()
         assert k.get_device() == v.get_device() == table.get_device()
-        self.k, self.v, self.table, self.dtype = k, v, table, k.dtype
+        self._k, self._v, self._table, self.dtype = k, v, table, k.dtype
         self.pages, self.H, self.page, self.D = k.shape
         self.B, self.most = table.shape
         self.device = k.get_device()
         self._shape, self._first, self._lens = (self.H, self.D), (self.B + 1,), (self.B,)   # what calls are compared with
         self.desc = ci_kvp(_ptr(k), _ptr(v), _ptr(table), self.pages, self.most, self.B, self.H, self.page, self.D, DTYPE_CODE[k.dtype])
         self.ptr = ctypes.addressof(self.desc)
+
+    # calls go by their addresses: written to, not replaced
+    k, v, table = property(lambda self: self._k), property(lambda self: self._v), property(lambda self: self._table)
 
 
 def kvp_cache(pages: int, H: int, page: int, D: int, dtype: torch.dtype, table: torch.Tensor) -> KvpCache:

@@ -48,3 +48,13 @@ def test_angles_of_another_size_or_type_are_refused(lib):
                      (lib.rope_turns(128)[::2], 64), (turns, 65), (turns[:0], -2), (turns[:1].expand(32), 64)):
         with pytest.raises(AssertionError):
             lib.RopeAngles(bad, 1.0, rot, "half")
+
+
+def test_tensors_whose_addresses_calls_go_by_are_not_replaced(lib):
+    cache, angles = _host(lib)[0], lib.rope_angles(64, device="cpu")
+    for owner, name in ((cache, "k"), (cache, "v"), (cache, "table"), (angles, "turns")):
+        was = getattr(owner, name)
+        with pytest.raises(AttributeError):
+            setattr(owner, name, was.clone())
+        assert getattr(owner, name) is was
+        was.zero_()      # written to they may be
