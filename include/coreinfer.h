@@ -692,7 +692,7 @@ typedef struct {
  * (k_norm [D], NULL: not) and turned by their positions (rope, NULL: not), as
  * coreinfer_rope does; pos [T] or NULL: a token's position is its slot.  q [T, Hq, D] (or NULL, with
  * Hq = 0) goes the same way, with q_norm, to q_out [T, Hq, D] contiguous, 16-byte aligned, not
- * overlapping q.  Values are copied.  No two tokens may go to the same slot.
+ * overlapping q (CI_ERR_BAD_LAYOUT).  Values are copied.  No two tokens may go to the same slot.
  */
 int coreinfer_kvp_append(const ci_kvp* cache, const void* k, const void* v, const int64_t* stride, int64_t T,
                          const int32_t* first, const int32_t* lens, const int32_t* pos, const ci_rope* rope,
@@ -710,7 +710,7 @@ int coreinfer_kvp_append(const ci_kvp* cache, const void* k, const void* v, cons
  *   max_rows  the most rows of a sentence, max_len the most slots (<= most * page): they choose
  *             and size the launches.  lens beyond 0 .. max_len are taken as its ends; rows
  *             of a sentence from max_rows on are left as they are.
- *   out [T, Hq, D] contiguous, 16-byte aligned, not overlapping q.
+ *   out [T, Hq, D] contiguous, 16-byte aligned, not overlapping q (CI_ERR_BAD_LAYOUT).
  *   lse [T, Hq] fp32 or NULL: log of the sum of exp(scale q . k_t) (-infinity where nothing is seen).
  * scale > 0 and finite, also times log2(e).  Softmax statistics and sums in fp32, in a fixed order.
  * Probabilities enter the product with 16-bit values in two pieces of that type where few

@@ -23,6 +23,38 @@ bool rows_overlap(const int64_t* stride, int64_t a, int64_t b, int64_t D) {
   const int64_t inner = swap ? stride[0] : stride[1], outer = swap ? stride[1] : stride[0], n = swap ? a : b, m = swap ? b : a;
   return (n > 1 && inner < D) || (m > 1 && outer < (n > 1 ? (n - 1) * inner : 0) + D);
 }
+// Whether one of the T x H rows of `bytes` that begin stride[0], stride[1] bytes apart from p on has a byte in the block from .. from + size.
+bool rows_touch(const void* p, const int64_t (&stride)[2], int64_t T, int64_t H, int64_t bytes, const void* from, int64_t size) {
+  const int64_t at = (int64_t)reinterpret_cast<uintptr_t>(p), begin = (int64_t)reinterpret_cast<uintptr_t>(from), end = begin + size;
+  const bool swap = stride[0] < stride[1];
+  const int64_t inner = swap ? stride[0] : stride[1], outer = swap ? stride[1] : stride[0], n = swap ? T : H, m = swap ? H : T;
+  const int64_t extent = (n - 1) * inner + bytes;   // of the rows that are `inner` apart
+  if (end <= at || begin >= at + (m - 1) * outer + extent) return false;
+  // the first index from which on rows `step` apart from `a` on reach past `begin`
+  auto past = [&](int64_t a, int64_t length, int64_t step) { return a + length > begin || step == 0 ? 0 : (begin - a - length) / step + 1; };
+  for (int64_t i = past(at, extent, outer); i < m && at + i * outer < end; ++i) {
+    const int64_t a = at + i * outer, j = past(a, bytes, inner);
+    if (j < n && a + j * inner < end && a + j * inner + bytes > begin) return true;
+    if (outer == 0) break;
+  }
+  return false;
+}
+// Whether rows of D elements share a byte with the T H D elements from `out` on.
+bool touches(const void* p, const int64_t* stride, int64_t T, int64_t H, int64_t D, int dtype, const void* out) {
+  const int64_t e = elem_bytes(dtype);
+  return rows_touch(p, {stride[0] * e, stride[1] * e}, T, H, D * e, out, T * H * D * e);
+}
+// The same of two sets of rows with the same strides, or of which one is a block; others are not looked at.
+bool rope_overlap(const void* x, const int64_t* stride, int64_t T, int64_t H, int64_t D, int dtype, const void* y, const int64_t* y_stride, bool same) {
+  auto block = [&](const int64_t* s) { return (T == 1 || s[0] == H * D) && (H == 1 || s[1] == D); };
+  if (block(y_stride)) return touches(x, stride, T, H, D, dtype, y);
+  if (block(stride)) return touches(y, y_stride, T, H, D, dtype, x);
+  if (!same) return false;
+  // a row of one set on a row of the other: their distance on one of the differences between two rows of a set
+  const int64_t e = elem_bytes(dtype), back = ((T - 1) * stride[0] + (H - 1) * stride[1]) * e;
+  return rows_touch(reinterpret_cast<const void*>((uintptr_t)((int64_t)(uintptr_t)x - back)), {stride[0] * e, stride[1] * e}, 2 * T - 1, 2 * H - 1, D * e,
+                    y, D * e);
+}
 
 int rope_status(const ci_rope* r, int64_t D) {
   if (!r) return CI_OK;
@@ -87,7 +119,9 @@ int coreinfer_rope(const void* x, const int64_t* stride, int64_t T, int64_t H, i
       !word_aligned(pos))
     return CI_ERR_BAD_LAYOUT;
   if (rows_overlap(y_stride, T, H, D)) return CI_ERR_BAD_LAYOUT;
-  if (x == y && (stride[0] != y_stride[0] || stride[1] != y_stride[1])) return CI_ERR_BAD_LAYOUT;
+  // strides of lengths of one say nothing
+  const bool same = (T == 1 || stride[0] == y_stride[0]) && (H == 1 || stride[1] == y_stride[1]);
+  if (x == y ? !same : rope_overlap(x, stride, T, H, D, dtype, y, y_stride, same)) return CI_ERR_BAD_LAYOUT;
   return launch_rope(x, {stride[0], stride[1]}, T, H, D, dtype, norm, eps, rope, pos, backward != 0, y, {y_stride[0], y_stride[1]},
                      (hipStream_t)stream);
 }
@@ -109,6 +143,7 @@ int coreinfer_kvp_append(const ci_kvp* cache, const void* k, const void* v, cons
       !elem_aligned(q, dtype) || !elem_aligned(k_norm, dtype) || !elem_aligned(q_norm, dtype) || !aligned16(q_out) || !word_aligned(first) ||
       !word_aligned(lens) || !word_aligned(pos))
     return CI_ERR_BAD_LAYOUT;
+  if (q && touches(q, q_stride, T, Hq, cache->D, dtype, q_out)) return CI_ERR_BAD_LAYOUT;
   const int64_t none[2] = {0, 0};
   const int64_t* qs = q ? q_stride : none;
   return launch_kvp_append(*cache, k, v, {stride[0], stride[1]}, T, first, lens, pos, rope, k_norm, eps, q, Hq, {qs[0], qs[1]}, q_norm,
@@ -141,6 +176,7 @@ int coreinfer_kvp_attend(const ci_kvp* cache, const void* q, int64_t Hq, const i
     return CI_ERR_BAD_LAYOUT;
   if (need && (!ws || ws_bytes < need)) return CI_ERR_WORKSPACE;
   if (need && !aligned16(ws)) return CI_ERR_BAD_LAYOUT;
+  if (touches(q, stride, T, Hq, cache->D, cache->dtype, out)) return CI_ERR_BAD_LAYOUT;
   return launch_kvp_attend(*cache, q, Hq / cache->H, {stride[0], stride[1]}, T, first, lens, std::min(max_rows, T), max_len, window, sinks,
                            scale, out, lse, ws, (hipStream_t)stream);
 }

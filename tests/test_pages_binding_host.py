@@ -1,5 +1,7 @@
 """What the Python calls of rotary positions and the cache in pages refuse by themselves, without a GPU.  No call here may reach a launch."""
 
+import ctypes
+
 import pytest
 import torch
 
@@ -58,3 +60,25 @@ def test_tensors_whose_addresses_calls_go_by_are_not_replaced(lib):
             setattr(owner, name, was.clone())
         assert getattr(owner, name) is was
         was.zero_()      # written to they may be
+
+
+@pytest.mark.parametrize("stride", [(384, 128), (128, 512), (1024, 128)])
+def test_results_over_the_rows_that_they_come_from_are_refused(lib, stride):
+    """Addresses that no call may touch: each is refused for the overlap alone, which other distances show (on the GPU, where they run)."""
+    F, T, H, D = 1 << 20, 4, 3, 128
+    strides = (ctypes.c_int64 * 2)(*stride)
+    last = (T - 1) * stride[0] + (H - 1) * stride[1] + D      # elements
+    size = T * H * D
+    cache = ctypes.byref(lib.ci_kvp(F, F, F, 8, 4, 2, 3, 16, D, 1))
+    rope = ctypes.byref(lib.ci_rope(F, 1.0, 64, 0))
+    block = (ctypes.c_int64 * 2)(H * D, D)
+    for away in (0, 8, -8, D, last - 8, 8 - size):      # out from q on; 16-byte aligned
+        q = 4 * F
+        out = q + 2 * away
+        assert lib.raw.coreinfer_kvp_attend(cache, q, H, strides, T, F, F, 4, 64, 0, 0, 1.0, out, None, F, 1 << 40, None) == lib.CI_ERR_BAD_LAYOUT
+        assert lib.raw.coreinfer_kvp_append(cache, F, F, block, T, F, F, None, None, None, 0.0, q, H, strides, None, out, None) == lib.CI_ERR_BAD_LAYOUT
+        if away or stride[0] < stride[1]:      # in place it may be, with the same strides
+            assert lib.raw.coreinfer_rope(q, strides, T, H, D, 1, None, 0.0, rope, F, 0, out, block, None) == lib.CI_ERR_BAD_LAYOUT
+            assert lib.raw.coreinfer_rope(out, block, T, H, D, 1, None, 0.0, rope, F, 0, q, strides, None) == lib.CI_ERR_BAD_LAYOUT
+    for away in (1, -1, 127, stride[0] - 127, stride[0] + stride[1] + 5, last - 1, 1 - last):
+        assert lib.raw.coreinfer_rope(4 * F, strides, T, H, D, 1, None, 0.0, rope, F, 0, 4 * F + 2 * away, strides, None) == lib.CI_ERR_BAD_LAYOUT
