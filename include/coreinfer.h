@@ -644,7 +644,7 @@ typedef struct {
  *     CI_ROPE_PARTS   f_i (g + (1 - g) / factor), g = (original f_i / (2 pi) - slow) /
  *                     (fast - slow) within 0 .. 1: pairs that turn more than `fast` times in the
  *                     `original` context stay, those below `slow` are squeezed (Peng et al.
- *                     2023, who also scale by 0.1 ln(factor) + 1: ci_rope's scale)
+ *                     2023, who also scale by 0.1 ln(factor) + 1 where factor > 1: ci_rope's scale)
  * Host-only.  rot even, 2 .. 512; base > 0; factor > 0 (not looked at for CI_ROPE_PLAIN);
  * original > 0 and fast > slow for CI_ROPE_PARTS only; everything finite.
  */

@@ -923,10 +923,10 @@ def rope_angles(rot: int, base: float = 10000.0, style: str = "half", scaling: s
                 device="cuda") -> RopeAngles:
     """Angles of the first `rot` channels of each head: pairs of channels rot / 2 apart ("half") or of neighbours
     ("interleaved"); scaling "none", "linear", "base" or "parts" for a context `factor` times as long as `original`.  scale:
-    of the turned channels; by default 1, and 0.1 ln(factor) + 1 for "parts"."""
+    of the turned channels; by default 1, and 0.1 ln(factor) + 1 for "parts" where the context is longer, factor > 1."""
     turns = rope_turns(rot, base, scaling, factor, original, fast, slow).to(device)
     if scale is None:
-        scale = 0.1 * math.log(factor) + 1.0 if scaling == "parts" else 1.0
+        scale = 0.1 * math.log(factor) + 1.0 if scaling == "parts" and factor > 1.0 else 1.0
     return RopeAngles(turns, float(scale), int(rot), style)
 
 

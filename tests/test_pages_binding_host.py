@@ -1,6 +1,7 @@
 """What the Python calls of rotary positions and the cache in pages refuse by themselves, without a GPU.  No call here may reach a launch."""
 
 import ctypes
+import math
 
 import pytest
 import torch
@@ -82,3 +83,11 @@ def test_results_over_the_rows_that_they_come_from_are_refused(lib, stride):
             assert lib.raw.coreinfer_rope(out, block, T, H, D, 1, None, 0.0, rope, F, 0, q, strides, None) == lib.CI_ERR_BAD_LAYOUT
     for away in (1, -1, 127, stride[0] - 127, stride[0] + stride[1] + 5, last - 1, 1 - last):
         assert lib.raw.coreinfer_rope(4 * F, strides, T, H, D, 1, None, 0.0, rope, F, 0, 4 * F + 2 * away, strides, None) == lib.CI_ERR_BAD_LAYOUT
+
+
+@pytest.mark.parametrize("factor,scale", [(4.0, 0.1 * math.log(4.0) + 1.0), (1.0, 1.0), (0.5, 1.0), (1e-6, 1.0)])
+def test_the_scale_of_parts_is_that_of_longer_contexts(lib, factor, scale):
+    """A factor of 1e-6 would make it -0.38, and turn the heads over."""
+    kw = dict(scaling="parts", factor=factor, original=4096.0, device="cpu")
+    assert lib.rope_angles(64, **kw).scale == scale
+    assert lib.rope_angles(64, scale=0.75, **kw).scale == 0.75
