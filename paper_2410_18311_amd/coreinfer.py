@@ -1068,7 +1068,7 @@ def kvp_attend(q: torch.Tensor, cache: KvpCache, first: torch.Tensor, lens: torc
     device = cache.device
     assert out.shape == shape and out.dtype is dtype and out.is_contiguous() and out.get_device() == device
     assert lse is None or (lse.shape == (T, Hq) and lse.dtype is torch.float32 and lse.is_contiguous() and lse.get_device() == device)
-    assert ws is None or ws.get_device() == device
+    assert ws is None or (ws.get_device() == device and ws.is_contiguous())
     assert device >= 0, _HOST
     if ws is None:
         need = kvp_attend_workspace_size(cache, T, Hq, max_rows, max_len, window, sinks)

@@ -91,3 +91,12 @@ def test_the_scale_of_parts_is_that_of_longer_contexts(lib, factor, scale):
     kw = dict(scaling="parts", factor=factor, original=4096.0, device="cpu")
     assert lib.rope_angles(64, **kw).scale == scale
     assert lib.rope_angles(64, scale=0.75, **kw).scale == 0.75
+
+
+def test_a_workspace_with_fewer_bytes_than_elements_is_refused(lib):
+    """An expanded tensor has one element's memory."""
+    cache, x, first, lens, _ = _host(lib)
+    for ws in (torch.empty(1, dtype=torch.uint8).expand(1 << 20), torch.empty(1 << 21, dtype=torch.uint8)[::2]):
+        with pytest.raises(AssertionError) as e:
+            lib.kvp_attend(x, cache, first, lens, ws=ws)
+        assert "host memory" not in str(e.value)
