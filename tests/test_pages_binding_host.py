@@ -1,6 +1,7 @@
 """What the Python calls of rotary positions and the cache in pages refuse by themselves, without a GPU.  No call here may reach a launch."""
 
 import ctypes
+import importlib.util
 import math
 
 import pytest
@@ -100,3 +101,43 @@ def test_a_workspace_with_fewer_bytes_than_elements_is_refused(lib):
         with pytest.raises(AssertionError) as e:
             lib.kvp_attend(x, cache, first, lens, ws=ws)
         assert "host memory" not in str(e.value)
+
+
+@pytest.fixture(scope="module")
+def plain(lib):
+    """The module as it is where the C module was not built."""
+    from paper_2410_18311_amd import build
+    was, build.BINDING_PATH = build.BINDING_PATH, "/nonexistent"
+    try:
+        spec = importlib.util.spec_from_file_location("paper_2410_18311_amd.coreinfer_plain", lib.__file__)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+    finally:
+        build.BINDING_PATH = was
+    assert module._binding is None
+    return module
+
+
+def test_calls_through_ctypes_say_the_same(lib, plain):
+    """Every argument in its place: no rows are nothing to do, and each refusal is the C module's."""
+    F = 1 << 20
+    angles, cache = lib.ci_rope(F, 1.0, 64, 0), lib.ci_kvp(F, F, F, 8, 1024, 2, 3, 16, 128, 1)
+    r, c = ctypes.addressof(angles), ctypes.addressof(cache)
+    rope = [F, 384, 128, 4, 3, 128, 1, None, 1e-6, r, F, 0, 4 * F, 384, 128, None]
+    append = [c, F, F, 384, 128, 4, F, F, None, r, None, 1e-6, F, 3, 384, 128, None, 4 * F, None]
+    attend = [c, F, 6, 768, 128, 4, F, F, 4, 16384, 0, 0, 1.0, 4 * F, None, F, 1 << 40, None]
+    ok, size, layout = lib.CI_OK, lib.CI_ERR_INVALID_ARG, lib.CI_ERR_BAD_LAYOUT
+    for name, args, T, changes in (
+            ("_rope_call", rope, 3, {0: (F + 1, layout), 1: (-1, layout), 2: (-1, layout), 4: (0, size), 5: (0, size), 6: (7, lib.CI_ERR_BAD_DTYPE),
+                                     7: (F + 1, layout), 9: (ctypes.addressof(lib.ci_rope(F, 1.0, 63, 0)), size), 10: (None, size), 12: (F + 2, layout),
+                                     13: (0, layout), 14: (0, layout)}),
+            ("_kvp_append_call", append, 5, {0: (None, size), 1: (F + 1, layout), 2: (None, size), 3: (-1, layout), 4: (-1, layout), 6: (None, size),
+                                             7: (F + 1, layout), 8: (F + 1, layout), 10: (F + 1, layout), 12: (None, size), 13: (-1, size),
+                                             14: (-1, layout), 15: (-1, layout), 16: (F + 1, layout), 17: (F, layout)}),
+            ("_kvp_attend_call", attend, 5, {0: (None, size), 1: (F + 1, layout), 2: (5, size), 3: (-1, layout), 4: (-1, layout), 6: (F + 1, layout),
+                                             7: (None, size), 8: (0, size), 9: (0, size), 10: (-1, size), 11: (-1, size), 12: (math.nan, size),
+                                             13: (F, layout), 14: (F + 1, layout), 15: (None, lib.CI_ERR_WORKSPACE),
+                                             16: (0, lib.CI_ERR_WORKSPACE)})):
+        for at, (value, status) in {**changes, T: (0, ok)}.items():
+            call = args[:at] + [value] + args[at + 1:]
+            assert getattr(lib, name)(*call) == getattr(plain, name)(*call) == status, (name, at)
