@@ -707,6 +707,8 @@ int coreinfer_kvp_append(const ci_kvp* cache, const void* k, const void* v, cons
  * and t < sinks.  A row that sees none gives zeros.  What it does not see, infinities and NaN
  * included, does not touch it.  A logit of +infinity or NaN that it sees gives NaN, in lse too;
  * where all that it sees are -infinity, it gives NaN, and lse -infinity.
+ * An infinite value that it sees gives that infinity, whatever its weight; values that are not finite cost
+ * the rows that meet them, seen or not, a second time through, of a few times the first's time.
  *   max_rows  the most rows of a sentence, max_len the most slots (<= most * page): they choose
  *             and size the launches.  lens beyond 0 .. max_len are taken as its ends; rows
  *             of a sentence from max_rows on are left as they are.
@@ -714,7 +716,9 @@ int coreinfer_kvp_append(const ci_kvp* cache, const void* k, const void* v, cons
  *   lse [T, Hq] fp32 or NULL: log of the sum of exp(scale q . k_t) (-infinity where nothing is seen).
  * scale > 0 and finite, also times log2(e).  Softmax statistics and sums in fp32, in a fixed order.
  * Probabilities enter the product with 16-bit values in two pieces of that type where few
- * rows share a head, and rounded to it in prompts.
+ * rows share a head, and rounded to it once in prompts: with R = min(max_rows, T) Hq / H, where
+ * R > 64, or R > 16 and B H ceil(R / 16) max_len >= 196608, but for sentences of up to 16 rows a head
+ * if T < B max_rows.  max_rows and max_len choose the last bits of a result by that rule.
  * ws: coreinfer_kvp_attend_workspace_size bytes, 16-byte aligned; NULL where that is 0.  Calls
  * that share a workspace must not overlap in time.
  * window, sinks >= 0.  Hq / H <= 4096, T * Hq <= 2^30.

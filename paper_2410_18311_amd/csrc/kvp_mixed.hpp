@@ -1,6 +1,6 @@
 // Attention of prompts and single tokens together over a cache in pages (kvp_attend.hpp): one launch of both kinds of workgroups, so that those that
 // wait for the cache's bytes run beside those that keep the matrix cores busy, and one that joins the pieces of both.  777 rows and
-// six single tokens of 32 heads over up to 8192 slots: 97 us; with the two kinds in launches of their own 122, with the single tokens spread among
+// six single tokens of 32 heads over up to 8192 slots: 97 to 101 us; with the two kinds in launches of their own 122, with the single tokens spread among
 // the tiles 120, because tiles that start late end late.
 #pragma once
 

@@ -6,8 +6,8 @@
 // fp32 caches go through fp32 products as they are.
 //
 // Eight sentences to 65536 slots, 8 x 8 heads of 128, bf16: 178 us for 973 MB, 5.5 TB/s (a copy of 1 GiB: 5.2), of which the join takes 6.  4096 slots
-// of 40 heads: 20.5 us for 84 MB, 4 of them the join.  fp32 prompts take this way too, 16 rows a workgroup, at 68 TFLOP/s (4096 tokens of 32 heads
-// of 128: 2031 us), where a library product reaches 153: each tile reads the cache from the L2 again.
+// of 40 heads: 20.5 us for 84 MB, 4 of them the join.  fp32 prompts take this way too, 16 rows a workgroup, at 70 TFLOP/s (4096 tokens of 32 heads
+// of 128: 1940 to 1990 us), where a library product reaches 153: each tile reads the cache from the L2 again.
 #pragma once
 
 #include "kvp_walk.hpp"

@@ -8,7 +8,9 @@
 // Weights are rounded to the cache's type, as the matrix cores take it: half a unit of a weight, averaged over the slots.  Their sum is that
 // of the rounded ones, so that a row's weights add up to 1; the log-sum, when asked for, is of the exact ones.
 //
-// 4096 tokens of 32 heads of 128, fp16, causal: 150 to 155 us, 0.9 PFLOP/s of the visible half, where a large product of the library reaches 1.2.  The matrix
+// 4096 tokens of 32 heads of 128, fp16, causal: 152 to 160 us (the first forty calls of a run up to 203, as the clock is regulated), 0.86 to 0.9 PFLOP/s of the visible half,
+// where a large product of the library reaches 1.17 to 1.2.  The LDS's reads are as high a bound as the products: 32 KB a wave and step, 2048 cycles for a
+// compute unit's eight waves, whose products take as many.  The matrix
 // cores are busy for 44 % of the cycles and vector instructions (4.5 a logit, one of them an exponential) take most of the others; the two
 // overlap little: of 32 products in 1030 cycles, reading their operands from the LDS makes 1290 and the next step's loads 1540.
 // Also measured, the same case: 256 rows in eight waves, whose halves take turns at products and softmax, 161 us; 64 rows a wave, one wave a SIMD,
